@@ -297,6 +297,137 @@ int pisa_selection_quality(const pisa_problem* p, const void* q, const void* k, 
                            const int32_t* rows, int32_t n_rows, float* metrics, int32_t* ref_idx, void* ws,
                            size_t ws_bytes, pisa_stream_t stream);
 
+/* ---- Rotary positions ------------------------------------------------------
+ *
+ * Queries and keys get their positions before the pyramid is built from the
+ * keys: the first `rot` dimensions of a head form rot/2 pairs, and pair i of
+ * the row at position t is turned by the angle t * freq[i] and multiplied by
+ * `amplitude`; dimensions from `rot` on are copied. */
+
+/* Strides, in elements, of a [B, heads, rows, d] tensor whose last dimension is
+ * contiguous, so that a projection's [B, rows, heads, d] is read (or written)
+ * as it stands.  Non-negative multiples of 16 bytes.  A NULL pisa_strides means
+ * the contiguous [B, heads, rows, d]. */
+typedef struct {
+  int64_t b, h, n;
+} pisa_strides;
+
+enum {
+  PISA_ROPE_HALF = 0,       /* pair i: dimensions i and i + rot/2 */
+  PISA_ROPE_INTERLEAVED = 1 /* pair i: dimensions 2i and 2i + 1   */
+};
+
+/* How pisa_rope_frequencies adapts the frequencies f_i = base^(-2i/rot) to a
+ * context `factor` times as long as the original one. */
+enum {
+  PISA_ROPE_SCALE_NONE = 0,
+  PISA_ROPE_SCALE_LINEAR = 1, /* f_i / factor                                     */
+  PISA_ROPE_SCALE_BASE = 2,   /* base * factor^(rot/(rot-2)) in base's place: the
+                                 slowest pair is slowed by factor, the fastest not */
+  PISA_ROPE_SCALE_PARTS = 3   /* f_i (y + (1-y)/factor), y = (turns - slow) /
+                                 (fast - slow) cut to [0, 1], turns = ctx f_i / 2 pi:
+                                 pairs that turn often within the original context
+                                 keep their frequency, slow ones are interpolated;
+                                 amplitude = 0.1 ln(factor) + 1                    */
+};
+
+#define PISA_ROPE_MAX_PAIRS 64
+
+/* q, q_out: [B, H, N, d]; k, k_out: [B, Hkv, N, d], any of H >= 1, Hkv >= 1.
+ * d in {64, 128}; rot even, 2 <= rot <= d.  Row n of batch b is at position
+ * pos0 + n, or where the call has `positions` (device int32) at
+ * positions[b * pos_bstride + n]; pos_bstride = 0 shares one list among the
+ * batch.  Positions may be negative.  Angles are computed in 64 bits and
+ * reduced before the sine, so far positions lose nothing. */
+typedef struct {
+  int32_t B, H, Hkv, N, d;
+  int32_t rot;
+  int32_t layout; /* PISA_ROPE_HALF / _INTERLEAVED                    */
+  int32_t dtype;  /* pisa_dtype of every tensor                       */
+  int32_t pos0;
+  int32_t reserved; /* 0 */
+  int64_t pos_bstride;
+  double amplitude;
+  double freq[PISA_ROPE_MAX_PAIRS]; /* radians per position; rot/2 are used */
+} pisa_rope;
+
+/* Fills r->freq and r->amplitude from r->rot (host only).  base > 1; factor >=
+ * 1; PARTS also takes ctx >= 1 (tokens of the original context) and
+ * fast > slow >= 0 (turns); the other scalings ignore them. */
+int pisa_rope_frequencies(pisa_rope* r, double base, int32_t scaling, double factor, int32_t ctx, double fast,
+                          double slow);
+
+/* Turns q and k (either may be NULL together with its output) in one launch.
+ * An output may be its own input (same pointer and strides); otherwise outputs
+ * overlap neither inputs nor each other.  Arithmetic in float32, rounded once. */
+int pisa_rope_fwd(const pisa_rope* r, const void* q, const pisa_strides* q_strides, const void* k,
+                  const pisa_strides* k_strides, const int32_t* positions, void* q_out,
+                  const pisa_strides* q_out_strides, void* k_out, const pisa_strides* k_out_strides,
+                  pisa_stream_t stream);
+
+/* Gradients of pisa_rope_fwd: d_q and d_k from the gradients of its outputs (the
+ * transposed map: turned back, times the same amplitude). */
+int pisa_rope_bwd(const pisa_rope* r, const void* d_q_out, const pisa_strides* d_q_out_strides, const void* d_k_out,
+                  const pisa_strides* d_k_out_strides, const int32_t* positions, void* d_q,
+                  const pisa_strides* d_q_strides, void* d_k, const pisa_strides* d_k_strides, pisa_stream_t stream);
+
+/* ---- 8-bit key/value cache --------------------------------------------------
+ *
+ * Keys and values in e4m3 (4 exponent, 3 mantissa bits, largest 448), one scale
+ * for each leaf block of C tokens and KV head, keys and values apart.  A scale
+ * is the smallest power of two 2^e, e >= -100, with max|x| <= 448 * 2^e over the
+ * block's finite values, so scaling never rounds and code * scale is exact in
+ * bf16; the code is x / 2^e rounded to nearest even.  Infinities and NaN become
+ * the NaN code.  Half the bytes of a bf16 cache.
+ *
+ * With M = ceil(Ncap / C) blocks (Ncap = 0 means N):
+ *   k        [B, Hkv, M, C, d]  codes
+ *   v        [B, Hkv, M, d, C]  codes, a block's tokens contiguous: the order
+ *                               in which the attention's matrix product reads them
+ *   k_scale, v_scale  [B, Hkv, M] float32
+ *   k_open, v_open    [B, Hkv, C, d] in the problem dtype: the raw rows of the
+ *                     last block, from which it is quantised anew as it fills, so
+ *                     that the cache does not depend on how it was appended to
+ *                     (pisa_qcache_append only; NULL elsewhere is fine)
+ */
+typedef struct {
+  void* k;
+  void* v;
+  float* k_scale;
+  float* v_scale;
+  void* k_open;
+  void* v_open;
+} pisa_qcache;
+
+/* Blocks M per (batch, KV head), and bytes of each code buffer (B*Hkv*M*C*d);
+ * a negative status, 0 for an invalid problem. */
+int32_t pisa_qcache_blocks(const pisa_problem* p);
+size_t pisa_qcache_bytes(const pisa_problem* p);
+
+/* Appends rows [n_old, N): k_new, v_new hold those rows, [B, Hkv, N - n_old, d]
+ * in the problem dtype (strides as in pisa_strides).  The cache holds the first
+ * n_old rows, as left by earlier appends with the same C and Ncap, and
+ * k_open, v_open the raw rows of the block of row n_old - 1 (of n_old, where it
+ * is a multiple of C, none are read).  Blocks from n_old / C on are quantised,
+ * codes of tokens past N in the last of them written as 0; afterwards k_open,
+ * v_open start with the raw rows of the last block (their other rows are left).
+ * The result equals one append of all N rows bit for bit.  pyramid (nullable):
+ * the mean pyramid of the raw keys for the same fanout and Ncap, brought from
+ * n_old to N, bit for bit as pisa_build_pyramid has it.  k_new and v_new must
+ * not overlap the cache.  0 <= n_old <= N; n_old = N does nothing.  No
+ * workspace; one launch where a single block changes and no level is new. */
+int pisa_qcache_append(const pisa_problem* p, const pisa_qcache* c, const void* k_new, const pisa_strides* k_strides,
+                       const void* v_new, const pisa_strides* v_strides, int32_t n_old, float* pyramid,
+                       pisa_stream_t stream);
+
+/* pisa_sparse_attn_fwd over the cache: the same result as over keys and values
+ * code * scale, up to fp32 rounding order.  Entries of block_idx as there; a row
+ * with no visible token gets o = 0 and lse = -inf; tokens that the causal mask or
+ * N hides are not used, whatever their codes.  o and lse (nullable) as there. */
+size_t pisa_qcache_attn_workspace_bytes(const pisa_problem* p);
+int pisa_qcache_attn_fwd(const pisa_problem* p, const pisa_qcache* c, const void* q, const int32_t* block_idx, void* o,
+                         float* lse, void* ws, size_t ws_bytes, pisa_stream_t stream);
+
 /* Per-kernel timing for benchmarks (not needed for computing anything).
  * pisa_profile_enable(1) makes every later call bracket each kernel it
  * launches with two hipEvents recorded on that call's stream (host-side

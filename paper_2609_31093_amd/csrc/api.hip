@@ -325,6 +325,102 @@ int static_scratch(void** out) {
   return PISA_OK;
 }
 
+// Strides of a [B, heads, rows, d] tensor (the contiguous ones where NULL).
+// Written tensors keep their rows apart.
+int check_strides(const pisa_strides* in, const char* name, int64_t B, int64_t heads, int64_t rows, int d, int dtype,
+                  bool written, pisa_strides* out) {
+  if (!in) {
+    *out = pisa_strides{heads * rows * d, rows * d, d};
+    return PISA_OK;
+  }
+  const int unit = dtype == PISA_DTYPE_BF16 ? 8 : 4;
+  for (const int64_t x : {in->b, in->h, in->n})
+    if (x < 0 || x % unit != 0)
+      return fail(PISA_ERR_INVALID_ARG, "strides of %s must be non-negative multiples of 16 bytes (got %lld elements)", name,
+                  static_cast<long long>(x));
+  if (written && ((B > 1 && in->b < d) || (heads > 1 && in->h < d) || (rows > 1 && in->n < d)))
+    return fail(PISA_ERR_INVALID_ARG, "strides of %s make its rows overlap", name);
+  *out = *in;
+  return PISA_OK;
+}
+
+int check_rope(const pisa_rope* r) {
+  if (!r) return fail(PISA_ERR_INVALID_ARG, "rope is NULL");
+  if (r->B < 1 || r->H < 1 || r->Hkv < 1 || r->N < 1)
+    return fail(PISA_ERR_INVALID_ARG, "B, H, Hkv and N must be >= 1 (got %d, %d, %d, %d)", r->B, r->H, r->Hkv, r->N);
+  if (r->d != 64 && r->d != 128) return fail(PISA_ERR_UNSUPPORTED, "head dim %d (supported: 64, 128)", r->d);
+  if (r->rot < 2 || r->rot > r->d || r->rot % 2 != 0)
+    return fail(PISA_ERR_INVALID_ARG, "rot must be even and in [2, d] (got %d, d=%d)", r->rot, r->d);
+  if (r->layout != PISA_ROPE_HALF && r->layout != PISA_ROPE_INTERLEAVED)
+    return fail(PISA_ERR_INVALID_ARG, "unknown layout %d", r->layout);
+  if (r->dtype != PISA_DTYPE_F32 && r->dtype != PISA_DTYPE_BF16)
+    return fail(PISA_ERR_INVALID_ARG, "unknown dtype %d", r->dtype);
+  if (r->reserved != 0) return fail(PISA_ERR_INVALID_ARG, "reserved must be 0");
+  if (r->pos_bstride < 0) return fail(PISA_ERR_INVALID_ARG, "pos_bstride must be >= 0");
+  if (!isfinite(r->amplitude)) return fail(PISA_ERR_INVALID_ARG, "amplitude is not finite");
+  for (int i = 0; i < r->rot / 2; ++i)
+    if (!(fabs(r->freq[i]) <= 1e6)) return fail(PISA_ERR_INVALID_ARG, "freq[%d] is not a number within 10^6", i);
+  if (static_cast<int64_t>(r->pos0) + r->N > INT32_MAX) return fail(PISA_ERR_UNSUPPORTED, "positions past 2^31-1");
+  if (static_cast<int64_t>(r->B) * r->N > (int64_t(1) << 28)) return fail(PISA_ERR_UNSUPPORTED, "B*N exceeds 2^28");
+  if (static_cast<int64_t>(r->H) + r->Hkv > 65535) return fail(PISA_ERR_UNSUPPORTED, "H + Hkv exceeds 65535");
+  return PISA_OK;
+}
+
+// One side (queries or keys) of a rotation; both pointers NULL leave it out.
+int check_rope_side(const pisa_rope* r, const char* name, int heads, const void* in, const pisa_strides* is, void* out,
+                    const pisa_strides* os, pisa::RopeSide* side) {
+  if (!in && !out) return PISA_OK;
+  char nout[32];
+  snprintf(nout, sizeof(nout), "%s (output)", name);
+  PISA_TRY(check_ptr(in, name));
+  PISA_TRY(check_ptr(out, nout));
+  pisa_strides si, so;
+  PISA_TRY(check_strides(is, name, r->B, heads, r->N, r->d, r->dtype, false, &si));
+  PISA_TRY(check_strides(os, nout, r->B, heads, r->N, r->d, r->dtype, true, &so));
+  if (in == out && ((r->B > 1 && si.b != so.b) || (heads > 1 && si.h != so.h) || (r->N > 1 && si.n != so.n)))
+    return fail(PISA_ERR_INVALID_ARG, "%s in place needs the same strides for input and output", name);
+  *side = pisa::RopeSide{in, out, si.b, si.h, si.n, so.b, so.h, so.n};
+  return PISA_OK;
+}
+
+int run_rope(const pisa_rope* r, const void* q, const pisa_strides* qs, const void* k, const pisa_strides* ks,
+             const int32_t* positions, void* qo, const pisa_strides* qos, void* ko, const pisa_strides* kos, float sign,
+             pisa_stream_t stream, const char* who) {
+  PISA_TRY(check_rope(r));
+  pisa::RopeArgs a{};
+  PISA_TRY(check_rope_side(r, "q", r->H, q, qs, qo, qos, &a.q));
+  PISA_TRY(check_rope_side(r, "k", r->Hkv, k, ks, ko, kos, &a.k));
+  if (!q && !k) return fail(PISA_ERR_INVALID_ARG, "neither q nor k given");
+  if (positions && (reinterpret_cast<uintptr_t>(positions) & 3u))
+    return fail(PISA_ERR_INVALID_ARG, "positions is not 4-byte aligned");
+  a.positions = positions;
+  a.pos_bstride = r->pos_bstride;
+  a.B = r->B;
+  a.H = q ? r->H : 0;
+  a.HH = a.H + (k ? r->Hkv : 0);
+  a.N = r->N;
+  a.d = r->d;
+  a.rot = r->rot;
+  a.pos0 = r->pos0;
+  a.amplitude = static_cast<float>(r->amplitude);
+  a.sign = sign;
+  for (int i = 0; i < r->rot / 2; ++i) a.turn[i] = r->freq[i] / 6.283185307179586476925286766559;
+  return device_status(pisa::launch_rope(a, r->dtype == PISA_DTYPE_BF16, r->layout == PISA_ROPE_HALF,
+                                         static_cast<hipStream_t>(stream)),
+                       who);
+}
+
+int check_qcache(const pisa_qcache* c, const pisa::Geo& g, pisa::QCache* out) {
+  if (!c) return fail(PISA_ERR_INVALID_ARG, "cache is NULL");
+  PISA_TRY(check_ptr(c->k, "cache k"));
+  PISA_TRY(check_ptr(c->v, "cache v"));
+  PISA_TRY(check_ptr(c->k_scale, "k_scale"));
+  PISA_TRY(check_ptr(c->v_scale, "v_scale"));
+  *out = pisa::QCache{static_cast<uint8_t*>(c->k), static_cast<uint8_t*>(c->v), c->k_scale, c->v_scale,
+                      (g.Nkv + g.C - 1) / g.C};
+  return PISA_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -590,6 +686,122 @@ int pisa_selection_quality(const pisa_problem* p, const void* q, const void* k, 
   return device_status(pisa::launch_quality(s, q, k, block_idx, rows, n_rows, metrics, ref_idx, ws,
                                             static_cast<hipStream_t>(stream)),
                        "pisa_selection_quality");
+}
+
+int pisa_rope_frequencies(pisa_rope* r, double base, int32_t scaling, double factor, int32_t ctx, double fast,
+                          double slow) {
+  if (!r) return fail(PISA_ERR_INVALID_ARG, "rope is NULL");
+  if (r->rot < 2 || r->rot > 2 * PISA_ROPE_MAX_PAIRS || r->rot % 2 != 0)
+    return fail(PISA_ERR_INVALID_ARG, "rot must be even and in [2, %d] (got %d)", 2 * PISA_ROPE_MAX_PAIRS, r->rot);
+  if (!(base > 1.0) || !isfinite(base)) return fail(PISA_ERR_INVALID_ARG, "base must be > 1");
+  if (!(factor >= 1.0) || !isfinite(factor)) return fail(PISA_ERR_INVALID_ARG, "factor must be >= 1");
+  if (scaling < PISA_ROPE_SCALE_NONE || scaling > PISA_ROPE_SCALE_PARTS)
+    return fail(PISA_ERR_INVALID_ARG, "unknown scaling %d", scaling);
+  if (scaling == PISA_ROPE_SCALE_BASE && r->rot == 2)
+    return fail(PISA_ERR_INVALID_ARG, "scaling the base needs rot > 2");
+  const bool parts = scaling == PISA_ROPE_SCALE_PARTS;
+  if (parts && (ctx < 1 || !(slow >= 0.0) || !(fast > slow) || !isfinite(fast)))
+    return fail(PISA_ERR_INVALID_ARG, "scaling by parts needs ctx >= 1 and fast > slow >= 0");
+  const int pairs = r->rot / 2;
+  if (scaling == PISA_ROPE_SCALE_BASE) base *= pow(factor, static_cast<double>(r->rot) / (r->rot - 2));
+  for (int i = 0; i < PISA_ROPE_MAX_PAIRS; ++i) {
+    double f = i < pairs ? pow(base, -2.0 * i / r->rot) : 0.0;
+    if (scaling == PISA_ROPE_SCALE_LINEAR) f /= factor;
+    if (parts) {
+      const double y = std::min(1.0, std::max(0.0, (ctx * f / 6.283185307179586476925286766559 - slow) / (fast - slow)));
+      f *= y + (1.0 - y) / factor;
+    }
+    r->freq[i] = f;
+  }
+  r->amplitude = parts ? 0.1 * log(factor) + 1.0 : 1.0;
+  return PISA_OK;
+}
+
+int pisa_rope_fwd(const pisa_rope* r, const void* q, const pisa_strides* q_strides, const void* k,
+                  const pisa_strides* k_strides, const int32_t* positions, void* q_out,
+                  const pisa_strides* q_out_strides, void* k_out, const pisa_strides* k_out_strides,
+                  pisa_stream_t stream) {
+  return run_rope(r, q, q_strides, k, k_strides, positions, q_out, q_out_strides, k_out, k_out_strides, 1.f, stream,
+                  "pisa_rope_fwd");
+}
+
+int pisa_rope_bwd(const pisa_rope* r, const void* d_q_out, const pisa_strides* d_q_out_strides, const void* d_k_out,
+                  const pisa_strides* d_k_out_strides, const int32_t* positions, void* d_q,
+                  const pisa_strides* d_q_strides, void* d_k, const pisa_strides* d_k_strides, pisa_stream_t stream) {
+  return run_rope(r, d_q_out, d_q_out_strides, d_k_out, d_k_out_strides, positions, d_q, d_q_strides, d_k, d_k_strides,
+                  -1.f, stream, "pisa_rope_bwd");
+}
+
+int32_t pisa_qcache_blocks(const pisa_problem* p) {
+  pisa::Geo g{};
+  PISA_TRY(check_problem(p, nullptr, &g));
+  return (g.Nkv + g.C - 1) / g.C;
+}
+
+size_t pisa_qcache_bytes(const pisa_problem* p) {
+  pisa::Geo g{};
+  if (check_problem(p, nullptr, &g) != PISA_OK) return 0;
+  return static_cast<size_t>(p->B) * p->Hkv * ((g.Nkv + g.C - 1) / g.C) * g.C * p->d;
+}
+
+int pisa_qcache_append(const pisa_problem* p, const pisa_qcache* c, const void* k_new, const pisa_strides* k_strides,
+                       const void* v_new, const pisa_strides* v_strides, int32_t n_old, float* pyramid,
+                       pisa_stream_t stream) {
+  pisa::Shape s{};
+  pisa::Geo g{};
+  pisa::QAppend a{};
+  PISA_TRY(check_problem(p, &s, &g));
+  PISA_TRY(check_qcache(c, g, &a.c));
+  PISA_TRY(check_ptr(c->k_open, "k_open"));
+  PISA_TRY(check_ptr(c->v_open, "v_open"));
+  PISA_TRY(check_ptr(pyramid, "pyramid", true));
+  if (n_old < 0 || n_old > p->N) return fail(PISA_ERR_INVALID_ARG, "need 0 <= n_old <= N (got %d, N=%d)", n_old, p->N);
+  if (n_old == p->N) return PISA_OK;
+  PISA_TRY(check_ptr(k_new, "k_new"));
+  PISA_TRY(check_ptr(v_new, "v_new"));
+  pisa_strides ks, vs;
+  PISA_TRY(check_strides(k_strides, "k_new", p->B, p->Hkv, p->N - n_old, p->d, p->dtype, false, &ks));
+  PISA_TRY(check_strides(v_strides, "v_new", p->B, p->Hkv, p->N - n_old, p->d, p->dtype, false, &vs));
+  a.k_new = k_new;
+  a.v_new = v_new;
+  a.ksb = ks.b;
+  a.ksh = ks.h;
+  a.ksn = ks.n;
+  a.vsb = vs.b;
+  a.vsh = vs.h;
+  a.vsn = vs.n;
+  a.k_open = c->k_open;
+  a.v_open = c->v_open;
+  a.pyr = pyramid;
+  a.Hkv = p->Hkv;
+  a.n_old = n_old;
+  pisa::Geo g_old{};
+  if (n_old > 0) compute_geo(n_old, p->C, p->fanout, &g_old, g.Nkv);
+  return device_status(pisa::launch_qcache_append(g, g_old, s.BH(), s.D, s.bf16, a, static_cast<hipStream_t>(stream)),
+                       "pisa_qcache_append");
+}
+
+size_t pisa_qcache_attn_workspace_bytes(const pisa_problem* p) {
+  pisa::Shape s{};
+  pisa::Geo g{};
+  if (check_problem(p, &s, &g) != PISA_OK) return 0;
+  return pisa::qcache_attn_ws(s, g);
+}
+
+int pisa_qcache_attn_fwd(const pisa_problem* p, const pisa_qcache* c, const void* q, const int32_t* block_idx, void* o,
+                         float* lse, void* ws, size_t ws_bytes, pisa_stream_t stream) {
+  pisa::Shape s{};
+  pisa::Geo g{};
+  pisa::QCache qc{};
+  PISA_TRY(check_problem(p, &s, &g));
+  PISA_TRY(check_qcache(c, g, &qc));
+  PISA_TRY(check_ptr(q, "q"));
+  PISA_TRY(check_ptr(block_idx, "block_idx"));
+  PISA_TRY(check_ptr(o, "o"));
+  PISA_TRY(check_ptr(lse, "lse", true));
+  PISA_TRY(check_ws(ws, ws_bytes, pisa::qcache_attn_ws(s, g)));
+  return device_status(pisa::launch_qcache_attn(s, g, qc, q, block_idx, o, lse, ws, static_cast<hipStream_t>(stream)),
+                       "pisa_qcache_attn_fwd");
 }
 
 const char* pisa_status_string(int status) {

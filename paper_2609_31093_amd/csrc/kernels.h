@@ -162,4 +162,49 @@ size_t bsa_ws(const Shape& s, const Geo& geo);
 hipError_t launch_flat_bsa(const Shape& s, const Geo& geo, const void* q, const float* pyr, int32_t* idx,
                            void* ws, hipStream_t st);
 
+// Rotary positions (rope.hip).  Strides in elements; `turn`: turns per position
+// of each pair (freq / 2 pi); sign: 1 forward, -1 backward.
+struct RopeSide {
+  const void* in;
+  void* out;
+  int64_t ib, ih, in_n, ob, oh, on;
+};
+struct RopeArgs {
+  RopeSide q, k;
+  const int32_t* positions;
+  int64_t pos_bstride;
+  int B, H, HH, N, d, rot, pos0;  // H: heads of q in this call (0: none), HH: of both
+  int heads;                      // heads per thread (set by the launcher)
+  float amplitude, sign;
+  double turn[64];
+};
+hipError_t launch_rope(const RopeArgs& a, bool bf16, bool half, hipStream_t st);
+
+// 8-bit cache (qcache.hip, qcache_attn.hip).
+struct QCache {
+  uint8_t* k;
+  uint8_t* v;
+  float* k_scale;
+  float* v_scale;
+  int M;  // blocks per (batch, KV head)
+};
+struct QAppend {
+  QCache c;
+  const void *k_new, *v_new;
+  int64_t ksb, ksh, ksn, vsb, vsh, vsn;  // strides in elements
+  void *k_open, *v_open;
+  float* pyr;
+  int Hkv, n_old;
+};
+hipError_t launch_qcache_append(const Geo& geo, const Geo& geo_old, int BH, int D, bool bf16, const QAppend& a,
+                                hipStream_t st);
+size_t qcache_attn_ws(const Shape& s, const Geo& geo);
+hipError_t launch_qcache_attn(const Shape& s, const Geo& geo, const QCache& c, const void* q, const int32_t* idx, void* o,
+                              float* lse, void* ws, hipStream_t st);
+
+// Pyramid levels 2 .. Lstore from level 1 (pool.hip): everything above leaf
+// block `leaf` and the blocks after it, for a pyramid whose other nodes are
+// those of the first n_old tokens.
+hipError_t launch_pyramid_levels(const Geo& geo, int BH, int D, float* pyr, int n_old, hipStream_t st);
+
 }  // namespace pisa

@@ -9,59 +9,31 @@
 // the mean of its existing children (the last node of a level may be short).
 #include "common.h"
 #include "kernels.h"
+#include "pool.h"
 
 namespace pisa {
 
-// Mean of leaf block `leaf` (rows [leaf*C, min((leaf+1)*C, N))) computed by
-// one wavefront: 16 lanes cover a key row, the 4 row groups take every 4th
-// row; lanes of row group 0 return the D/16 means of their column slice.
-// Both the full build and the decode-cache update use this, so their leaf
-// means agree bit for bit.
-template <typename T, int D>
-__device__ __forceinline__ void leaf_mean(const T* __restrict__ kb, const Geo& geo, int leaf, int sub, int rg,
-                                          float (&m)[D / 16]) {
-  constexpr int DPL = D / 16;
-  const int64_t row0 = static_cast<int64_t>(leaf) * geo.C;
-  const int nrows = min(geo.C, geo.N - static_cast<int>(row0));
-  float acc[DPL];
-#pragma unroll
-  for (int e = 0; e < DPL; ++e) acc[e] = 0.f;
-  const T* base = kb + row0 * D + sub * DPL;
-  int r = rg;
-  for (; r + 12 < nrows; r += 16) {
-    float x0[DPL], x1[DPL], x2[DPL], x3[DPL];
-    load_row_part<T, DPL>(base + static_cast<int64_t>(r) * D, x0);
-    load_row_part<T, DPL>(base + static_cast<int64_t>(r + 4) * D, x1);
-    load_row_part<T, DPL>(base + static_cast<int64_t>(r + 8) * D, x2);
-    load_row_part<T, DPL>(base + static_cast<int64_t>(r + 12) * D, x3);
-#pragma unroll
-    for (int e = 0; e < DPL; ++e) acc[e] += (x0[e] + x1[e]) + (x2[e] + x3[e]);
+// Coarser levels whose nodes lie inside a run of lpb leaves from leaf0 on, whose
+// means are in `src`.
+__device__ __forceinline__ void pool_run_levels(float* __restrict__ pb, const Geo& geo, int s_levels, int lpb, int leaf0,
+                                                int D, float* src, float* dstb) {
+  const int top = min(s_levels + 1, geo.Lstore);
+  for (int lv = 2; lv <= top; ++lv) {
+    const int first = anc_at(geo, leaf0, lv);  // node index of the run start
+    const int below_first = anc_at(geo, leaf0, lv - 1);
+    const int nnode = min(lpb / geo.gp[lv], geo.M[lv] - first);
+    for (int e = threadIdx.x; e < nnode * D; e += blockDim.x) {
+      const int j = e / D, col = e - j * D;
+      const int node = first + j;
+      const float mval = node_mean(geo, lv, node, col, [&](int ch, int cc) { return src[(ch - below_first) * D + cc]; });
+      dstb[j * D + col] = mval;
+      pb[(geo.off[lv] + node) * D + col] = mval;
+    }
+    __syncthreads();
+    float* tmp = src;
+    src = dstb;
+    dstb = tmp;
   }
-  for (; r < nrows; r += 4) {
-    float x0[DPL];
-    load_row_part<T, DPL>(base + static_cast<int64_t>(r) * D, x0);
-#pragma unroll
-    for (int e = 0; e < DPL; ++e) acc[e] += x0[e];
-  }
-#pragma unroll
-  for (int e = 0; e < DPL; ++e) {
-    acc[e] += __shfl_xor(acc[e], 16);
-    acc[e] += __shfl_xor(acc[e], 32);
-  }
-  const float inv = 1.0f / static_cast<float>(nrows);
-#pragma unroll
-  for (int e = 0; e < DPL; ++e) m[e] = acc[e] * inv;
-}
-
-// Node `node` of level lv (>= 2): the mean of its existing children, summed
-// in index order; `child(ch, col)` reads column col of child ch.
-template <typename F>
-__device__ __forceinline__ float node_mean(const Geo& geo, int lv, int node, int col, F child) {
-  const int c0 = node * geo.g;
-  const int c1 = min(c0 + geo.g, geo.M[lv - 1]);
-  float s = 0.f;
-  for (int ch = c0; ch < c1; ++ch) s += child(ch, col);
-  return s / static_cast<float>(c1 - c0);
 }
 
 template <typename T, int D>
@@ -100,26 +72,7 @@ __global__ __launch_bounds__(256) void pool_leaf_kernel(const T* __restrict__ k,
   }
   __syncthreads();
 
-  // Coarser levels whose nodes lie inside this run of leaves.
-  const int top = min(s_levels + 1, geo.Lstore);
-  float* src = buf0;
-  float* dstb = buf1;
-  for (int lv = 2; lv <= top; ++lv) {
-    const int first = anc_at(geo, leaf0, lv);  // node index of the run start
-    const int below_first = anc_at(geo, leaf0, lv - 1);
-    const int nnode = min(lpb / geo.gp[lv], geo.M[lv] - first);
-    for (int e = threadIdx.x; e < nnode * D; e += blockDim.x) {
-      const int j = e / D, col = e - j * D;
-      const int node = first + j;
-      const float mval = node_mean(geo, lv, node, col, [&](int ch, int cc) { return src[(ch - below_first) * D + cc]; });
-      dstb[j * D + col] = mval;
-      pb[(geo.off[lv] + node) * D + col] = mval;
-    }
-    __syncthreads();
-    float* tmp = src;
-    src = dstb;
-    dstb = tmp;
-  }
+  pool_run_levels(pb, geo, s_levels, lpb, leaf0, D, buf0, buf1);
 }
 
 // Levels from `first_level` to Lstore, one workgroup per (batch, KV head).
@@ -351,6 +304,27 @@ static int pool_s_levels(int g) {
   return s;
 }
 
+// Levels from s + 2 on, from level s + 1.
+static hipError_t launch_pool_top(const Geo& geo, int BH, int D, int s, float* pyr, hipStream_t st) {
+  if (geo.Lstore < s + 2) return hipSuccess;
+  ProfScope ps("pool_top", st);
+  // levels s+1 (read) and s+2 (the largest computed) in LDS, the coarser
+  // ones reuse the two buffers
+  const size_t tlds = static_cast<size_t>(geo.M[s + 1] + geo.M[s + 2]) * D * sizeof(float);
+  bool fits = tlds <= kPoolTopLds;
+  if (fits && tlds > 65536) {
+    fits = hipFuncSetAttribute(reinterpret_cast<const void*>(pool_top_lds_kernel),
+                               hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(tlds)) == hipSuccess;
+    if (!fits) (void)hipGetLastError();  // the refusal is not the caller's error
+  }
+  if (fits) {
+    pool_top_lds_kernel<<<BH, 1024, tlds, st>>>(pyr, geo, s + 2, D);
+  } else {
+    pool_top_kernel<<<BH, 256, 0, st>>>(pyr, geo, s + 2, D);
+  }
+  return hipGetLastError();
+}
+
 hipError_t launch_build_pyramid(const Geo& geo, int BH, int D, bool bf16, const void* k, float* pyr,
                                 hipStream_t st) {
   const int s = pool_s_levels(geo.g);
@@ -372,27 +346,41 @@ hipError_t launch_build_pyramid(const Geo& geo, int BH, int D, bool bf16, const 
       pool_leaf_kernel<float, 64><<<grid, 256, lds, st>>>(static_cast<const float*>(k), pyr, geo, s, lpb);
   }
   }
-  hipError_t e = hipGetLastError();
+  const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (geo.Lstore >= s + 2) {
-    ProfScope ps("pool_top", st);
-    // levels s+1 (read) and s+2 (the largest computed) in LDS, the coarser
-    // ones reuse the two buffers
-    const size_t tlds = static_cast<size_t>(geo.M[s + 1] + geo.M[s + 2]) * D * sizeof(float);
-    bool fits = tlds <= kPoolTopLds;
-    if (fits && tlds > 65536) {
-      fits = hipFuncSetAttribute(reinterpret_cast<const void*>(pool_top_lds_kernel),
-                                 hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(tlds)) == hipSuccess;
-      if (!fits) (void)hipGetLastError();  // the refusal is not the caller's error
-    }
-    if (fits) {
-      pool_top_lds_kernel<<<BH, 1024, tlds, st>>>(pyr, geo, s + 2, D);
-    } else {
-      pool_top_kernel<<<BH, 256, 0, st>>>(pyr, geo, s + 2, D);
-    }
-    e = hipGetLastError();
+  return launch_pool_top(geo, BH, D, s, pyr, st);
+}
+
+// The runs' coarser levels alone, from level-1 means that are in memory: a
+// workgroup per run of lpb leaf blocks, the first one `run0`.
+__global__ __launch_bounds__(256) void pool_runs_kernel(float* __restrict__ pyr, Geo geo, int s_levels, int lpb, int run0,
+                                                        int D) {
+  extern __shared__ __align__(16) float lds[];  // two buffers of lpb * D floats
+  const int bh = blockIdx.y;
+  const int leaf0 = (run0 + static_cast<int>(blockIdx.x)) * lpb;
+  const int nleaf = min(lpb, geo.M[1] - leaf0);
+  float* pb = pyr + static_cast<int64_t>(bh) * geo.R * D;
+  for (int e = threadIdx.x; e < nleaf * D; e += blockDim.x) lds[e] = pb[(geo.off[1] + leaf0) * D + e];
+  __syncthreads();
+  pool_run_levels(pb, geo, s_levels, lpb, leaf0, D, lds, lds + lpb * D);
+}
+
+// The first run is that of the last old leaf block: every level inside an
+// earlier run was stored by n_old tokens already (level s + 1 has two nodes as
+// soon as a second run begins).
+hipError_t launch_pyramid_levels(const Geo& geo, int BH, int D, float* pyr, int n_old, hipStream_t st) {
+  const int s = pool_s_levels(geo.g);
+  int lpb = 1;
+  for (int i = 0; i < s; ++i) lpb *= geo.g;
+  if (s > 0 && geo.Lstore >= 2) {
+    const int run0 = n_old > 0 ? (n_old - 1) / geo.C / lpb : 0;
+    const dim3 grid((geo.M[1] + lpb - 1) / lpb - run0, BH);
+    ProfScope ps("pool_runs", st);
+    pool_runs_kernel<<<grid, 256, 2 * static_cast<size_t>(lpb) * D * sizeof(float), st>>>(pyr, geo, s, lpb, run0, D);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
   }
-  return e;
+  return launch_pool_top(geo, BH, D, s, pyr, st);
 }
 
 }  // namespace pisa

@@ -26,6 +26,14 @@ PISA_SCORE_LSE = 0
 PISA_SCORE_MEAN = 1
 PISA_SCORE_MEAN_VAR = 2
 
+PISA_ROPE_HALF = 0
+PISA_ROPE_INTERLEAVED = 1
+PISA_ROPE_SCALE_NONE = 0
+PISA_ROPE_SCALE_LINEAR = 1
+PISA_ROPE_SCALE_BASE = 2
+PISA_ROPE_SCALE_PARTS = 3
+PISA_ROPE_MAX_PAIRS = 64
+
 PISA_OK = 0
 PISA_ERR_INVALID_ARG = -1
 PISA_ERR_UNSUPPORTED = -2
@@ -39,6 +47,9 @@ EXPORTS = (
     "pisa_sparse_attn_fwd", "pisa_attn_union_min_tiles",
     "pisa_attn_bwd_workspace_bytes", "pisa_sparse_attn_bwd",
     "pisa_quality_workspace_bytes", "pisa_selection_quality",
+    "pisa_rope_frequencies", "pisa_rope_fwd", "pisa_rope_bwd",
+    "pisa_qcache_blocks", "pisa_qcache_bytes", "pisa_qcache_append",
+    "pisa_qcache_attn_workspace_bytes", "pisa_qcache_attn_fwd",
     "pisa_profile_enable", "pisa_profile_report", "pisa_status_string", "pisa_last_error",
 )
 
@@ -59,13 +70,33 @@ class Problem(ctypes.Structure):
         return "Problem(" + ", ".join(f"{n}={getattr(self, n)}" for n, _ in self._fields_) + ")"
 
 
+class Strides(ctypes.Structure):
+    """Mirror of ``pisa_strides`` (elements)."""
+    _fields_ = [("b", ctypes.c_int64), ("h", ctypes.c_int64), ("n", ctypes.c_int64)]
+
+
+class Rope(ctypes.Structure):
+    """Mirror of ``pisa_rope``."""
+    _fields_ = ([(n, ctypes.c_int32) for n in ("B", "H", "Hkv", "N", "d", "rot", "layout", "dtype", "pos0", "reserved")]
+                + [("pos_bstride", ctypes.c_int64), ("amplitude", ctypes.c_double),
+                   ("freq", ctypes.c_double * PISA_ROPE_MAX_PAIRS)])
+
+
+class QCacheBuffers(ctypes.Structure):
+    """Mirror of ``pisa_qcache``."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "k_open", "v_open")]
+
+
+_DTYPES = {"bf16": PISA_DTYPE_BF16, "f32": PISA_DTYPE_F32,
+           torch.bfloat16: PISA_DTYPE_BF16, torch.float32: PISA_DTYPE_F32}
+_TORCH = {PISA_DTYPE_BF16: torch.bfloat16, PISA_DTYPE_F32: torch.float32}
+
+
 def make_problem(B, H, Hkv, Nq, N, d, C, fanout, K, causal=1, dtype="bf16", schedule=PISA_SCHEDULE_AUTO, Ncap=0,
                  score=0):
     """A pisa_problem; Ncap > N reserves rows of k, v and the pyramid for a growing N;
     score picks the selection's block score (PISA_SCORE_LSE / _MEAN / _MEAN_VAR)."""
-    dt = {"bf16": PISA_DTYPE_BF16, "f32": PISA_DTYPE_F32,
-          torch.bfloat16: PISA_DTYPE_BF16, torch.float32: PISA_DTYPE_F32}[dtype]
-    return Problem(B, H, Hkv, Nq, N, d, C, fanout, K, int(causal), dt, schedule, Ncap, score)
+    return Problem(B, H, Hkv, Nq, N, d, C, fanout, K, int(causal), _DTYPES[dtype], schedule, Ncap, score)
 
 
 def _load():
@@ -94,6 +125,15 @@ def _load():
         "pisa_sparse_attn_bwd": (ctypes.c_int, [P, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
         "pisa_quality_workspace_bytes": (sz, [P, i32]),
         "pisa_selection_quality": (ctypes.c_int, [P, vp, vp, vp, vp, i32, vp, vp, vp, sz, vp]),
+        "pisa_rope_frequencies": (ctypes.c_int, [ctypes.POINTER(Rope), ctypes.c_double, i32, ctypes.c_double, i32,
+                                                 ctypes.c_double, ctypes.c_double]),
+        "pisa_rope_fwd": (ctypes.c_int, [ctypes.POINTER(Rope), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]),
+        "pisa_rope_bwd": (ctypes.c_int, [ctypes.POINTER(Rope), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]),
+        "pisa_qcache_blocks": (ctypes.c_int32, [P]),
+        "pisa_qcache_bytes": (sz, [P]),
+        "pisa_qcache_append": (ctypes.c_int, [P, vp, vp, vp, vp, vp, i32, vp, vp]),
+        "pisa_qcache_attn_workspace_bytes": (sz, [P]),
+        "pisa_qcache_attn_fwd": (ctypes.c_int, [P, vp, vp, vp, vp, vp, vp, sz, vp]),
         "pisa_profile_enable": (ctypes.c_int, [ctypes.c_int]),
         "pisa_profile_report": (ctypes.c_int, [ctypes.c_char_p, sz]),
         "pisa_status_string": (ctypes.c_char_p, [ctypes.c_int]),
@@ -235,6 +275,54 @@ def pisa_selection_quality(p: Problem, q, k, block_idx, rows, n_rows: int, metri
                   "pisa_selection_quality")
 
 
+def pisa_rope_frequencies(r: Rope, base: float, scaling: int, factor: float, ctx: int, fast: float, slow: float) -> int:
+    return _check(_lib.pisa_rope_frequencies(ctypes.byref(r), base, scaling, factor, ctx, fast, slow),
+                  "pisa_rope_frequencies")
+
+
+def _rope_call(name, r, q, qs, k, ks, positions, qo, qos, ko, kos, stream):
+    st = [None if x is None else ctypes.addressof(x) for x in (qs, ks, qos, kos)]
+    return _check(getattr(_lib, name)(ctypes.byref(r), _ptr(q), st[0], _ptr(k), st[1], _ptr(positions), _ptr(qo), st[2],
+                                      _ptr(ko), st[3], _stream(stream)), name)
+
+
+def pisa_rope_fwd(r: Rope, q, q_strides, k, k_strides, positions, q_out, q_out_strides, k_out, k_out_strides,
+                  stream=None) -> int:
+    return _rope_call("pisa_rope_fwd", r, q, q_strides, k, k_strides, positions, q_out, q_out_strides, k_out,
+                      k_out_strides, stream)
+
+
+def pisa_rope_bwd(r: Rope, d_q_out, d_q_out_strides, d_k_out, d_k_out_strides, positions, d_q, d_q_strides, d_k,
+                  d_k_strides, stream=None) -> int:
+    return _rope_call("pisa_rope_bwd", r, d_q_out, d_q_out_strides, d_k_out, d_k_out_strides, positions, d_q, d_q_strides,
+                      d_k, d_k_strides, stream)
+
+
+def pisa_qcache_blocks(p: Problem) -> int:
+    M = _lib.pisa_qcache_blocks(ctypes.byref(p))
+    return _check(M, "pisa_qcache_blocks") if M < 0 else M
+
+
+def pisa_qcache_bytes(p: Problem) -> int:
+    return _lib.pisa_qcache_bytes(ctypes.byref(p))
+
+
+def pisa_qcache_append(p: Problem, cache, k_new, k_strides, v_new, v_strides, n_old: int, pyramid=None,
+                       stream=None) -> int:
+    st = [None if x is None else ctypes.addressof(x) for x in (k_strides, v_strides)]
+    return _check(_lib.pisa_qcache_append(ctypes.byref(p), cache.address, _ptr(k_new), st[0], _ptr(v_new), st[1], n_old,
+                                          _ptr(pyramid), _stream(stream)), "pisa_qcache_append")
+
+
+def pisa_qcache_attn_workspace_bytes(p: Problem) -> int:
+    return _lib.pisa_qcache_attn_workspace_bytes(ctypes.byref(p))
+
+
+def pisa_qcache_attn_fwd(p: Problem, cache, q, block_idx, o, lse=None, ws=None, ws_bytes=0, stream=None) -> int:
+    return _check(_lib.pisa_qcache_attn_fwd(ctypes.byref(p), cache.address, _ptr(q), _ptr(block_idx), _ptr(o), _ptr(lse),
+                                            _ptr(ws), ws_bytes, _stream(stream)), "pisa_qcache_attn_fwd")
+
+
 def pisa_attn_union_min_tiles(n: int) -> int:
     """Sets the row-tile union threshold of pisa_sparse_attn_fwd (n < 0: off); returns the previous one."""
     return _lib.pisa_attn_union_min_tiles(int(n))
@@ -340,3 +428,148 @@ def sparse_attn_bwd(p: Problem, q, k, v, block_idx, o, lse, d_o, stream=None):
     nb = pisa_attn_bwd_workspace_bytes(p)
     pisa_sparse_attn_bwd(p, q, k, v, block_idx, o, lse, d_o, dq, dk, dv, _workspace(nb, q.device), nb, stream)
     return dq, dk, dv
+
+
+# ------------------------------------------------- rotary positions, 8-bit cache ---
+
+_LAYOUTS = {"half": PISA_ROPE_HALF, "interleaved": PISA_ROPE_INTERLEAVED}
+_SCALINGS = {"none": PISA_ROPE_SCALE_NONE, "linear": PISA_ROPE_SCALE_LINEAR, "base": PISA_ROPE_SCALE_BASE,
+             "parts": PISA_ROPE_SCALE_PARTS}
+
+
+def _take(x, name, dtype, shape, device, contiguous=True):
+    """x, a tensor of the current device (`device`) with this dtype and shape; ValueError otherwise."""
+    if x.dtype != dtype or x.shape != shape or x.device != device or (contiguous and not x.is_contiguous()):
+        raise ValueError(f"{name}: expected {'a contiguous ' if contiguous else ''}{dtype} {tuple(shape)} on {device}, "
+                         f"got {x.dtype} {tuple(x.shape)} (strides {x.stride()}) on {x.device}")
+    return x
+
+
+def _device():
+    return torch.device("cuda", torch.cuda.current_device())
+
+
+def _strided(x, name, dtype, shape, device):
+    """The pisa_strides of a [B, heads, rows, d] tensor (None where it is contiguous)."""
+    _take(x, name, dtype, shape, device, contiguous=False)
+    if x.is_contiguous():
+        return None
+    b, h, n, one = x.stride()
+    if one != 1:
+        raise ValueError(f"{name}: its last dimension must be contiguous (strides {x.stride()})")
+    # the stride of a dimension of one entry is never used
+    return Strides(b if shape[0] > 1 else 0, h if shape[1] > 1 else 0, n if shape[2] > 1 else 0)
+
+
+def make_rope(B, H, Hkv, N, d, rot=None, layout="half", dtype="bf16", base=10000.0, scaling="none", factor=1.0, ctx=4096,
+              fast=32.0, slow=1.0, pos0=0):
+    """A pisa_rope with the frequencies of pisa_rope_frequencies; rot defaults to d."""
+    r = Rope(B, H, Hkv, N, d, d if rot is None else rot, _LAYOUTS[layout], _DTYPES[dtype], pos0, 0, 0, 1.0)
+    pisa_rope_frequencies(r, base, _SCALINGS[scaling], factor, ctx, fast, slow)
+    return r
+
+
+def _rope(turn, r: Rope, q, k, positions, q_out, k_out, stream):
+    dt, dev = _TORCH[r.dtype], _device()
+    if positions is not None:
+        if positions.shape == (r.N,):
+            _take(positions, "positions", torch.int32, (r.N,), dev)
+            r.pos_bstride = 0
+        else:
+            _take(positions, "positions", torch.int32, (r.B, r.N), dev)
+            r.pos_bstride = r.N
+    args, out = [], []
+    for name, x, y, heads in (("q", q, q_out, r.H), ("k", k, k_out, r.Hkv)):
+        if x is None:
+            if y is not None:
+                raise ValueError(f"{name}_out without {name}")
+            args.append((None, None, None, None))
+        else:
+            shape = (r.B, heads, r.N, r.d)
+            xs = _strided(x, name, dt, shape, dev)
+            if y is None:
+                y = torch.empty(shape, dtype=dt, device=dev)
+            args.append((x, xs, y, _strided(y, name + "_out", dt, shape, dev)))
+        out.append(y)
+    (q, qs, qo, qos), (k, ks, ko, kos) = args
+    turn(r, q, qs, k, ks, positions, qo, qos, ko, kos, stream)
+    return tuple(out)
+
+
+def rope_fwd(r: Rope, q, k=None, positions=None, q_out=None, k_out=None, stream=None):
+    """Turn q [B, H, N, d] and k [B, Hkv, N, d] (views with a contiguous last dimension; either may be None)
+    by their positions (int32 [N] or [B, N]; default pos0, pos0 + 1, ...).  Returns (q_out, k_out), allocated
+    contiguous where not given."""
+    return _rope(pisa_rope_fwd, r, q, k, positions, q_out, k_out, stream)
+
+
+def rope_bwd(r: Rope, d_q_out, d_k_out=None, positions=None, d_q=None, d_k=None, stream=None):
+    """The gradients of rope_fwd's inputs from those of its outputs; tensors as there."""
+    return _rope(pisa_rope_bwd, r, d_q_out, d_k_out, positions, d_q, d_k, stream)
+
+
+class QCache:
+    """The buffers of an 8-bit key/value cache (pisa_qcache): uint8 codes k [B, Hkv, M, C, d] and v [B, Hkv, M, d, C],
+    float32 scales [B, Hkv, M], and for appending the raw rows of the last block, [B, Hkv, C, d]."""
+
+    def __init__(self, k, v, k_scale, v_scale, k_open=None, v_open=None):
+        B, H, M, C, d = k.shape
+        dev = k.device
+        if dev.type != "cuda":
+            raise ValueError(f"the cache lives on a GPU, got {dev}")
+        _take(k, "k", torch.uint8, (B, H, M, C, d), dev)
+        _take(v, "v", torch.uint8, (B, H, M, d, C), dev)
+        _take(k_scale, "k_scale", torch.float32, (B, H, M), dev)
+        _take(v_scale, "v_scale", torch.float32, (B, H, M), dev)
+        if (k_open is None) != (v_open is None):
+            raise ValueError("k_open and v_open come together")
+        if k_open is not None:
+            _take(k_open, "k_open", k_open.dtype, (B, H, C, d), dev)
+            _take(v_open, "v_open", k_open.dtype, (B, H, C, d), dev)
+        self.k, self.v, self.k_scale, self.v_scale, self.k_open, self.v_open = k, v, k_scale, v_scale, k_open, v_open
+        self._c = QCacheBuffers(*(_ptr(x) for x in (k, v, k_scale, v_scale, k_open, v_open)))
+        self.address = ctypes.addressof(self._c)
+
+    def check(self, p: Problem, appending=False):
+        """ValueError unless this is a cache of problem p on the current device."""
+        if self.k.shape != (p.B, p.Hkv, pisa_qcache_blocks(p), p.C, p.d):
+            raise ValueError(f"the cache's codes {tuple(self.k.shape)} do not fit {p}")
+        if self.k.device != _device():
+            raise ValueError(f"the cache is on {self.k.device}, the current device is {_device()}")
+        if appending and (self.k_open is None or self.k_open.dtype != _TORCH[p.dtype]):
+            raise ValueError("appending needs k_open and v_open in the problem's dtype")
+
+
+def make_qcache(p: Problem, device=None):
+    """An empty cache for problem p (reserving Ncap tokens)."""
+    M, dev = pisa_qcache_blocks(p), _device() if device is None else device
+    new = dict(device=dev)
+    k = torch.zeros((p.B, p.Hkv, M, p.C, p.d), dtype=torch.uint8, **new)
+    v = torch.zeros((p.B, p.Hkv, M, p.d, p.C), dtype=torch.uint8, **new)
+    scales = (torch.ones((p.B, p.Hkv, M), dtype=torch.float32, **new) for _ in range(2))
+    raw = (torch.zeros((p.B, p.Hkv, p.C, p.d), dtype=_TORCH[p.dtype], **new) for _ in range(2))
+    return QCache(k, v, *scales, *raw)
+
+
+def qcache_append(p: Problem, cache: QCache, k_new, v_new, n_old: int, pyramid=None, stream=None):
+    """Append rows n_old .. N-1 (k_new, v_new: [B, Hkv, N - n_old, d], views with a contiguous last dimension) to
+    the cache, and bring the pyramid with it where one is given."""
+    cache.check(p, appending=True)
+    shape, dt, dev = (p.B, p.Hkv, p.N - n_old, p.d), _TORCH[p.dtype], cache.k.device
+    ks, vs = _strided(k_new, "k_new", dt, shape, dev), _strided(v_new, "v_new", dt, shape, dev)
+    if pyramid is not None:
+        _take(pyramid, "pyramid", torch.float32, (p.B, p.Hkv, pisa_pyramid_layout(p)[1], p.d), dev)
+    pisa_qcache_append(p, cache, k_new, ks, v_new, vs, n_old, pyramid, stream)
+
+
+def qcache_attn_fwd(p: Problem, cache: QCache, q, block_idx, stream=None):
+    """Allocate outputs and workspace, run pisa_qcache_attn_fwd; returns (o, lse)."""
+    cache.check(p)
+    dev = cache.k.device
+    _take(q, "q", _TORCH[p.dtype], (p.B, p.H, p.Nq, p.d), dev)
+    _take(block_idx, "block_idx", torch.int32, (p.B, p.Hkv, p.Nq, p.K), dev)
+    o = torch.empty_like(q)
+    lse = torch.empty((p.B, p.H, p.Nq), dtype=torch.float32, device=dev)
+    nb = pisa_qcache_attn_workspace_bytes(p)
+    pisa_qcache_attn_fwd(p, cache, q, block_idx, o, lse, _workspace(nb, dev), nb, stream)
+    return o, lse

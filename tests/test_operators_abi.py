@@ -1,0 +1,192 @@
+"""Rotary positions and the 8-bit cache at the C ABI, without a GPU: the frequency table, buffer sizes, and every
+refusal (exact status, a detail that names the argument) before anything is launched."""
+import ctypes
+import math
+
+import pytest
+
+pisa = pytest.importorskip("paper_2609_31093_amd.pisa", reason="libpisa.so not built")
+
+FAKE = 1 << 20  # an aligned, non-null address; never dereferenced because validation fails first
+INVALID, UNSUPPORTED = pisa.PISA_ERR_INVALID_ARG, pisa.PISA_ERR_UNSUPPORTED
+LIB = pisa.library()
+
+
+def rope(**kw):
+    base = dict(B=2, H=4, Hkv=2, N=100, d=128)
+    fields = {n: kw.pop(n) for n in list(kw) if n in ("rot_", "layout_", "dtype_", "reserved", "amplitude", "pos_bstride")}
+    r = pisa.make_rope(**{**base, **kw})
+    for n, v in fields.items():
+        setattr(r, n.rstrip("_"), v)
+    return r
+
+
+# ------------------------------------------------------------ frequencies ---
+
+@pytest.mark.parametrize("rot", [2, 6, 50, 64, 128])
+def test_frequencies_by_their_formulas(rot):
+    base, s, ctx, fast, slow = 10000.0, 8.0, 4096, 32.0, 1.0
+    plain = [base ** (-2 * i / rot) for i in range(rot // 2)]
+    got = pisa.make_rope(1, 1, 1, 1, 128, rot=rot)
+    assert list(got.freq)[:rot // 2] == pytest.approx(plain, rel=1e-14) and got.amplitude == 1.0
+    assert list(got.freq)[rot // 2:] == [0.0] * (64 - rot // 2)
+    got = pisa.make_rope(1, 1, 1, 1, 128, rot=rot, scaling="linear", factor=s)
+    assert list(got.freq)[:rot // 2] == pytest.approx([f / s for f in plain], rel=1e-14)
+    if rot > 2:
+        got = pisa.make_rope(1, 1, 1, 1, 128, rot=rot, scaling="base", factor=s)
+        f = list(got.freq)[:rot // 2]
+        assert f[0] == 1.0 and f[-1] == pytest.approx(plain[-1] / s, rel=1e-12)
+    got = pisa.make_rope(1, 1, 1, 1, 128, rot=rot, scaling="parts", factor=s, ctx=ctx, fast=fast, slow=slow)
+    for f, g in zip(plain, got.freq):
+        turns = ctx * f / (2 * math.pi)
+        if turns >= fast:
+            assert g == pytest.approx(f, rel=1e-14)
+        elif turns <= slow:
+            assert g == pytest.approx(f / s, rel=1e-14)
+        else:
+            assert f / s < g < f
+    assert got.amplitude == pytest.approx(0.1 * math.log(s) + 1)
+
+
+def test_frequency_refusals():
+    r = rope()
+    call = lambda *a: LIB.pisa_rope_frequencies(ctypes.byref(r), *a)  # noqa: E731
+    for bad in ((1.0, 0, 1.0, 1, 32, 1), (float("nan"), 0, 1.0, 1, 32, 1), (float("inf"), 0, 1.0, 1, 32, 1),
+                (1e4, 4, 1.0, 1, 32, 1), (1e4, -1, 1.0, 1, 32, 1), (1e4, 1, 0.5, 1, 32, 1), (1e4, 1, float("nan"), 1, 32, 1),
+                (1e4, 3, 2.0, 0, 32, 1), (1e4, 3, 2.0, 10, 1, 1), (1e4, 3, 2.0, 10, 32, -1)):
+        assert call(*bad) == INVALID, bad
+        assert pisa.pisa_last_error()
+    assert LIB.pisa_rope_frequencies(None, 1e4, 0, 1.0, 1, 32.0, 1.0) == INVALID
+    for rot in (0, 1, 3, 130, -2):
+        r.rot = rot
+        assert call(1e4, 0, 1.0, 1, 32.0, 1.0) == INVALID, rot
+    r.rot = 2
+    assert call(1e4, 2, 2.0, 1, 32.0, 1.0) == INVALID  # no base to change: the exponent has no value
+
+
+# -------------------------------------------------------------- rotations ---
+
+@pytest.mark.parametrize("name", ["pisa_rope_fwd", "pisa_rope_bwd"])
+@pytest.mark.parametrize("kw,status", [
+    (dict(B=0), INVALID), (dict(H=0), INVALID), (dict(Hkv=0), INVALID), (dict(N=0), INVALID),
+    (dict(d=96, rot=64), UNSUPPORTED), (dict(rot_=3), INVALID), (dict(rot_=0), INVALID), (dict(rot_=130), INVALID),
+    (dict(d=64, rot_=66), INVALID), (dict(layout_=2), INVALID), (dict(dtype_=2), INVALID), (dict(reserved=1), INVALID),
+    (dict(pos_bstride=-1), INVALID), (dict(amplitude=float("nan")), INVALID), (dict(pos0=2**31 - 50), UNSUPPORTED),
+    (dict(B=16, N=(1 << 24) + 1), UNSUPPORTED), (dict(H=65535), UNSUPPORTED),
+])
+def test_rope_refuses_bad_descriptors(name, kw, status):
+    r = rope(**kw)
+    st = getattr(LIB, name)(ctypes.byref(r), FAKE, None, FAKE, None, None, FAKE, None, FAKE, None, None)
+    assert st == status and pisa.pisa_last_error()
+
+
+@pytest.mark.parametrize("name", ["pisa_rope_fwd", "pisa_rope_bwd"])
+def test_rope_refuses_bad_tensors(name):
+    r = rope()
+    S = pisa.Strides
+
+    def call(q=FAKE, qs=None, k=FAKE, ks=None, pos=None, qo=FAKE, qos=None, ko=FAKE, kos=None, rr=r):
+        st = [None if x is None else ctypes.addressof(x) for x in (qs, ks, qos, kos)]
+        return getattr(LIB, name)(None if rr is None else ctypes.byref(rr), q, st[0], k, st[1], pos, qo, st[2], ko, st[3], None)
+    assert call(rr=None) == INVALID
+    assert call(q=None) == INVALID and "q" in pisa.pisa_last_error()
+    assert call(ko=None) == INVALID and "k" in pisa.pisa_last_error()
+    assert call(q=None, qo=None, k=None, ko=None) == INVALID
+    assert call(q=FAKE + 8) == INVALID and "aligned" in pisa.pisa_last_error()
+    assert call(pos=FAKE + 2) == INVALID and "positions" in pisa.pisa_last_error()
+    good = (4 * 100 * 128, 100 * 128, 128)
+    for at in range(3):
+        for x in (-8, 4, 129):  # negative, and no multiple of 16 bytes
+            bad = list(good)
+            bad[at] = x
+            assert call(qs=S(*bad)) == INVALID and "strides" in pisa.pisa_last_error(), bad
+        bad = list(good)
+        bad[at] = 0  # a broadcast output would be written by many
+        assert call(qo=FAKE * 2, qos=S(*bad)) == INVALID and "overlap" in pisa.pisa_last_error()
+    assert call(qos=S(4 * 100 * 128, 128, 4 * 128)) == INVALID and "in place" in pisa.pisa_last_error()
+    r32 = rope(dtype="f32")
+    assert call(qs=S(4 * 100 * 128, 100 * 128, 130), rr=r32) == INVALID
+    r.freq[3] = float("nan")
+    assert call() == INVALID and "freq" in pisa.pisa_last_error()
+
+
+# ------------------------------------------------------------------ cache ---
+
+def problem(**kw):
+    base = dict(B=1, H=4, Hkv=2, Nq=256, N=1024, d=128, C=64, fanout=2, K=4, causal=1, dtype="bf16")
+    return pisa.make_problem(**{**base, **kw})
+
+
+def buffers(**kw):
+    return pisa.QCacheBuffers(*[kw.get(n, FAKE) for n, _ in pisa.QCacheBuffers._fields_])
+
+
+def test_cache_sizes():
+    assert pisa.pisa_qcache_blocks(problem(N=1000)) == 16
+    assert pisa.pisa_qcache_blocks(problem(N=1000, Ncap=2049)) == 33
+    assert pisa.pisa_qcache_bytes(problem(N=1000, Ncap=2049)) == 2 * 33 * 64 * 128
+    assert pisa.pisa_qcache_bytes(problem(B=2, N=1, Nq=1, C=32, d=64)) == 2 * 2 * 32 * 64
+    assert pisa.pisa_qcache_bytes(problem(d=96)) == 0
+    assert LIB.pisa_qcache_blocks(ctypes.byref(problem(d=96))) == UNSUPPORTED
+
+
+BAD = [(dict(H=3), INVALID), (dict(Nq=2048), INVALID), (dict(K=2), INVALID), (dict(d=96), UNSUPPORTED),
+       (dict(C=48), UNSUPPORTED), (dict(C=288), UNSUPPORTED), (dict(H=68), UNSUPPORTED), (dict(Ncap=1000), INVALID)]
+
+
+@pytest.mark.parametrize("kw,status", BAD)
+def test_cache_calls_refuse_bad_problems(kw, status):
+    p, c = problem(**kw), buffers()
+    assert LIB.pisa_qcache_append(ctypes.byref(p), ctypes.byref(c), FAKE, None, FAKE, None, 0, None, None) == status
+    assert LIB.pisa_qcache_attn_fwd(ctypes.byref(p), ctypes.byref(c), FAKE, FAKE, FAKE, None, FAKE, 1 << 40, None) == status
+    assert pisa.pisa_last_error()
+    assert pisa.pisa_qcache_attn_workspace_bytes(p) == 0
+
+
+def test_append_refusals():
+    p = problem()
+
+    def call(c=None, k=FAKE, ks=None, v=FAKE, vs=None, n_old=0, pyr=None):
+        c = buffers() if c is None else c
+        st = [None if x is None else ctypes.addressof(x) for x in (ks, vs)]
+        return LIB.pisa_qcache_append(ctypes.byref(p), ctypes.byref(c), k, st[0], v, st[1], n_old, pyr, None)
+    assert LIB.pisa_qcache_append(ctypes.byref(p), None, FAKE, None, FAKE, None, 0, None, None) == INVALID
+    for n in ("k", "v", "k_scale", "v_scale", "k_open", "v_open"):
+        assert call(c=buffers(**{n: None})) == INVALID and n in pisa.pisa_last_error(), n
+        assert call(c=buffers(**{n: FAKE + 4})) == INVALID and "aligned" in pisa.pisa_last_error(), n
+    for n_old in (-1, 1025):
+        assert call(n_old=n_old) == INVALID and "n_old" in pisa.pisa_last_error()
+    assert call(k=None) == INVALID and "k_new" in pisa.pisa_last_error()
+    assert call(v=FAKE + 2) == INVALID and "v_new" in pisa.pisa_last_error()
+    assert call(pyr=FAKE + 4) == INVALID and "pyramid" in pisa.pisa_last_error()
+    assert call(vs=pisa.Strides(0, 0, 4)) == INVALID and "v_new" in pisa.pisa_last_error()
+    assert call(n_old=1024) == pisa.PISA_OK  # nothing to append, nothing launched
+
+
+def test_attention_refusals():
+    p = problem(Nq=1)
+    need = pisa.pisa_qcache_attn_workspace_bytes(p)
+
+    def call(c=None, q=FAKE, idx=FAKE, o=FAKE, lse=FAKE, ws=FAKE, nb=need):
+        c = buffers() if c is None else c
+        return LIB.pisa_qcache_attn_fwd(ctypes.byref(p), ctypes.byref(c), q, idx, o, lse, ws, nb, None)
+    for n in ("k", "v", "k_scale", "v_scale"):
+        assert call(c=buffers(**{n: None})) == INVALID and n in pisa.pisa_last_error(), n
+    for n, arg in (("q", "q"), ("idx", "block_idx"), ("o", "o")):
+        assert call(**{n: None}) == INVALID and arg in pisa.pisa_last_error(), n
+    for n in ("q", "idx", "o", "lse"):
+        assert call(**{n: FAKE + 8}) == INVALID and "aligned" in pisa.pisa_last_error(), n
+
+
+def test_workspaces_are_asked_for_before_a_launch():
+    for kw in (dict(Nq=1), dict(Nq=1, N=8192, C=128, K=32, fanout=4), dict(Nq=4096, N=16384), dict(Nq=300, dtype="f32")):
+        p = problem(**{**dict(N=1024), **kw})
+        need = pisa.pisa_qcache_attn_workspace_bytes(p)
+        if need:
+            c = buffers()
+            st = LIB.pisa_qcache_attn_fwd(ctypes.byref(p), ctypes.byref(c), FAKE, FAKE, FAKE, None, FAKE, need - 1, None)
+            assert st == pisa.PISA_ERR_WORKSPACE and str(need) in pisa.pisa_last_error()
+            st = LIB.pisa_qcache_attn_fwd(ctypes.byref(p), ctypes.byref(c), FAKE, FAKE, FAKE, None, None, need, None)
+            assert st == pisa.PISA_ERR_WORKSPACE
+            st = LIB.pisa_qcache_attn_fwd(ctypes.byref(p), ctypes.byref(c), FAKE, FAKE, FAKE, None, FAKE + 16, need, None)
+            assert st == INVALID
