@@ -267,6 +267,14 @@ SHAPES = [
     (1, 4, 4, 70, 70, 64, 32, 2, 3, 0, "bf16", 0),
     (1, 4, 2, 300, 300, 128, 64, 2, 5, 1, "bf16", 0),
     (1, 2, 1, 2, 4100, 64, 32, 2, 120, 1, "bf16", 0),
+    # from few rows, whose units are spread over workgroups, to many, one wavefront each; 16 heads to a KV head
+    (1, 16, 1, 1, 1000, 128, 64, 2, 8, 1, "bf16", 0),
+    (1, 16, 1, 2, 3000, 128, 64, 2, 16, 1, "bf16", 0),
+    (2, 8, 2, 3, 3000, 128, 128, 4, 30, 1, "bf16", 3100),
+    (2, 8, 2, 2, 2500, 128, 128, 4, 20, 0, "f32", 0),
+    (1, 4, 4, 40, 1500, 64, 64, 2, 16, 1, "bf16", 0),
+    (1, 2, 2, 128, 900, 64, 32, 2, 12, 1, "f32", 0),
+    (1, 3, 3, 300, 600, 64, 32, 2, 7, 1, "bf16", 0),
 ]
 
 
