@@ -162,8 +162,14 @@ def _ptr(x):
     return x.data_ptr()
 
 
+# the current stream's handle without the Stream object that torch.cuda.current_stream() builds (0.1 us against 2.7)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream):
     if stream is None:
+        if _raw_stream is not None:
+            return _raw_stream(torch.cuda.current_device())
         return torch.cuda.current_stream().cuda_stream
     if isinstance(stream, int):
         return stream
@@ -437,21 +443,22 @@ _SCALINGS = {"none": PISA_ROPE_SCALE_NONE, "linear": PISA_ROPE_SCALE_LINEAR, "ba
              "parts": PISA_ROPE_SCALE_PARTS}
 
 
-def _take(x, name, dtype, shape, device, contiguous=True):
-    """x, a tensor of the current device (`device`) with this dtype and shape; ValueError otherwise."""
-    if x.dtype != dtype or x.shape != shape or x.device != device or (contiguous and not x.is_contiguous()):
-        raise ValueError(f"{name}: expected {'a contiguous ' if contiguous else ''}{dtype} {tuple(shape)} on {device}, "
-                         f"got {x.dtype} {tuple(x.shape)} (strides {x.stride()}) on {x.device}")
+def _refuse(x, name, dtype, shape, device, contiguous=True):
+    raise ValueError(f"{name}: expected {'a contiguous ' if contiguous else ''}{dtype} {tuple(shape)} on the current device "
+                     f"(cuda:{device}), got {x.dtype} {tuple(x.shape)} (strides {x.stride()}) on {x.device}")
+
+
+def _take(x, name, dtype, shape, device):
+    """x, a contiguous tensor of device number `device` with this dtype and shape; ValueError otherwise."""
+    if x.dtype != dtype or x.shape != shape or x.get_device() != device or not x.is_contiguous():
+        _refuse(x, name, dtype, shape, device)
     return x
-
-
-def _device():
-    return torch.device("cuda", torch.cuda.current_device())
 
 
 def _strided(x, name, dtype, shape, device):
     """The pisa_strides of a [B, heads, rows, d] tensor (None where it is contiguous)."""
-    _take(x, name, dtype, shape, device, contiguous=False)
+    if x.dtype != dtype or x.shape != shape or x.get_device() != device:
+        _refuse(x, name, dtype, shape, device, contiguous=False)
     if x.is_contiguous():
         return None
     b, h, n, one = x.stride()
@@ -470,7 +477,7 @@ def make_rope(B, H, Hkv, N, d, rot=None, layout="half", dtype="bf16", base=10000
 
 
 def _rope(turn, r: Rope, q, k, positions, q_out, k_out, stream):
-    dt, dev = _TORCH[r.dtype], _device()
+    dt, dev = _TORCH[r.dtype], torch.cuda.current_device()
     if positions is not None:
         if positions.shape == (r.N,):
             _take(positions, "positions", torch.int32, (r.N,), dev)
@@ -488,7 +495,7 @@ def _rope(turn, r: Rope, q, k, positions, q_out, k_out, stream):
             shape = (r.B, heads, r.N, r.d)
             xs = _strided(x, name, dt, shape, dev)
             if y is None:
-                y = torch.empty(shape, dtype=dt, device=dev)
+                y = torch.empty(shape, dtype=dt, device=x.device)
             args.append((x, xs, y, _strided(y, name + "_out", dt, shape, dev)))
         out.append(y)
     (q, qs, qo, qos), (k, ks, ko, kos) = args
@@ -514,9 +521,9 @@ class QCache:
 
     def __init__(self, k, v, k_scale, v_scale, k_open=None, v_open=None):
         B, H, M, C, d = k.shape
-        dev = k.device
-        if dev.type != "cuda":
-            raise ValueError(f"the cache lives on a GPU, got {dev}")
+        dev = k.get_device()
+        if dev < 0:
+            raise ValueError(f"the cache lives on a GPU, got {k.device}")
         _take(k, "k", torch.uint8, (B, H, M, C, d), dev)
         _take(v, "v", torch.uint8, (B, H, M, d, C), dev)
         _take(k_scale, "k_scale", torch.float32, (B, H, M), dev)
@@ -527,22 +534,24 @@ class QCache:
             _take(k_open, "k_open", k_open.dtype, (B, H, C, d), dev)
             _take(v_open, "v_open", k_open.dtype, (B, H, C, d), dev)
         self.k, self.v, self.k_scale, self.v_scale, self.k_open, self.v_open = k, v, k_scale, v_scale, k_open, v_open
+        self.device, self._shape = dev, (B, H, M, C, d)
         self._c = QCacheBuffers(*(_ptr(x) for x in (k, v, k_scale, v_scale, k_open, v_open)))
         self.address = ctypes.addressof(self._c)
 
     def check(self, p: Problem, appending=False):
         """ValueError unless this is a cache of problem p on the current device."""
-        if self.k.shape != (p.B, p.Hkv, pisa_qcache_blocks(p), p.C, p.d):
-            raise ValueError(f"the cache's codes {tuple(self.k.shape)} do not fit {p}")
-        if self.k.device != _device():
-            raise ValueError(f"the cache is on {self.k.device}, the current device is {_device()}")
+        B, H, M, C, d = self._shape
+        if (B, H, C, d) != (p.B, p.Hkv, p.C, p.d) or M != -(-(p.Ncap or p.N) // C):
+            raise ValueError(f"the cache's codes {self._shape} do not fit {p}")
+        if self.device != torch.cuda.current_device():
+            raise ValueError(f"the cache is on cuda:{self.device}, the current device is cuda:{torch.cuda.current_device()}")
         if appending and (self.k_open is None or self.k_open.dtype != _TORCH[p.dtype]):
             raise ValueError("appending needs k_open and v_open in the problem's dtype")
 
 
 def make_qcache(p: Problem, device=None):
     """An empty cache for problem p (reserving Ncap tokens)."""
-    M, dev = pisa_qcache_blocks(p), _device() if device is None else device
+    M, dev = pisa_qcache_blocks(p), torch.device("cuda", torch.cuda.current_device()) if device is None else device
     new = dict(device=dev)
     k = torch.zeros((p.B, p.Hkv, M, p.C, p.d), dtype=torch.uint8, **new)
     v = torch.zeros((p.B, p.Hkv, M, p.d, p.C), dtype=torch.uint8, **new)
@@ -555,21 +564,23 @@ def qcache_append(p: Problem, cache: QCache, k_new, v_new, n_old: int, pyramid=N
     """Append rows n_old .. N-1 (k_new, v_new: [B, Hkv, N - n_old, d], views with a contiguous last dimension) to
     the cache, and bring the pyramid with it where one is given."""
     cache.check(p, appending=True)
-    shape, dt, dev = (p.B, p.Hkv, p.N - n_old, p.d), _TORCH[p.dtype], cache.k.device
+    shape, dt, dev = (p.B, p.Hkv, p.N - n_old, p.d), _TORCH[p.dtype], cache.device
     ks, vs = _strided(k_new, "k_new", dt, shape, dev), _strided(v_new, "v_new", dt, shape, dev)
     if pyramid is not None:
-        _take(pyramid, "pyramid", torch.float32, (p.B, p.Hkv, pisa_pyramid_layout(p)[1], p.d), dev)
+        _take(pyramid, "pyramid", torch.float32, (p.B, p.Hkv, pyramid.shape[2], p.d), dev)
+        if pyramid.numel() * 4 != pisa_pyramid_bytes(p):
+            raise ValueError(f"pyramid: {tuple(pyramid.shape)} does not fit {p}")
     pisa_qcache_append(p, cache, k_new, ks, v_new, vs, n_old, pyramid, stream)
 
 
 def qcache_attn_fwd(p: Problem, cache: QCache, q, block_idx, stream=None):
     """Allocate outputs and workspace, run pisa_qcache_attn_fwd; returns (o, lse)."""
     cache.check(p)
-    dev = cache.k.device
+    dev = cache.device
     _take(q, "q", _TORCH[p.dtype], (p.B, p.H, p.Nq, p.d), dev)
     _take(block_idx, "block_idx", torch.int32, (p.B, p.Hkv, p.Nq, p.K), dev)
     o = torch.empty_like(q)
-    lse = torch.empty((p.B, p.H, p.Nq), dtype=torch.float32, device=dev)
+    lse = torch.empty((p.B, p.H, p.Nq), dtype=torch.float32, device=q.device)
     nb = pisa_qcache_attn_workspace_bytes(p)
-    pisa_qcache_attn_fwd(p, cache, q, block_idx, o, lse, _workspace(nb, dev), nb, stream)
+    pisa_qcache_attn_fwd(p, cache, q, block_idx, o, lse, _workspace(nb, q.device), nb, stream)
     return o, lse
