@@ -368,11 +368,16 @@ __global__ __launch_bounds__(256) void pool_runs_kernel(float* __restrict__ pyr,
 // The first run is that of the last old leaf block: every level inside an
 // earlier run was stored by n_old tokens already (level s + 1 has two nodes as
 // soon as a second run begins).
+// A pyramid whose two lowest levels fit 64 KB of LDS takes them all there, in one
+// launch (8 heads of 128: 64 leaf blocks 14.8 us with the append against 17.2, 141
+// blocks 26.8 against 25.5).
 hipError_t launch_pyramid_levels(const Geo& geo, int BH, int D, float* pyr, int n_old, hipStream_t st) {
+  if (geo.Lstore < 2) return hipSuccess;
+  if (static_cast<size_t>(geo.M[1] + geo.M[2]) * D * sizeof(float) <= 65536) return launch_pool_top(geo, BH, D, 0, pyr, st);
   const int s = pool_s_levels(geo.g);
   int lpb = 1;
   for (int i = 0; i < s; ++i) lpb *= geo.g;
-  if (s > 0 && geo.Lstore >= 2) {
+  {
     const int run0 = n_old > 0 ? (n_old - 1) / geo.C / lpb : 0;
     const dim3 grid((geo.M[1] + lpb - 1) / lpb - run0, BH);
     ProfScope ps("pool_runs", st);
