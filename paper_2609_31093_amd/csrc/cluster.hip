@@ -19,7 +19,6 @@
 namespace pisa {
 
 constexpr int kClusterThreads = 1024;
-constexpr int kClusterRows = 1024;  // rows per workgroup chunk
 
 __device__ __forceinline__ bool cluster_pair(const ClusterArgs& a, int bh, int r, int slot, int& blk) {
   const int64_t rg = static_cast<int64_t>(bh) * a.Nq + a.row0 + r;
@@ -63,8 +62,8 @@ __global__ __launch_bounds__(kClusterThreads) void cluster_hist_kernel(ClusterAr
                                                                        int32_t* __restrict__ chunk_base) {
   extern __shared__ __align__(16) int32_t h[];
   const int bh = blockIdx.y;
-  const int r0 = blockIdx.x * kClusterRows;
-  const int nr = min(kClusterRows, a.nrows - r0);
+  const int r0 = blockIdx.x * a.chunk_rows;
+  const int nr = min(a.chunk_rows, a.nrows - r0);
   for (int i = threadIdx.x; i < a.M1; i += kClusterThreads) h[i] = 0;
   __syncthreads();
   const int npairs = nr * a.S;
@@ -238,8 +237,8 @@ __global__ __launch_bounds__(kClusterThreads) void cluster_scatter_kernel(Cluste
                                                                           int32_t* __restrict__ pairs) {
   extern __shared__ __align__(16) int32_t h[];
   const int bh = blockIdx.y;
-  const int r0 = blockIdx.x * kClusterRows;
-  const int nr = min(kClusterRows, a.nrows - r0);
+  const int r0 = blockIdx.x * a.chunk_rows;
+  const int nr = min(a.chunk_rows, a.nrows - r0);
   // bin i of this chunk starts at its cluster's offset plus the chunk's
   // offset inside the cluster (reserved by cluster_hist_kernel)
   const int32_t* go = offs + static_cast<int64_t>(bh) * a.M1;
@@ -257,9 +256,9 @@ __global__ __launch_bounds__(kClusterThreads) void cluster_scatter_kernel(Cluste
   }
 }
 
-size_t cluster_ws(int BH, int M1, int64_t max_pairs, int max_rows) {
+size_t cluster_ws(int BH, int M1, int64_t max_pairs, int max_rows, int chunk_rows) {
   const size_t ncl = static_cast<size_t>(BH) * M1;
-  const size_t nchunk = static_cast<size_t>(BH) * ((max_rows + kClusterRows - 1) / kClusterRows);
+  const size_t nchunk = static_cast<size_t>(BH) * ((max_rows + chunk_rows - 1) / chunk_rows);
   return 3 * ((ncl + 1) * 4 + 256) + (nchunk * M1 * 4 + 256) + static_cast<size_t>(max_pairs) * 4 + 256;
 }
 
@@ -271,11 +270,11 @@ static size_t al(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
 hipError_t launch_cluster(const ClusterArgs& a, int BH, void* ws, ClusterOut* out, hipStream_t st, int tile) {
   // the rows read are [row0, row0 + nrows) of [0, Nq): refuse anything else
-  if (a.row0 < 0 || a.nrows < 1 || a.row0 + a.nrows > a.Nq || a.M1 < 1 || tile < 1 ||
+  if (a.row0 < 0 || a.nrows < 1 || a.row0 + a.nrows > a.Nq || a.M1 < 1 || tile < 1 || a.chunk_rows < 1 ||
       (a.mode == kClusterLeafParent && a.g < 2))
     return hipErrorInvalidValue;
   const int64_t ncl = static_cast<int64_t>(BH) * a.M1;
-  const int nchunk = (a.nrows + kClusterRows - 1) / kClusterRows;  // row chunks per (batch, KV head)
+  const int nchunk = (a.nrows + a.chunk_rows - 1) / a.chunk_rows;  // row chunks per (batch, KV head)
   char* base = static_cast<char*>(ws);
   int32_t* hist = reinterpret_cast<int32_t*>(base);
   int32_t* offs = reinterpret_cast<int32_t*>(base + al((ncl + 1) * 4));

@@ -44,6 +44,7 @@ constexpr int kClusterLeafParent = 2;  // leaf scoring grouped by parent node: o
                                        // (row, parent) at the slot of its first non-forced child
 constexpr int kClusterAttnFar = 3;     // causal attention: every non-negative slot except the row's first,
                                        // previous and own leaf block (those are attended per leaf block)
+constexpr int kClusterRows = 1024;     // rows per workgroup of the grouping, unless the caller asks for others
 struct ClusterArgs {
   const int32_t* list;  // [BH, Nq, S] block per slot, -1 = none
   const int32_t* cnt;   // [BH, Nq] candidates per row (leaf mode only)
@@ -54,6 +55,7 @@ struct ClusterArgs {
   // (row >> skip_shift)]) were attended by the row-tile union kernel
   const uint8_t* skip = nullptr;
   int skip_shift = 0, skip_tiles = 0;
+  int chunk_rows = kClusterRows;
 };
 constexpr int kClusterTile = 256;  // pairs per inner tile of the block attention's workgroup chunks
 struct ClusterOut {
@@ -63,8 +65,8 @@ struct ClusterOut {
   int64_t ncl;           // BH*M1
 };
 // workspace of launch_cluster for up to max_pairs pairs and max_rows rows per
-// (batch, KV head) in one launch
-size_t cluster_ws(int BH, int M1, int64_t max_pairs, int max_rows);
+// (batch, KV head) in one launch (the launch's rows per workgroup: chunk_rows)
+size_t cluster_ws(int BH, int M1, int64_t max_pairs, int max_rows, int chunk_rows = kClusterRows);
 
 // Chunk w of the cluster list when the consumer takes up to `tile` pairs per
 // workgroup (the tile offsets of launch_cluster(..., tile)): its cluster (the

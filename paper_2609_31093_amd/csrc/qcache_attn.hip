@@ -11,10 +11,14 @@
 //                    are dealt so that a lane reads D/4 consecutive bytes.
 //   O^T += V^T P^T   the same keys: a lane reads KU/4 consecutive tokens of one
 //                    dimension, which is why the cache keeps values transposed.
-// e4m3 times a power of two is exact in bf16, and so are its products with q in
-// fp32.  32-bit queries are split into three bf16 terms that add up to them
-// exactly, and so are their weights; bf16 queries' weights are rounded to bf16
-// (relative 2^-8 at most each, as in the other attention kernels), their sum is not.
+// An e4m3 key times its power of two is exact in bf16, and so are its products
+// with q in fp32.  32-bit queries are split into three bf16 terms that add up to
+// them exactly, and so are their weights.  bf16 queries' weights are rounded to
+// fp16 (relative 2^-11; bf16's 2^-8 left the result 1.3 times as far from the
+// exact one as rounding it does), in which value codes are exact too; the values'
+// scale is applied to the product in fp32.  Those weights are taken up to 2^14
+// (kHeadroom), so that ones of 2^-28 of the largest are still normal numbers.
+// Sums of weights are not rounded.
 #include <algorithm>
 
 #include "attn_shared.h"
@@ -75,6 +79,48 @@ __device__ __forceinline__ void split_terms(const float (&x)[8], bf16x8a (&t)[NT
   }
 }
 
+// log2 of the largest weight.
+template <int NT>
+constexpr float kHeadroom = NT == 1 ? 14.f : 0.f;
+
+// Weights as the values' operands: fp16, or with NT = 3 bf16 terms, and four
+// codes (unscaled) to go with them.
+typedef _Float16 f16x2a __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8a __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ uint32_t pack2_f16(float a, float b) {
+  const f32x2_t v = {a, b};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2a));
+}
+template <int NT>
+struct Weights {
+  bf16x8a t[NT];
+  __device__ __forceinline__ void set(const float (&p)[8]) { split_terms<NT>(p, t); }
+  static __device__ __forceinline__ bf16x8a codes(uint32_t w0, uint32_t w1) { return codes8_bf16(w0, w1, 1.f); }
+  __device__ __forceinline__ f32x4a times(bf16x8a v, f32x4a acc) const {
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, t[j], acc, 0, 0, 0);
+    return acc;
+  }
+};
+template <>
+struct Weights<1> {
+  f16x8a t;
+  __device__ __forceinline__ void set(const float (&p)[8]) {
+    t = __builtin_bit_cast(f16x8a, make_uint4(pack2_f16(p[0], p[1]), pack2_f16(p[2], p[3]), pack2_f16(p[4], p[5]), pack2_f16(p[6], p[7])));
+  }
+  static __device__ __forceinline__ uint2 codes4(uint32_t w) {
+    return make_uint2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, false)),
+                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, true)));
+  }
+  static __device__ __forceinline__ f16x8a codes(uint32_t w0, uint32_t w1) {
+    const uint2 a = codes4(w0), b = codes4(w1);
+    return __builtin_bit_cast(f16x8a, make_uint4(a.x, a.y, b.x, b.y));
+  }
+  __device__ __forceinline__ f32x4a times(f16x8a v, f32x4a acc) const {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(v, t, acc, 0, 0, 0);
+  }
+};
+
 // Word w of codes at token `at`: those of tokens >= limit cleared.
 __device__ __forceinline__ uint32_t keep_below(uint32_t w, int at, int limit) {
   const int n = limit - at;
@@ -92,9 +138,8 @@ struct Unit {
   static constexpr int VW = KU / 16;  // words of a lane's part of a dimension (KU/4 tokens)
   uint32_t kw[MT][KW], vw[DT][VW];
   float ksc, vsc;
-  int nkeys;  // visible keys, from the first on
 
-  __device__ __forceinline__ void load(const QCache& c, int64_t cell, int C, int u, int visible, int col, int grp) {
+  __device__ __forceinline__ void load(const QCache& c, int64_t cell, int C, int u, int col, int grp) {
     const uint8_t* kp = c.k + (cell * C + u * KU) * D + grp * (D / 4);
     const uint8_t* vp = c.v + cell * C * D + u * KU + grp * (KU / 4);
 #pragma unroll
@@ -119,85 +164,156 @@ struct Unit {
     }
     ksc = c.k_scale[cell];
     vsc = c.v_scale[cell];
-    nkeys = visible;
+  }
+  // Keeps the compiler from turning all codes into operands ahead of a loop,
+  // which its registers could not hold.
+  __device__ __forceinline__ void pin() {
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+      for (int i = 0; i < KW; ++i) asm volatile("" : "+v"(kw[mt][i]));
+    }
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+#pragma unroll
+      for (int i = 0; i < VW; ++i) asm volatile("" : "+v"(vw[dt][i]));
+    }
+  }
+  // Clears the values' codes of tokens from `limit` on (0 times a NaN code would
+  // not be 0).
+  __device__ __forceinline__ void clear_from(int limit, int grp) {
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+#pragma unroll
+      for (int i = 0; i < VW; ++i) vw[dt][i] = keep_below(vw[dt][i], grp * (KU / 4) + 4 * i, limit);
+    }
+  }
+  __device__ __forceinline__ bf16x8a key(int mt, int ks) const { return codes8_bf16(kw[mt][2 * ks], kw[mt][2 * ks + 1], ksc); }
+  template <int NT>
+  __device__ __forceinline__ auto value(int st, int dt) const { return Weights<NT>::codes(vw[dt][2 * st], vw[dt][2 * st + 1]); }
+  template <int NT>
+  __device__ __forceinline__ auto value_below(int st, int dt, int limit, int grp) const {
+    const int at = grp * (KU / 4) + 8 * st;
+    return Weights<NT>::codes(keep_below(vw[dt][2 * st], at, limit), keep_below(vw[dt][2 * st + 1], at + 4, limit));
+  }
+  __device__ __forceinline__ bool nan_value() const {  // among any lane's values
+    uint32_t any = 0;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+#pragma unroll
+      for (int i = 0; i < VW; ++i) any |= ((vw[dt][i] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+    }
+    return __any(any != 0);
   }
 };
 
-// Running softmax of a wavefront's 16 columns over key units.
+// Logits of a unit for 16 columns, masked: s[mt][i] is key grp*KU/4 + 4*mt + i.
+// nkeys: this column's visible keys, from the first on.
+template <int D, int KU, int NT>
+__device__ __forceinline__ void unit_logits(const Unit<D, KU>& u, const bf16x8a (&qt)[D / 32][NT], bool partial, int nkeys, int grp,
+                                            f32x4a (&s)[KU / 16]) {
+#pragma unroll
+  for (int mt = 0; mt < KU / 16; ++mt) {
+    s[mt] = f32x4a{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int ks = 0; ks < D / 32; ++ks) {
+      const bf16x8a kv = u.key(mt, ks);
+#pragma unroll
+      for (int j = 0; j < NT; ++j) s[mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kv, qt[ks][j], s[mt], 0, 0, 0);
+    }
+  }
+  if (partial) {
+#pragma unroll
+    for (int mt = 0; mt < KU / 16; ++mt) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[mt][i] = grp * (KU / 4) + 4 * mt + i < nkeys ? s[mt][i] : -INFINITY;
+    }
+  }
+}
+// A column's largest logit.
+template <int MT>
+__device__ __forceinline__ float column_max(const f32x4a (&s)[MT]) {
+  float mx = -INFINITY;
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) mx = fmaxf(mx, fmaxf(fmaxf(s[mt][0], s[mt][1]), fmaxf(s[mt][2], s[mt][3])));
+  mx = fmaxf(mx, __shfl_xor(mx, 16));
+  return fmaxf(mx, __shfl_xor(mx, 32));
+}
+// Logits to weights 2^(s * qscale2 - ref), as operands; returns this lane's sum.
+template <int MT, int NT>
+__device__ __forceinline__ float weights(const f32x4a (&s)[MT], float qscale2, float ref, Weights<NT> (&pt)[MT / 2]) {
+  float sum = 0.f;
+#pragma unroll
+  for (int st = 0; st < MT / 2; ++st) {
+    float p[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      p[i] = fast_exp2(fmaf(s[2 * st + i / 4][i % 4], qscale2, -ref));
+      sum += p[i];
+    }
+    pt[st].set(p);
+  }
+  return sum;
+}
+// Dimension tile dt of the weights times the value codes.
+template <int D, int KU, int NT>
+__device__ __forceinline__ f32x4a value_tile(const Unit<D, KU>& u, int dt, const Weights<NT> (&pt)[KU / 32]) {
+  f32x4a acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int st = 0; st < KU / 32; ++st) acc = pt[st].times(u.template value<NT>(st, dt), acc);
+  return acc;
+}
+// The same where a NaN value is seen by some columns and hidden from others (a
+// weight of 0 does not hide it): a product for each column, without the codes
+// that this column does not see.
+template <int D, int KU, int NT>
+__device__ __forceinline__ f32x4a value_tile_by_column(const Unit<D, KU>& u, int dt, const Weights<NT> (&pt)[KU / 32], int nkeys,
+                                                       int grp) {
+  f32x4a kept = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+  for (int c = 0; c < 16; ++c) {
+    const int limit = __builtin_amdgcn_readlane(nkeys, c);
+    f32x4a x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int st = 0; st < KU / 32; ++st) x = pt[st].times(u.template value_below<NT>(st, dt, limit, grp), x);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) kept[i] = (threadIdx.x & 15) == c ? x[i] : kept[i];
+  }
+  return kept;
+}
+
+// Running softmax of a wavefront's 16 columns over key units.  MIXED: the
+// columns' visible keys differ (otherwise the hidden values' codes are cleared),
+// and the units are of one block, whose values' scale is left to the caller.
 template <int D, int KU, int NT>
 struct Softmax {
   using U = Unit<D, KU>;
-  static constexpr int KS = D / 32;  // k-steps of S
   f32x4a oacc[U::DT];
-  float m = -INFINITY, l = 0.f;
+  float m = -INFINITY, l = 0.f;  // what the weights are relative to (log2), their sum
 
   __device__ __forceinline__ Softmax() {
 #pragma unroll
     for (int dt = 0; dt < U::DT; ++dt) oacc[dt] = f32x4a{0.f, 0.f, 0.f, 0.f};
   }
-  __device__ __forceinline__ void add(U& u, const bf16x8a (&qt)[KS][NT], float qscale2, int grp) {
+  template <bool MIXED>
+  __device__ __forceinline__ void add(U& u, const bf16x8a (&qt)[D / 32][NT], float qscale2, int nkeys, int grp) {
+    const bool partial = MIXED ? __any(nkeys < KU) : nkeys < KU;
+    if (!MIXED && partial) u.clear_from(nkeys, grp);
     f32x4a s[U::MT];
-#pragma unroll
-    for (int mt = 0; mt < U::MT; ++mt) {
-      s[mt] = f32x4a{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const bf16x8a kv = codes8_bf16(u.kw[mt][2 * ks], u.kw[mt][2 * ks + 1], u.ksc);
-#pragma unroll
-        for (int j = 0; j < NT; ++j) s[mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kv, qt[ks][j], s[mt], 0, 0, 0);
-      }
-    }
-    // lane (col, grp) holds keys grp*KU/4 + 4*mt + i; hidden ones: weight 0, and
-    // their codes are cleared (0 times a NaN code would not be 0)
-    const int k0 = grp * (KU / 4);
-    if (u.nkeys < KU) {
-#pragma unroll
-      for (int mt = 0; mt < U::MT; ++mt) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[mt][i] = k0 + 4 * mt + i < u.nkeys ? s[mt][i] : -INFINITY;
-      }
-#pragma unroll
-      for (int dt = 0; dt < U::DT; ++dt) {
-#pragma unroll
-        for (int i = 0; i < U::VW; ++i) u.vw[dt][i] = keep_below(u.vw[dt][i], k0 + 4 * i, u.nkeys);
-      }
-    }
-    float mx = -INFINITY;
-#pragma unroll
-    for (int mt = 0; mt < U::MT; ++mt) mx = fmaxf(mx, fmaxf(fmaxf(s[mt][0], s[mt][1]), fmaxf(s[mt][2], s[mt][3])));
-    mx = fmaxf(mx, __shfl_xor(mx, 16));
-    mx = fmaxf(mx, __shfl_xor(mx, 32));
-    const float mn = fmaxf(m, mx * qscale2);
+    unit_logits<D, KU, NT>(u, qt, partial, nkeys, grp, s);
+    const float mn = fmaxf(m, column_max<U::MT>(s) * qscale2 - kHeadroom<NT>);
     const float ref = mn == -INFINITY ? 0.f : mn;
     const float corr = fast_exp2(m - ref);
     m = mn;
-    float sum = 0.f;
-#pragma unroll
-    for (int mt = 0; mt < U::MT; ++mt) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        s[mt][i] = fast_exp2(fmaf(s[mt][i], qscale2, -ref));
-        sum += s[mt][i];
-      }
-    }
-    l = l * corr + sum;
+    Weights<NT> pt[U::MT / 2];
+    l = l * corr + weights<U::MT, NT>(s, qscale2, ref, pt);
+    const bool by_column = MIXED && partial && u.nan_value();
+    const float scale = MIXED ? 1.f : u.vsc;
 #pragma unroll
     for (int dt = 0; dt < U::DT; ++dt) {
+      const f32x4a x = MIXED && by_column ? value_tile_by_column<D, KU, NT>(u, dt, pt, nkeys, grp) : value_tile<D, KU, NT>(u, dt, pt);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) oacc[dt][i] *= corr;
-    }
-#pragma unroll
-    for (int st = 0; st < U::MT / 2; ++st) {
-      const float p[8] = {s[2 * st][0], s[2 * st][1], s[2 * st][2], s[2 * st][3],
-                          s[2 * st + 1][0], s[2 * st + 1][1], s[2 * st + 1][2], s[2 * st + 1][3]};
-      bf16x8a pt[NT];
-      split_terms<NT>(p, pt);
-#pragma unroll
-      for (int dt = 0; dt < U::DT; ++dt) {
-        const bf16x8a vv = codes8_bf16(u.vw[dt][2 * st], u.vw[dt][2 * st + 1], u.vsc);
-#pragma unroll
-        for (int j = 0; j < NT; ++j) oacc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, pt[j], oacc[dt], 0, 0, 0);
-      }
+      for (int i = 0; i < 4; ++i) oacc[dt][i] = fmaf(x[i], scale, oacc[dt][i] * corr);
     }
   }
 };
@@ -237,30 +353,31 @@ __global__ __launch_bounds__(NW * 64, 2) void qcache_attn_kernel(QAttnArgs a) {
   const int per = a.C / KU;  // key units of a block
   const int ntask = a.K * per, step = a.splits * NW;
   // the next unit from `task` on with a visible key: loaded into u; ntask at the end
-  auto fetch = [&](int task, Unit<D, KU>& u) {
+  auto fetch = [&](int task, Unit<D, KU>& u, int& visible) {
     for (; task < ntask; task += step) {
       const int slot = task / per, part = task - slot * per;
       const int blk = __builtin_amdgcn_readlane(slot < 64 ? sel0 : sel1, slot & 63);
       if (static_cast<uint32_t>(blk) >= static_cast<uint32_t>(a.M1)) continue;  // padding
-      const int visible = min(KU, end - (blk * a.C + part * KU));
+      visible = min(KU, end - (blk * a.C + part * KU));
       if (visible <= 0) continue;
-      u.load(a.c, static_cast<int64_t>(bh) * a.c.M + blk, a.C, part, visible, col, grp);
+      u.load(a.c, static_cast<int64_t>(bh) * a.c.M + blk, a.C, part, col, grp);
       break;
     }
     return task;
   };
   Unit<D, KU> ua, ub;
-  int ta = fetch(split * NW + wave, ua);
+  int na = 0, nb = 0;
+  int ta = fetch(split * NW + wave, ua, na);
   bf16x8a qt[KS][NT];
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) split_terms<NT>(qx[ks], qt[ks]);
   Softmax<D, KU, NT> sm;
   while (ta < ntask) {  // the next unit's loads are in flight while one is added
-    const int tb = fetch(ta + step, ub);
-    sm.add(ua, qt, a.qscale2, grp);
+    const int tb = fetch(ta + step, ub, nb);
+    sm.template add<false>(ua, qt, a.qscale2, na, grp);
     if (tb >= ntask) break;
-    ta = fetch(tb + step, ua);
-    sm.add(ub, qt, a.qscale2, grp);
+    ta = fetch(tb + step, ua, na);
+    sm.template add<false>(ub, qt, a.qscale2, nb, grp);
   }
   auto& oacc = sm.oacc;
   const float m = sm.m;
@@ -363,6 +480,227 @@ __global__ __launch_bounds__(64) void qcache_merge_kernel(QAttnArgs a) {
   if (a.lse && lane == 0) a.lse[orow] = ll == 0.f ? -INFINITY : (ref + fast_log2(ll)) * kLn2;
 }
 
+// Many rows (bf16): the (row, slot) pairs are grouped by key block, and a
+// wavefront's 16 columns are the heads of 16 / G pairs of one block instead of
+// one row's G heads: the block's codes are read once and turned into operands
+// once for all of them.  Each pair leaves its own softmax of the block, normalised,
+// in units of the values' scale (so at most 448) and rounded to fp16 (relative
+// 2^-11; its log sum stays in fp32), and qcache_combine_kernel merges a row's K.
+//   part_o [BH][rows][K][G][D], within each 32 dimensions in the order
+//   [grp][dimension tile 0..1][4], so that a lane stores 16 bytes at a time
+constexpr int kBlockWaves = 4;
+constexpr int kBlockTiles = 4;  // tiles of a wavefront
+
+struct QBlockArgs {
+  QAttnArgs a;
+  const int32_t *offs, *toffs, *pairs;  // launch_cluster
+  int64_t ncl;
+  uint16_t* part_o;
+  float* part_lse;
+  int nrows;  // rows of this launch, from a.row0 on
+  int chunk;  // pairs of one block per workgroup, at most
+};
+
+// WHOLE: a unit is a block, whose codes stay in registers (152 of them, three
+// wavefronts on a SIMD; with the operands there instead, 256 and two, the same
+// 4096 rows of 16 heads took 157 us in this kernel against 126); otherwise its
+// units are read again, from the cache, for every tile.  What bounds it is the
+// partials' 268 MB out and the queries' 268 MB in.
+template <int D, int KU, bool WHOLE>
+__global__ __launch_bounds__(kBlockWaves * 64, WHOLE ? (D == 128 ? 3 : 4) : 2) void qcache_block_kernel(QBlockArgs p) {
+  constexpr int KS = D / 32, DT = D / 16;
+  const QAttnArgs& a = p.a;
+  int64_t cl;
+  int beg, end;
+  if (!cluster_chunk(p.offs, p.toffs, p.ncl, blockIdx.x, p.chunk, cl, beg, end)) return;
+  const int bh = static_cast<int>(cl / a.M1), blk = static_cast<int>(cl - static_cast<int64_t>(bh) * a.M1);
+  const int b = bh / a.Hkv, h = bh - b * a.Hkv;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 15, grp = lane >> 4;
+  const int ppt = 16 / a.G;                // pairs of a tile
+  const int cp = col / a.G, hh = col - cp * a.G;  // this column's pair and head
+  const bool head = cp < ppt;
+  const int per = a.C / KU;
+  const int64_t cell = static_cast<int64_t>(bh) * a.c.M + blk;
+  const int tok0 = blk * a.C;
+
+  // this wavefront's tiles: wave, wave + 4, ...; their pairs are read up front and
+  // the next tile's queries while one is computed
+  const int ntile = (end - beg + ppt - 1) / ppt;
+  const int mine = (ntile - wave + kBlockWaves - 1) / kBlockWaves;
+  if (mine <= 0) return;
+  int words[kBlockTiles];
+#pragma unroll
+  for (int j = 0; j < kBlockTiles; ++j) {
+    const int at = beg + (wave + j * kBlockWaves) * ppt + cp;
+    words[j] = head && at < end ? p.pairs[at] : -1;
+  }
+  Unit<D, KU> whole;
+  if constexpr (WHOLE) whole.load(a.c, cell, a.C, 0, col, grp);
+  uint4 qn[KS];
+  auto gather = [&](int word) {
+    const uint16_t* q = static_cast<const uint16_t*>(a.q) +
+                        ((static_cast<int64_t>(b) * a.H + h * a.G + hh) * a.Nq + a.row0 + (word >> 8)) * D + grp * (D / 4);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      qn[ks] = make_uint4(0, 0, 0, 0);
+      if (word >= 0) qn[ks] = *reinterpret_cast<const uint4*>(q + ks * 8);
+    }
+  };
+  gather(words[0]);
+  if constexpr (WHOLE) {
+    whole.clear_from(a.N - tok0, grp);
+  }
+#pragma unroll 1
+  for (int j = 0; j < mine; ++j) {
+    bf16x8a qt[KS][1];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qt[ks][0] = u4_as_bf16x8(qn[ks]);
+    const int word = words[0];
+    const bool live = word >= 0;
+    const int rr = live ? word >> 8 : 0, slot = word & 255;
+    const int t = a.N - a.Nq + a.row0 + rr;
+    const int visible = live ? (a.causal ? min(a.N, t + 1) : a.N) - tok0 : a.C;  // keys of the block
+#pragma unroll
+    for (int i = 0; i + 1 < kBlockTiles; ++i) words[i] = words[i + 1];
+    if (j + 1 < mine) gather(words[0]);
+    uint16_t* dst = nullptr;
+    const int64_t pidx = ((static_cast<int64_t>(bh) * p.nrows + rr) * a.K + slot) * a.G + hh;
+    if (live) dst = p.part_o + pidx * D + grp * 8;
+    auto store = [&](int j, f32x4a x, f32x4a y, float inv) {  // dimension tiles 2j and 2j + 1
+      uint4 w;
+      w.x = pack2_f16(x[0] * inv, x[1] * inv);
+      w.y = pack2_f16(x[2] * inv, x[3] * inv);
+      w.z = pack2_f16(y[0] * inv, y[1] * inv);
+      w.w = pack2_f16(y[2] * inv, y[3] * inv);
+      if (live) *reinterpret_cast<uint4*>(dst + j * 32) = w;
+    };
+    float m, l, inv;
+    auto close = [&] {  // the column's sum over its four lanes
+      l += __shfl_xor(l, 16);
+      l += __shfl_xor(l, 32);
+      inv = l == 0.f ? 0.f : 1.f / l;
+    };
+    if constexpr (WHOLE) {
+      // one softmax per tile: its sum is known before the values, whose tiles are
+      // stored as they come
+      whole.pin();
+      const int nkeys = min(KU, visible);
+      const bool partial = __any(nkeys < KU);
+      f32x4a s[KU / 16];
+      unit_logits<D, KU, 1>(whole, qt, partial, nkeys, grp, s);
+      m = column_max<KU / 16>(s) * a.qscale2 - kHeadroom<1>;
+      Weights<1> pt[KU / 32];
+      l = weights<KU / 16, 1>(s, a.qscale2, m == -INFINITY ? 0.f : m, pt);
+      close();
+      if (partial && whole.nan_value()) {
+#pragma unroll
+        for (int dj = 0; dj < DT / 2; ++dj)
+          store(dj, value_tile_by_column<D, KU, 1>(whole, 2 * dj, pt, nkeys, grp),
+                value_tile_by_column<D, KU, 1>(whole, 2 * dj + 1, pt, nkeys, grp), inv);
+      } else {
+#pragma unroll
+        for (int dj = 0; dj < DT / 2; ++dj)
+          store(dj, value_tile<D, KU, 1>(whole, 2 * dj, pt), value_tile<D, KU, 1>(whole, 2 * dj + 1, pt), inv);
+      }
+    } else {
+      Softmax<D, KU, 1> sm;
+      for (int part = 0; part < per; ++part) {
+        Unit<D, KU> u;
+        u.load(a.c, cell, a.C, part, col, grp);
+        u.clear_from(a.N - tok0 - part * KU, grp);
+        sm.template add<true>(u, qt, a.qscale2, min(KU, visible - part * KU), grp);
+      }
+      m = sm.m;
+      l = sm.l;
+      close();
+#pragma unroll
+      for (int dj = 0; dj < DT / 2; ++dj) store(dj, sm.oacc[2 * dj], sm.oacc[2 * dj + 1], inv);
+    }
+    if (live && grp == 0) p.part_lse[pidx] = l == 0.f ? -INFINITY : m + fast_log2(l);
+  }
+}
+
+// One wavefront per (row, head): 16 lanes hold a partial (8 values each for
+// d = 128), so four slots at a time.
+template <int D>
+__global__ __launch_bounds__(256) void qcache_combine_kernel(QBlockArgs p) {
+  constexpr int E = D / 16;
+  constexpr int SPL = 4;  // rounds in flight
+  const QAttnArgs& a = p.a;
+  const int lane = threadIdx.x & 63;
+  const int64_t e = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);  // heads of a row side by side, as its partials
+  const int rr = static_cast<int>(e / a.G), hh = static_cast<int>(e - static_cast<int64_t>(rr) * a.G);
+  if (rr >= p.nrows) return;
+  const int grp = lane >> 4, sub = lane & 15;
+  const int bh = blockIdx.y, b = bh / a.Hkv;
+  const int hq = (bh - b * a.Hkv) * a.G + hh;
+  const int row = a.row0 + rr;
+  const int32_t* sel = a.idx + (static_cast<int64_t>(bh) * a.Nq + row) * a.K;
+  const int64_t base = (static_cast<int64_t>(bh) * p.nrows + rr) * a.K;
+  float m = -INFINITY, l = 0.f, o[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) o[e] = 0.f;
+  for (int s0 = grp; s0 < a.K; s0 += 4 * SPL) {
+    float ls[SPL], sc[SPL], x[SPL][E];
+#pragma unroll
+    for (int i = 0; i < SPL; ++i) {
+      const int slot = s0 + 4 * i;
+      const int blk = slot < a.K ? sel[slot] : -1;
+      const bool have = static_cast<uint32_t>(blk) < static_cast<uint32_t>(a.M1);  // padding left no partial
+      ls[i] = have ? p.part_lse[(base + slot) * a.G + hh] : -INFINITY;
+      sc[i] = have ? a.c.v_scale[static_cast<int64_t>(bh) * a.c.M + blk] : 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[i][e] = 0.f;
+      if (have) {
+        _Float16 raw[E];
+        __builtin_memcpy(raw, __builtin_assume_aligned(p.part_o + ((base + slot) * a.G + hh) * D + sub * E, 2 * E), 2 * E);
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[i][e] = static_cast<float>(raw[e]);
+      }
+    }
+    float top = m;
+#pragma unroll
+    for (int i = 0; i < SPL; ++i) top = fmaxf(top, ls[i]);
+    const float ref = top == -INFINITY ? 0.f : top;
+    const float f = fast_exp2(m - ref);
+    l *= f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] *= f;
+#pragma unroll
+    for (int i = 0; i < SPL; ++i) {
+      const float w = fast_exp2(ls[i] - ref);
+      l += w;
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] = fmaf(w * sc[i], x[i][e], o[e]);
+    }
+    m = top;
+  }
+#pragma unroll
+  for (int msk = 16; msk <= 32; msk <<= 1) {
+    const float m2 = __shfl_xor(m, msk), l2 = __shfl_xor(l, msk);
+    const float top = fmaxf(m, m2), ref = top == -INFINITY ? 0.f : top;
+    const float f = fast_exp2(m - ref), f2 = fast_exp2(m2 - ref);
+    l = l * f + l2 * f2;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = o[e] * f + __shfl_xor(o[e], msk) * f2;
+    m = top;
+  }
+  if (grp == 0) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const int64_t orow = (static_cast<int64_t>(b) * a.H + hq) * a.Nq + row;
+    uint16_t* dst = static_cast<uint16_t*>(a.o) + orow * D;
+    // value i of this lane's part is at position sub*E + i of the stored order
+#pragma unroll
+    for (int e = 0; e < E; e += 4) {
+      const int pos = sub * E + e;
+      const int d = pos / 32 * 32 + (pos & 4) * 4 + (pos % 32) / 8 * 4;
+      *reinterpret_cast<uint2*>(dst + d) = make_uint2(pack2_bf16(o[e] * inv, o[e + 1] * inv), pack2_bf16(o[e + 2] * inv, o[e + 3] * inv));
+    }
+    if (a.lse && sub == 0) a.lse[orow] = l == 0.f ? -INFINITY : (m + fast_log2(l)) * kLn2;
+  }
+}
+
 namespace {
 
 // How many wavefronts share a row's key units, NW of them in a workgroup and
@@ -430,11 +768,97 @@ hipError_t launch_nw(const Shape& s, const QAttnArgs& a, int nw, hipStream_t st)
 
 }  // namespace
 
+static size_t al256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
+
+// Does grouping the rows by block pay?  A row alone reads its K blocks, of 2 C D
+// bytes, at about 10 TB/s over all; grouped, a block is read once for many rows,
+// but each (row, slot) writes and reads back a partial of 2 D bytes a head (0.33
+// ns per KB and 64 keys of the block), and the grouping costs 45 us and 4.5 ns per
+// block of every KV head.  Measured, alone and grouped (us): 128-wide heads, 16
+// blocks of 64 keys, 32768 keys, 4 heads to a KV head: 2048 rows x KV heads 63 and
+// 69, 4096 112 and 84, 16384 369 and 223; 1 head: 2048 60 and 56, 16384 372 and
+// 94; 8 heads: 8192 213 and 210; 16 heads of 64, 8 blocks: 8192 65 and 140;
+// over 524288 keys, 4 heads: 8192 237 and 299, 16384 455 and 419.
+static bool use_blocks(const Shape& s, const Geo& geo) {
+  if (!s.bf16 || geo.M[1] > 16384) return false;  // the grouping's LDS histogram
+  const double rows = static_cast<double>(s.BH()) * s.Nq;
+  const double saved = rows * s.K * s.D / 1024 * (0.2 * s.C - 1.32 * s.G * std::max(1.0, s.C / 64.0));
+  return saved >= 45000 + 4.5 * s.BH() * geo.M[1];
+}
+
+// Rows per pass: their partials take at most 1 GB.
+constexpr size_t kPartialBytes = size_t(1) << 30;
+static int block_rows(const Shape& s) {
+  const size_t per_row = static_cast<size_t>(s.BH()) * s.K * s.G * (s.D * 2 + 4);
+  return static_cast<int>(std::min<size_t>(s.Nq, std::max<size_t>(kPartialBytes / per_row, 1)));
+}
+// Rows per workgroup of the grouping: about 4096 pairs (262144 pairs on 4 KV heads:
+// 28 us, 47 with 1024 rows).
+static int group_rows(const Shape& s) { return std::max(64, 4096 / s.K); }
+// Pairs of one block per workgroup: four tiles for each wavefront.
+static int pair_chunk(const Shape& s) { return 16 / s.G * kBlockWaves * kBlockTiles; }
+struct BlockWs {
+  size_t part_o, part_lse, cl, total;
+};
+static BlockWs block_layout(const Shape& s, const Geo& geo) {
+  const int rows = block_rows(s);
+  const size_t np = static_cast<size_t>(s.BH()) * rows * s.K;
+  BlockWs w{};
+  w.part_lse = al256(np * s.G * s.D * 2);
+  w.cl = w.part_lse + al256(np * s.G * 4);
+  w.total = w.cl + al256(cluster_ws(s.BH(), geo.M[1], static_cast<int64_t>(np), rows, group_rows(s)));
+  return w;
+}
+
+template <int D>
+static hipError_t launch_blocks(const Shape& s, const Geo& geo, const QAttnArgs& a, char* base, int ku, hipStream_t st) {
+  const BlockWs w = block_layout(s, geo);
+  const int rows = block_rows(s);
+  QBlockArgs p{};
+  p.a = a;
+  p.part_o = reinterpret_cast<uint16_t*>(base + w.part_o);
+  p.part_lse = reinterpret_cast<float*>(base + w.part_lse);
+  for (int row0 = 0; row0 < s.Nq; row0 += rows) {
+    p.a.row0 = row0;
+    p.nrows = std::min(rows, s.Nq - row0);
+    ClusterArgs ca{a.idx, nullptr, s.K, s.Nq, s.N, s.C, s.K, s.causal, geo.M[1], kClusterAttn, row0, p.nrows, s.g};
+    ca.chunk_rows = group_rows(s);
+    p.chunk = pair_chunk(s);
+    ClusterOut co{};
+    hipError_t e = launch_cluster(ca, s.BH(), base + w.cl, &co, st, p.chunk);
+    if (e != hipSuccess) return e;
+    p.offs = co.offs;
+    p.toffs = co.toffs;
+    p.pairs = co.pairs;
+    p.ncl = co.ncl;
+    {
+      ProfScope ps("qcache_block", st);
+      const unsigned grid = static_cast<unsigned>(
+          cluster_max_chunks(s.BH(), geo.M[1], static_cast<int64_t>(s.BH()) * p.nrows * s.K, p.chunk));
+      if (s.C == 64)
+        qcache_block_kernel<D, 64, true><<<grid, kBlockWaves * 64, 0, st>>>(p);
+      else if (s.C == 32)
+        qcache_block_kernel<D, 32, true><<<grid, kBlockWaves * 64, 0, st>>>(p);
+      else if (ku == 64)
+        qcache_block_kernel<D, 64, false><<<grid, kBlockWaves * 64, 0, st>>>(p);
+      else
+        qcache_block_kernel<D, 32, false><<<grid, kBlockWaves * 64, 0, st>>>(p);
+    }
+    {
+      ProfScope ps("qcache_combine", st);
+      qcache_combine_kernel<D><<<dim3(static_cast<unsigned>((static_cast<int64_t>(p.nrows) * s.G + 3) / 4), s.BH()), 256, 0, st>>>(p);
+    }
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 static size_t part_ml_at(const Shape& s, int splits) {
   return (static_cast<size_t>(s.BH()) * s.Nq * splits * s.G * s.D * sizeof(float) + 255) & ~static_cast<size_t>(255);
 }
 
-size_t qcache_attn_ws(const Shape& s, const Geo&) {
+size_t qcache_attn_ws(const Shape& s, const Geo& geo) {
+  if (use_blocks(s, geo)) return block_layout(s, geo).total;
   const int splits = spread(s, unit_keys(s)).splits;
   return splits > 1 ? part_ml_at(s, splits) + static_cast<size_t>(s.BH()) * s.Nq * splits * s.G * sizeof(float2) : 0;
 }
@@ -446,6 +870,8 @@ hipError_t launch_qcache_attn(const Shape& s, const Geo& geo, const QCache& c, c
   char* base = static_cast<char*>(ws);
   QAttnArgs a{c, q, idx, o, lse, reinterpret_cast<float*>(base), nullptr, s.H, s.Hkv, s.G, s.Nq, s.N, s.C, s.K, s.causal,
               geo.M[1], s.BH(), sp.splits, 0, kLog2e / sqrtf(static_cast<float>(s.D))};
+  if (use_blocks(s, geo))
+    return s.D == 128 ? launch_blocks<128>(s, geo, a, base, ku, st) : launch_blocks<64>(s, geo, a, base, ku, st);
   if (sp.splits > 1) a.part_ml = reinterpret_cast<float2*>(base + part_ml_at(s, sp.splits));
   if (s.bf16) {
     if (s.D == 128)

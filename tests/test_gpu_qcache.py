@@ -6,9 +6,10 @@ e4m3 value (ties to even) and nothing else.
 Tolerance of the attention.  Keys and values are exact in what they stand for.  A logit is a sum of d products, exact in
 32 bits (8 bits times 24 at most), so off by at most delta = (d + 4) 2^-24 sum|q_i k_i| / sqrt(d) in any order and after
 its scaling; the exponent of base 2 adds the rounding of its argument (2^-24 |z - m| / ln 2) and 2 ulp.  A weight is then
-off by w = exp(2 delta) - 1 + 2^-21 + 2^-23 max|z - m| relative, its sum likewise, and sums of n terms by n 2^-24; bf16 weights by another
-2^-8.  With W the sum of weight times |value|: |o - o_ref| <= (2 w + 2^-8 [bf16] + 2 n 2^-24) W + 2^-8 |o| [bf16] + 2^-23 |o|,
-|lse - lse_ref| <= delta + w + n 2^-24 + 2^-22 max(1, |lse|).
+off by w = exp(2 delta) - 1 + 2^-21 + 2^-23 max|z - m| relative, its sum likewise, and sums of n terms by n 2^-24; weights
+of bf16 queries by another 2^-11 (fp16; they reach down to 2^-28 of the largest before they lose bits, which n 2^-24
+covers).  With W the sum of weight times |value|: |o - o_ref| <= (2 w + 2^-11 [bf16] + 2 n 2^-24) W + 2^-8 |o| [bf16] +
+2^-23 |o|, |lse - lse_ref| <= delta + w + n 2^-24 + 2^-22 max(1, |lse|).
 """
 import math
 
@@ -190,8 +191,9 @@ def test_strided_rows_and_untouched_neighbours():
 
 # -------------------------------------------------------------- attention ---
 
-def reference(p, cache, q, idx):
-    """(o, lse, bound of o's error, of lse's) in 64 bits."""
+def reference(p, cache, q, idx, rows=None, more=0.0):
+    """(o, lse, bound of o's error, of lse's) in 64 bits, of the given rows (default: all; others stay 0); `more`: another
+    relative error of what is summed."""
     C, d, G, M = p.C, p.d, p.H // p.Hkv, -(-p.N // p.C)
     kk = values(cache.k) * cache.k_scale.double().cpu().numpy()[..., None, None]
     vv = values(cache.v).swapaxes(-1, -2) * cache.v_scale.double().cpu().numpy()[..., None, None]
@@ -199,10 +201,10 @@ def reference(p, cache, q, idx):
     o = np.zeros((p.B, p.H, p.Nq, d))
     lse = np.full((p.B, p.H, p.Nq), -np.inf)
     tol_o, tol_l = np.zeros_like(o), np.zeros_like(lse)
-    half = 2.0 ** -8 if p.dtype == pisa.PISA_DTYPE_BF16 else 0.0
+    half, weight = (2.0 ** -8, 2.0 ** -11) if p.dtype == pisa.PISA_DTYPE_BF16 else (0.0, 0.0)
     for b in range(p.B):
         for hk in range(p.Hkv):
-            for r in range(p.Nq):
+            for r in range(p.Nq) if rows is None else rows:
                 t = p.N - p.Nq + r if p.causal else p.N - 1
                 blocks = [j for j in sel[b, hk, r] if 0 <= j < M]
                 tok = np.concatenate([np.arange(j * C, min((j + 1) * C, t + 1)) for j in blocks] or [np.zeros(0, int)]).astype(int)
@@ -218,19 +220,21 @@ def reference(p, cache, q, idx):
                     o[b, h, r], lse[b, h, r] = w @ vt, m + math.log(total)
                     delta = (d + 4) * 2.0 ** -24 * (abs(kt) @ abs(q64[b, h, r])).max() / math.sqrt(d)
                     rel = math.expm1(2 * delta) + 2.0 ** -21 + 2.0 ** -23 * (m - z).max()
-                    tol_o[b, h, r] = (2 * rel + half + 2 * n * 2.0 ** -24) * (w @ abs(vt)) + (half + 2.0 ** -23) * abs(o[b, h, r])
+                    tol_o[b, h, r] = (2 * rel + weight + more + 2 * n * 2.0 ** -24) * (w @ abs(vt)) + (half + 2.0 ** -23) * abs(o[b, h, r])
                     tol_l[b, h, r] = delta + rel + n * 2.0 ** -24 + 2.0 ** -22 * max(1, abs(lse[b, h, r]))
     return o, lse, tol_o, tol_l
 
 
-def check_attention(p, cache, q, idx, o, lse):
-    want_o, want_l, tol_o, tol_l = reference(p, cache, q, idx)
+def check_attention(p, cache, q, idx, o, lse, rows=None):
+    want_o, want_l, tol_o, tol_l = reference(p, cache, q, idx, rows)
     got_o, got_l = o.double().cpu().numpy(), lse.double().cpu().numpy()
+    if rows is not None:
+        want_o, want_l, tol_o, tol_l, got_o, got_l = (x[:, :, rows] for x in (want_o, want_l, tol_o, tol_l, got_o, got_l))
     empty = np.isneginf(want_l)
     assert np.array_equal(np.isneginf(got_l), empty) and (got_o[empty] == 0).all()
     off = abs(got_o - want_o) - tol_o
     assert (off <= 0).all(), (off.max(), np.argwhere(off > 0)[:3])
-    off = (abs(got_l - want_l) - tol_l)[~empty]
+    off = abs(got_l[~empty] - want_l[~empty]) - tol_l[~empty]
     assert (off <= 0).all(), off.max()
 
 
@@ -289,6 +293,137 @@ def test_attention(shape):
     idx = random_selection(p, 4)
     o, lse = pisa.qcache_attn_fwd(p, cache, q, idx)
     check_attention(p, cache, q, idx, o, lse)
+
+
+# Rows enough to be grouped by block.  Their partials are normalised and rounded to fp16 before they are weighted and
+# summed: another 2^-11 of W.
+GROUPED = [
+    (1, 1, 1, 2500, 2600, 128, 64, 2, 16, 1, "bf16", 0),
+    (1, 4, 1, 3500, 9000, 128, 64, 2, 16, 1, "bf16", 9100),
+    (2, 6, 2, 1500, 2100, 64, 64, 2, 32, 1, "bf16", 0),
+    (1, 4, 4, 2300, 2300, 64, 32, 2, 30, 1, "bf16", 0),
+    (1, 5, 1, 2200, 4000, 128, 128, 4, 16, 1, "bf16", 0),
+    (1, 2, 2, 1200, 3333, 128, 96, 2, 16, 0, "bf16", 0),
+    (1, 3, 1, 1500, 2500, 64, 256, 2, 16, 1, "bf16", 0),
+    (1, 9, 1, 6500, 6600, 128, 128, 2, 50, 0, "bf16", 0),
+]
+
+
+def quick_selection(p, seed):
+    """random_selection for many rows: distinct blocks of the whole cache, some of them padding."""
+    M = -(-p.N // p.C)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    order = torch.rand((p.B, p.Hkv, p.Nq, M), generator=gen, device="cuda").argsort(-1)[..., :p.K].int()
+    order = torch.nn.functional.pad(order, (0, p.K - order.shape[-1]), value=-1)
+    drop = torch.rand(order.shape, generator=gen, device="cuda")
+    order = torch.where(drop < 0.1, -1, torch.where(drop < 0.15, M + 5, order))
+    order[:, :, ::97] = -1
+    return order.int().contiguous()
+
+
+def sample(p, seed, n=40):
+    rng = np.random.default_rng(seed)
+    return sorted({0, 1, 97, p.Nq - 1, p.Nq - 2, *rng.integers(0, p.Nq, n).tolist()})
+
+
+def check_grouped(p, cache, q, idx, o, lse, rows):
+    want_o, want_l, tol_o, tol_l = (x[:, :, rows] for x in reference(p, cache, q, idx, rows, more=2.0 ** -11))
+    got_o, got_l = o[:, :, rows].double().cpu().numpy(), lse[:, :, rows].double().cpu().numpy()
+    empty = np.isneginf(want_l)
+    assert np.array_equal(np.isneginf(got_l), empty) and (got_o[empty] == 0).all()
+    off = abs(got_o - want_o) - tol_o
+    assert (off <= 0).all(), (off.max(), np.argwhere(off > 0)[:3])
+    assert (abs(got_l[~empty] - want_l[~empty]) <= tol_l[~empty]).all()
+
+
+@pytest.mark.parametrize("shape", GROUPED, ids=str)
+def test_many_rows(shape):
+    B, H, Hkv, Nq, N, d, C, g, K, causal, dtype, cap = shape
+    p = problem(*shape)
+    few = problem(*shape[:3], 1, *shape[4:])
+    assert pisa.pisa_qcache_attn_workspace_bytes(p) > B * H * Nq * K * d * 2 > pisa.pisa_qcache_attn_workspace_bytes(few)
+    k, v = normal((B, Hkv, N, d), 1, dtype, 0.5), normal((B, Hkv, N, d), 2, dtype, 0.5)
+    q = normal((B, H, Nq, d), 3, dtype)
+    cache = pisa.make_qcache(p)
+    pisa.qcache_append(p, cache, k, v, 0)
+    idx = quick_selection(p, 4)
+    o, lse = torch.full_like(q, 7.0), torch.full((B, H, Nq), 7.0, device="cuda")
+    nb = pisa.pisa_qcache_attn_workspace_bytes(p)
+    band = torch.full((nb + 8192,), 0xA5, dtype=torch.uint8, device="cuda")
+    pisa.pisa_qcache_attn_fwd(p, cache, q, idx, o, lse, band[4096:], nb)
+    check_grouped(p, cache, q, idx, o, lse, sample(p, 5))
+    assert bool((band[:4096] == 0xA5).all()) and bool((band[-4096:] == 0xA5).all())
+    assert torch.isfinite(o).all()
+    o2 = torch.empty_like(o)
+    pisa.pisa_qcache_attn_fwd(p, cache, q, idx, o2, None, band[4096:], nb)
+    assert torch.equal(o2, o)
+
+
+@pytest.mark.parametrize("C", [64, 128])
+def test_many_rows_hidden_tokens(C):
+    """Values that are NaN or infinite, and keys: rows before them are as without them, rows after them NaN where they
+    attend them."""
+    B, H, Hkv, Nq, N, d, K = 1, 2, 1, 4000, 4000, 128, 16
+    p = problem(B, H, Hkv, Nq, N, d, C, 2, K, 1, "bf16")
+    k, v, q = normal((B, Hkv, N, d), 1, "bf16"), normal((B, Hkv, N, d), 2, "bf16"), normal((B, H, Nq, d), 3, "bf16")
+    idx = quick_selection(p, 4)
+    rows = torch.arange(N, device="cuda")
+    idx[..., 0] = (rows // C).int()  # every row its own block
+    idx[..., 1:] = torch.where(idx[..., 1:] == idx[..., :1], -1, idx[..., 1:])
+    clean, dirty = pisa.make_qcache(p), pisa.make_qcache(p)
+    pisa.qcache_append(p, clean, k, v, 0)
+    want = pisa.qcache_attn_fwd(p, clean, q, idx)
+    at = [130, 131, 1000, 3999]
+    pisa.qcache_append(p, dirty, k, v, 0)
+    dirty.v[0, 0, at[0] // C, 5, at[0] % C] = 0x7F
+    dirty.v[0, 0, at[1] // C, 77, at[1] % C] = 0xFF
+    dirty.k[0, 0, at[2] // C, at[2] % C, 9] = 0x7F
+    dirty.v[0, 0, at[3] // C, :, at[3] % C] = 0x7F
+    o, lse = pisa.qcache_attn_fwd(p, dirty, q, idx)
+    sees = torch.zeros((Nq, len(at)), dtype=torch.bool, device="cuda")
+    for i, x in enumerate(at):
+        sees[:, i] = (idx[0, 0] == x // C).any(-1) & (rows >= x)
+    free = ~sees.any(-1)
+    assert torch.equal(o[:, :, free], want[0][:, :, free]) and torch.equal(lse[:, :, free], want[1][:, :, free])
+    nan = torch.isnan(o[0])
+    assert bool(nan[:, sees[:, 0], 5].all()) and bool(nan[:, sees[:, 1], 77].all())
+    assert bool(nan[:, sees[:, 2]].all()) and bool(nan[:, sees[:, 3]].all()) and bool(torch.isnan(lse[0][:, sees[:, 2]]).all())
+    only = sees[:, 0] & ~sees[:, 1] & ~sees[:, 2] & ~sees[:, 3]
+    assert int(nan[:, only].sum()) == 2 * int(only.sum())  # one dimension of each head
+
+
+def test_many_rows_in_passes():
+    """Partials past the bound of one pass."""
+    p = problem(1, 32, 8, 9000, 9000, 128, 64, 2, 16, 1, "bf16")
+    k, v = normal((1, 8, 9000, 128), 1, "bf16"), normal((1, 8, 9000, 128), 2, "bf16")
+    q = torch.randn((1, 32, 9000, 128), device="cuda").bfloat16()
+    cache = pisa.make_qcache(p)
+    pisa.qcache_append(p, cache, k, v, 0)
+    idx = quick_selection(p, 4)
+    assert pisa.pisa_qcache_attn_workspace_bytes(p) < 9000 * 8 * 16 * 4 * 260
+    o, lse = pisa.qcache_attn_fwd(p, cache, q, idx)
+    check_grouped(p, cache, q, idx, o, lse, [5, 8063, 8064, 8065, 8066, 8067, 8999])
+
+
+def test_rows_past_one_launch():
+    """4.2 million rows, a wavefront each: two launches."""
+    B, Hkv, Nq, N, d, C = 64, 64, 1026, 1026, 64, 32
+    p = problem(B, Hkv, Hkv, Nq, N, d, C, 2, 1, 0, "f32")
+    assert pisa.pisa_qcache_attn_workspace_bytes(p) == 0
+    cache = pisa.make_qcache(p)
+    k = torch.randn((B, Hkv, N, d), device="cuda", dtype=torch.float32)
+    pisa.qcache_append(p, cache, k, k, 0)
+    idx = torch.randint(0, 33, (B, Hkv, Nq, 1), dtype=torch.int32, device="cuda")
+    o = torch.full((B, Hkv, Nq, d), 7.0, dtype=torch.float32, device="cuda")
+    lse = torch.full((B, Hkv, Nq), 7.0, device="cuda")
+    pisa.pisa_qcache_attn_fwd(p, cache, k, idx, o, lse)
+    assert bool((o != 7).any(-1).all()) and bool((lse != 7).all())
+    part = problem(1, 2, 2, Nq, N, d, C, 2, 1, 0, "f32")
+    for b, h in ((0, 0), (63, 62)):
+        cut = lambda x: x[b:b + 1, h:h + 2].contiguous()  # noqa: E731
+        small = pisa.QCache(*(cut(x) for x in (cache.k, cache.v, cache.k_scale, cache.v_scale)))
+        check_attention(part, small, cut(k), cut(idx), cut(o), cut(lse), [0, 1, 1023, 1024, 1025])
 
 
 @pytest.mark.parametrize("Nq", [1, 33])
