@@ -353,14 +353,15 @@ hipError_t launch_build_pyramid(const Geo& geo, int BH, int D, bool bf16, const 
 
 // The runs' coarser levels alone, from level-1 means that are in memory: a
 // workgroup per run of lpb leaf blocks, the first one `run0`.
-__global__ __launch_bounds__(256) void pool_runs_kernel(float* __restrict__ pyr, Geo geo, int s_levels, int lpb, int run0,
-                                                        int D) {
+template <int D>
+__global__ __launch_bounds__(256) void pool_runs_kernel(float* __restrict__ pyr, Geo geo, int s_levels, int lpb, int run0) {
   extern __shared__ __align__(16) float lds[];  // two buffers of lpb * D floats
   const int bh = blockIdx.y;
   const int leaf0 = (run0 + static_cast<int>(blockIdx.x)) * lpb;
   const int nleaf = min(lpb, geo.M[1] - leaf0);
   float* pb = pyr + static_cast<int64_t>(bh) * geo.R * D;
-  for (int e = threadIdx.x; e < nleaf * D; e += blockDim.x) lds[e] = pb[(geo.off[1] + leaf0) * D + e];
+  const float4* src = reinterpret_cast<const float4*>(pb + (geo.off[1] + leaf0) * D);
+  for (int e = threadIdx.x; e < nleaf * (D / 4); e += 256) reinterpret_cast<float4*>(lds)[e] = src[e];
   __syncthreads();
   pool_run_levels(pb, geo, s_levels, lpb, leaf0, D, lds, lds + lpb * D);
 }
@@ -381,7 +382,11 @@ hipError_t launch_pyramid_levels(const Geo& geo, int BH, int D, float* pyr, int 
     const int run0 = n_old > 0 ? (n_old - 1) / geo.C / lpb : 0;
     const dim3 grid((geo.M[1] + lpb - 1) / lpb - run0, BH);
     ProfScope ps("pool_runs", st);
-    pool_runs_kernel<<<grid, 256, 2 * static_cast<size_t>(lpb) * D * sizeof(float), st>>>(pyr, geo, s, lpb, run0, D);
+    const size_t lds = 2 * static_cast<size_t>(lpb) * D * sizeof(float);
+    if (D == 128)
+      pool_runs_kernel<128><<<grid, 256, lds, st>>>(pyr, geo, s, lpb, run0);
+    else
+      pool_runs_kernel<64><<<grid, 256, lds, st>>>(pyr, geo, s, lpb, run0);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

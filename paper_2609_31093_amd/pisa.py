@@ -162,6 +162,10 @@ def _ptr(x):
     return x.data_ptr()
 
 
+def _at(x):
+    return None if x is None else ctypes.addressof(x)
+
+
 # the current stream's handle without the Stream object that torch.cuda.current_stream() builds (0.1 us against 2.7)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
@@ -286,21 +290,20 @@ def pisa_rope_frequencies(r: Rope, base: float, scaling: int, factor: float, ctx
                   "pisa_rope_frequencies")
 
 
-def _rope_call(name, r, q, qs, k, ks, positions, qo, qos, ko, kos, stream):
-    st = [None if x is None else ctypes.addressof(x) for x in (qs, ks, qos, kos)]
-    return _check(getattr(_lib, name)(ctypes.byref(r), _ptr(q), st[0], _ptr(k), st[1], _ptr(positions), _ptr(qo), st[2],
-                                      _ptr(ko), st[3], _stream(stream)), name)
+def _rope_call(fn, name, r, q, qs, k, ks, positions, qo, qos, ko, kos, stream):
+    return _check(fn(ctypes.byref(r), _ptr(q), _at(qs), _ptr(k), _at(ks), _ptr(positions), _ptr(qo), _at(qos), _ptr(ko),
+                     _at(kos), _stream(stream)), name)
 
 
 def pisa_rope_fwd(r: Rope, q, q_strides, k, k_strides, positions, q_out, q_out_strides, k_out, k_out_strides,
                   stream=None) -> int:
-    return _rope_call("pisa_rope_fwd", r, q, q_strides, k, k_strides, positions, q_out, q_out_strides, k_out,
+    return _rope_call(_lib.pisa_rope_fwd, "pisa_rope_fwd", r, q, q_strides, k, k_strides, positions, q_out, q_out_strides, k_out,
                       k_out_strides, stream)
 
 
 def pisa_rope_bwd(r: Rope, d_q_out, d_q_out_strides, d_k_out, d_k_out_strides, positions, d_q, d_q_strides, d_k,
                   d_k_strides, stream=None) -> int:
-    return _rope_call("pisa_rope_bwd", r, d_q_out, d_q_out_strides, d_k_out, d_k_out_strides, positions, d_q, d_q_strides,
+    return _rope_call(_lib.pisa_rope_bwd, "pisa_rope_bwd", r, d_q_out, d_q_out_strides, d_k_out, d_k_out_strides, positions, d_q, d_q_strides,
                       d_k, d_k_strides, stream)
 
 
@@ -315,9 +318,8 @@ def pisa_qcache_bytes(p: Problem) -> int:
 
 def pisa_qcache_append(p: Problem, cache, k_new, k_strides, v_new, v_strides, n_old: int, pyramid=None,
                        stream=None) -> int:
-    st = [None if x is None else ctypes.addressof(x) for x in (k_strides, v_strides)]
-    return _check(_lib.pisa_qcache_append(ctypes.byref(p), cache.address, _ptr(k_new), st[0], _ptr(v_new), st[1], n_old,
-                                          _ptr(pyramid), _stream(stream)), "pisa_qcache_append")
+    return _check(_lib.pisa_qcache_append(ctypes.byref(p), cache.address, _ptr(k_new), _at(k_strides), _ptr(v_new),
+                                          _at(v_strides), n_old, _ptr(pyramid), _stream(stream)), "pisa_qcache_append")
 
 
 def pisa_qcache_attn_workspace_bytes(p: Problem) -> int:
@@ -476,31 +478,28 @@ def make_rope(B, H, Hkv, N, d, rot=None, layout="half", dtype="bf16", base=10000
     return r
 
 
+def _side(x, y, name, dtype, shape, device):
+    """(x, its strides, output, its strides) of one side of a rotation, the output allocated where y is None."""
+    if x is None:
+        if y is not None:
+            raise ValueError(f"{name}_out without {name}")
+        return None, None, None, None
+    xs = _strided(x, name, dtype, shape, device)
+    if y is None:
+        return x, xs, torch.empty(shape, dtype=dtype, device=x.device), None
+    return x, xs, y, _strided(y, name + "_out", dtype, shape, device)
+
+
 def _rope(turn, r: Rope, q, k, positions, q_out, k_out, stream):
-    dt, dev = _TORCH[r.dtype], torch.cuda.current_device()
+    dt, dev, B, N, d = _TORCH[r.dtype], torch.cuda.current_device(), r.B, r.N, r.d
     if positions is not None:
-        if positions.shape == (r.N,):
-            _take(positions, "positions", torch.int32, (r.N,), dev)
-            r.pos_bstride = 0
-        else:
-            _take(positions, "positions", torch.int32, (r.B, r.N), dev)
-            r.pos_bstride = r.N
-    args, out = [], []
-    for name, x, y, heads in (("q", q, q_out, r.H), ("k", k, k_out, r.Hkv)):
-        if x is None:
-            if y is not None:
-                raise ValueError(f"{name}_out without {name}")
-            args.append((None, None, None, None))
-        else:
-            shape = (r.B, heads, r.N, r.d)
-            xs = _strided(x, name, dt, shape, dev)
-            if y is None:
-                y = torch.empty(shape, dtype=dt, device=x.device)
-            args.append((x, xs, y, _strided(y, name + "_out", dt, shape, dev)))
-        out.append(y)
-    (q, qs, qo, qos), (k, ks, ko, kos) = args
-    turn(r, q, qs, k, ks, positions, qo, qos, ko, kos, stream)
-    return tuple(out)
+        shared = positions.dim() == 1
+        _take(positions, "positions", torch.int32, (N,) if shared else (B, N), dev)
+        r.pos_bstride = 0 if shared else N
+    q, qs, q_out, qos = _side(q, q_out, "q", dt, (B, r.H, N, d), dev)
+    k, ks, k_out, kos = _side(k, k_out, "k", dt, (B, r.Hkv, N, d), dev)
+    turn(r, q, qs, k, ks, positions, q_out, qos, k_out, kos, stream)
+    return q_out, k_out
 
 
 def rope_fwd(r: Rope, q, k=None, positions=None, q_out=None, k_out=None, stream=None):
