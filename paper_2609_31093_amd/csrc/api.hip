@@ -762,6 +762,20 @@ int pisa_qcache_append(const pisa_problem* p, const pisa_qcache* c, const void* 
   pisa_strides ks, vs;
   PISA_TRY(check_strides(k_strides, "k_new", p->B, p->Hkv, p->N - n_old, p->d, p->dtype, false, &ks));
   PISA_TRY(check_strides(v_strides, "v_new", p->B, p->Hkv, p->N - n_old, p->d, p->dtype, false, &vs));
+  // the appended rows are read while the cache is written
+  const size_t esz = s.bf16 ? 2 : 4, codes = pisa_qcache_bytes(p), open = static_cast<size_t>(s.BH()) * s.C * s.D * esz;
+  auto span = [&](const pisa_strides& x) {  // bytes from a tensor's first value to its last
+    return ((p->B - 1) * x.b + (p->Hkv - 1) * x.h + (p->N - n_old - 1) * x.n + p->d) * static_cast<int64_t>(esz);
+  };
+  const struct { const void* ptr; size_t bytes; const char* name; } fresh[] = {{k_new, static_cast<size_t>(span(ks)), "k_new"},
+                                                                                {v_new, static_cast<size_t>(span(vs)), "v_new"}},
+      held[] = {{c->k, codes, ""}, {c->v, codes, ""}, {c->k_open, open, ""}, {c->v_open, open, ""}};
+  for (const auto& x : fresh) {
+    for (const auto& y : held) {
+      const uintptr_t u = reinterpret_cast<uintptr_t>(x.ptr), w = reinterpret_cast<uintptr_t>(y.ptr);
+      if (u < w + y.bytes && w < u + x.bytes) return fail(PISA_ERR_INVALID_ARG, "%s overlaps the cache", x.name);
+    }
+  }
   a.k_new = k_new;
   a.v_new = v_new;
   a.ksb = ks.b;

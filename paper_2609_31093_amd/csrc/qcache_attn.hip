@@ -781,6 +781,7 @@ static size_t al256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 // over 524288 keys, 4 heads: 8192 237 and 299, 16384 455 and 419.
 static bool use_blocks(const Shape& s, const Geo& geo) {
   if (!s.bf16 || geo.M[1] > 16384) return false;  // the grouping's LDS histogram
+  if (static_cast<int64_t>(s.BH()) * geo.M[1] > (1 << 23)) return false;  // a workgroup per block fits one launch
   const double rows = static_cast<double>(s.BH()) * s.Nq;
   const double saved = rows * s.K * s.D / 1024 * (0.2 * s.C - 1.32 * s.G * std::max(1.0, s.C / 64.0));
   return saved >= 45000 + 4.5 * s.BH() * geo.M[1];

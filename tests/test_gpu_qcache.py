@@ -182,6 +182,11 @@ def test_strided_rows_and_untouched_neighbours():
     for got, ref in ((cache.k, want.k), (cache.v, want.v), (cache.k_scale, want.k_scale), (cache.v_scale, want.v_scale)):
         assert torch.equal(got[:, :, :used], ref[:, :, :used])
         assert bool((got[:, :, used:].contiguous().view(torch.uint8) == 0xA5).all())
+    # one row for every token and head
+    one, same = normal((1, 1, 1, d), 5, "bf16").expand(B, Hkv, N, d), (pisa.make_qcache(p), pisa.make_qcache(p))
+    pisa.qcache_append(p, same[0], one, one, 0)
+    pisa.qcache_append(p, same[1], one.contiguous(), one.contiguous(), 0)
+    assert torch.equal(same[0].k, same[1].k) and torch.equal(same[0].v, same[1].v) and torch.equal(same[0].v_open, same[1].v_open)
     before = cache.k[:, :, :4].clone()
     pisa.qcache_append(p, cache, k[:, :, 140:], v[:, :, 140:], 140)
     assert torch.equal(cache.k[:, :, :4], before) and torch.equal(cache.k[:, :, 4], want.k[:, :, 4])
@@ -279,6 +284,8 @@ SHAPES = [
     (1, 4, 4, 40, 1500, 64, 64, 2, 16, 1, "bf16", 0),
     (1, 2, 2, 128, 900, 64, 32, 2, 12, 1, "f32", 0),
     (1, 3, 3, 300, 600, 64, 32, 2, 7, 1, "bf16", 0),
+    (1, 7, 1, 5, 1234, 128, 192, 2, 6, 1, "bf16", 1500),
+    (1, 2, 2, 33, 800, 64, 224, 2, 3, 1, "f32", 0),
 ]
 
 
@@ -532,6 +539,37 @@ def test_guards_and_streams():
         assert bool((x[:4096] == 0xA5).all()) and bool((x[-4096:] == 0xA5).all())
 
 
+def test_offsets_past_32_bits():
+    """A cache of 4.3 GB of keys: rows that attend its last blocks, and an append to its last one."""
+    Hkv, d, C, M, K, Nq = 8, 128, 64, 65535, 8, 3
+    N = M * C
+    p = problem(1, 16, Hkv, Nq, N, d, C, 2, K, 0, "bf16")
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(1)
+    codes = lambda shape: torch.randint(0, 0x70, shape, generator=gen, device="cuda", dtype=torch.uint8)  # noqa: E731
+    scale = lambda: 2.0 ** torch.randint(-6, -3, (1, Hkv, M), generator=gen, device="cuda").float()  # noqa: E731
+    raw = normal((1, Hkv, C, d), 2, "bf16")
+    big = pisa.QCache(codes((1, Hkv, M, C, d)), codes((1, Hkv, M, d, C)), scale(), scale(), raw.clone(), raw.clone())
+    q = normal((1, 16, Nq, d), 3, "bf16")
+    blocks = torch.stack([torch.tensor([M - 1 - j * 7 - h for j in range(K)], device="cuda") for h in range(Hkv)])
+    idx = blocks[None, :, None].expand(1, Hkv, Nq, K).int().contiguous()
+    o, lse = pisa.qcache_attn_fwd(p, big, q, idx)
+    small_p = problem(1, 16, Hkv, Nq, K * C, d, C, 2, K, 0, "bf16")
+    h = torch.arange(Hkv, device="cuda")[:, None]
+    small = pisa.QCache(*(x[0][h, blocks][None].contiguous() for x in (big.k, big.v, big.k_scale, big.v_scale)))
+    order = torch.arange(K, dtype=torch.int32, device="cuda").expand(1, Hkv, Nq, K).contiguous()
+    want = pisa.qcache_attn_fwd(small_p, small, q, order)
+    assert torch.equal(o, want[0]) and torch.equal(lse, want[1])
+    check_attention(small_p, small, q, order, o, lse)
+    new = normal((1, Hkv, 3, d), 4, "bf16")
+    before = big.k[:, :, :M - 1].sum(dtype=torch.int64)
+    pisa.qcache_append(p, big, new, new, N - 3)
+    rows = torch.cat((raw[:, :, :C - 3], new), 2)
+    last = pisa.QCache(*(x[:, :, M - 1:].contiguous() for x in (big.k, big.v, big.k_scale, big.v_scale)), big.k_open, big.v_open)
+    check_cache(problem(1, Hkv, Hkv, 1, C, d, C, 2, 4, 1, "bf16"), last, rows, rows)
+    assert big.k[:, :, :M - 1].sum(dtype=torch.int64) == before
+
+
 # ------------------------------------------------------- together, as used ---
 
 def test_a_sequence_from_prompt_to_tokens():
@@ -611,6 +649,45 @@ def test_graph_replays_match_eager():
         for got, want in zip((o, lse, cache.k, cache.v, cache.k_scale, pyr), eager[i]):
             assert torch.equal(torch.nan_to_num(got.float(), 7.0), torch.nan_to_num(want.float(), 7.0)), i
         (torch.randn(1000, device="cuda") @ torch.randn(1000, device="cuda")).item()
+
+
+def test_two_graphs_share_a_workspace():
+    """Many rows and few rows of one cache, captured on their own with one workspace, replayed in turn with eager work
+    between."""
+    H, Hkv, N, d, C, K = 8, 4, 3000, 128, 64, 16
+    k, v = normal((1, Hkv, N, d), 1, "bf16"), normal((1, Hkv, N, d), 2, "bf16")
+    runs = []
+    for Nq in (3000, 2):
+        p = problem(1, H, Hkv, Nq, N, d, C, 2, K, 1, "bf16")
+        runs.append([p, normal((1, H, Nq, d), 3, "bf16"), quick_selection(p, Nq), torch.empty((1, H, Nq, d), dtype=torch.bfloat16, device="cuda"),
+                     torch.empty((1, H, Nq), device="cuda")])
+    cache = pisa.make_qcache(runs[0][0])
+    pisa.qcache_append(runs[0][0], cache, k, v, 0)
+    need = [pisa.pisa_qcache_attn_workspace_bytes(x[0]) for x in runs]
+    assert min(need) > 0
+    ws = torch.empty(max(need), dtype=torch.uint8, device="cuda")
+    call = lambda x: pisa.pisa_qcache_attn_fwd(x[0], cache, *x[1:], ws, ws.numel())  # noqa: E731
+    graphs = []
+    for x in runs:
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            call(x)
+        torch.cuda.current_stream().wait_stream(side)
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            call(x)
+    for i, n in enumerate((0, 1, 1, 0, 1, 0)):
+        x = runs[n]
+        x[1].copy_(normal(x[1].shape, 30 + i, "bf16"))
+        call(x)
+        torch.cuda.synchronize()
+        want = [t.clone() for t in x[3:]]
+        x[3].fill_(7)
+        x[4].fill_(7)
+        graphs[n].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(x[3], want[0]) and torch.equal(x[4], want[1]), i
 
 
 def test_wrapper_refusals():

@@ -159,6 +159,20 @@ def test_many_heads_and_rows_past_one_workgroup():
     check(yk, k, pos, r, "interleaved", 1, "bf16")
 
 
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_offsets_past_32_bits(layout):
+    """2.5e9 values: heads and rows at the far end as on their own."""
+    H, N, d = 64, 300001, 128
+    q = torch.randn((1, H, N, d), device="cuda", dtype=torch.bfloat16)
+    r = pisa.make_rope(1, H, 1, N, d, layout=layout)
+    pisa.rope_fwd(r, q, q_out=(out := torch.empty_like(q)))
+    for h in (0, 33, 63):
+        one = pisa.make_rope(1, 1, 1, 500, d, layout=layout, pos0=N - 500)
+        want, _ = pisa.rope_fwd(one, q[:, h:h + 1, N - 500:])
+        assert torch.equal(out[:, h:h + 1, N - 500:], want)
+    check(out[:, 63:, -3:], q[:, 63:, -3:], np.arange(N - 3, N)[None], r, layout, 1, "bf16")
+
+
 def test_wrapper_refusals():
     r = pisa.make_rope(1, 2, 1, 8, 64, dtype="bf16")
     q = torch.zeros((1, 2, 8, 64), dtype=torch.bfloat16, device="cuda")

@@ -117,8 +117,11 @@ def problem(**kw):
     return pisa.make_problem(**{**base, **kw})
 
 
+CACHE = 1 << 30  # where the cache's buffers are said to be
+
+
 def buffers(**kw):
-    return pisa.QCacheBuffers(*[kw.get(n, FAKE) for n, _ in pisa.QCacheBuffers._fields_])
+    return pisa.QCacheBuffers(*[kw.get(n, CACHE + (i << 24)) for i, (n, _) in enumerate(pisa.QCacheBuffers._fields_)])
 
 
 def test_cache_sizes():
@@ -160,6 +163,14 @@ def test_append_refusals():
     assert call(v=FAKE + 2) == INVALID and "v_new" in pisa.pisa_last_error()
     assert call(pyr=FAKE + 4) == INVALID and "pyramid" in pisa.pisa_last_error()
     assert call(vs=pisa.Strides(0, 0, 4)) == INVALID and "v_new" in pisa.pisa_last_error()
+    row = 128 * 2
+    for i, size in ((0, 2 * 1024 * 128), (1, 2 * 1024 * 128), (4, 2 * 64 * row), (5, 2 * 64 * row)):
+        at = CACHE + (i << 24)
+        for x in (at, at + size - row, at - 2 * 1024 * row + row):  # the same place, from the end on, up to the start
+            assert call(k=x) == INVALID and "k_new overlaps" in pisa.pisa_last_error()
+            assert call(v=x) == INVALID and "v_new overlaps" in pisa.pisa_last_error()
+    # one row per head that is read as many: its span ends with it
+    assert call(k=CACHE + 15 * row, ks=pisa.Strides(0, 0, 0)) == INVALID
     assert call(n_old=1024) == pisa.PISA_OK  # nothing to append, nothing launched
 
 
@@ -190,3 +201,11 @@ def test_workspaces_are_asked_for_before_a_launch():
             assert st == pisa.PISA_ERR_WORKSPACE
             st = LIB.pisa_qcache_attn_fwd(ctypes.byref(p), ctypes.byref(c), FAKE, FAKE, FAKE, None, FAKE + 16, need, None)
             assert st == INVALID
+
+
+def test_rows_are_grouped_by_block_only_where_a_launch_holds_the_blocks():
+    many = dict(H=1, Hkv=1, Nq=2000, N=32768, C=32, K=16)
+    assert pisa.pisa_qcache_attn_workspace_bytes(problem(B=4096, **many)) > 0
+    assert pisa.pisa_qcache_attn_workspace_bytes(problem(B=16384, **many)) == 0     # 2^24 blocks
+    assert pisa.pisa_qcache_attn_workspace_bytes(problem(B=8, **{**many, "N": 32 * 16385, "Nq": 60000})) == 0
+    assert pisa.pisa_qcache_attn_workspace_bytes(problem(B=8, dtype="f32", **many)) == 0
