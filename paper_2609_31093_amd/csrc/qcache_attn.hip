@@ -488,8 +488,7 @@ __global__ __launch_bounds__(64) void qcache_merge_kernel(QAttnArgs a) {
 // 2^-11; its log sum stays in fp32), and qcache_combine_kernel merges a row's K.
 //   part_o [BH][rows][K][G][D], within each 32 dimensions in the order
 //   [grp][dimension tile 0..1][4], so that a lane stores 16 bytes at a time
-constexpr int kBlockWaves = 4;
-constexpr int kBlockTiles = 4;  // tiles of a wavefront
+constexpr int kBlockTiles = 8;  // tiles of a wavefront, at most
 
 struct QBlockArgs {
   QAttnArgs a;
@@ -502,12 +501,12 @@ struct QBlockArgs {
 };
 
 // WHOLE: a unit is a block, whose codes stay in registers (152 of them, three
-// wavefronts on a SIMD; with the operands there instead, 256 and two, the same
-// 4096 rows of 16 heads took 157 us in this kernel against 126); otherwise its
-// units are read again, from the cache, for every tile.  What bounds it is the
-// partials' 268 MB out and the queries' 268 MB in.
+// wavefronts on a SIMD; with the operands there instead, 256 and two, 4096 rows of
+// 16 heads on 4 took 157 us in this kernel against 126); otherwise its units are
+// read again, from the cache, for every tile.  What bounds it there (119 us) is the
+// partials' 268 MB out and the queries' 268 MB in, 4.5 TB/s.
 template <int D, int KU, bool WHOLE>
-__global__ __launch_bounds__(kBlockWaves * 64, WHOLE ? (D == 128 ? 3 : 4) : 2) void qcache_block_kernel(QBlockArgs p) {
+__global__ __launch_bounds__(64, WHOLE ? (D == 128 ? 3 : 4) : 2) void qcache_block_kernel(QBlockArgs p) {
   constexpr int KS = D / 32, DT = D / 16;
   const QAttnArgs& a = p.a;
   int64_t cl;
@@ -515,8 +514,7 @@ __global__ __launch_bounds__(kBlockWaves * 64, WHOLE ? (D == 128 ? 3 : 4) : 2) v
   if (!cluster_chunk(p.offs, p.toffs, p.ncl, blockIdx.x, p.chunk, cl, beg, end)) return;
   const int bh = static_cast<int>(cl / a.M1), blk = static_cast<int>(cl - static_cast<int64_t>(bh) * a.M1);
   const int b = bh / a.Hkv, h = bh - b * a.Hkv;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int col = lane & 15, grp = lane >> 4;
+  const int col = threadIdx.x & 15, grp = threadIdx.x >> 4;
   const int ppt = 16 / a.G;                // pairs of a tile
   const int cp = col / a.G, hh = col - cp * a.G;  // this column's pair and head
   const bool head = cp < ppt;
@@ -524,15 +522,13 @@ __global__ __launch_bounds__(kBlockWaves * 64, WHOLE ? (D == 128 ? 3 : 4) : 2) v
   const int64_t cell = static_cast<int64_t>(bh) * a.c.M + blk;
   const int tok0 = blk * a.C;
 
-  // this wavefront's tiles: wave, wave + 4, ...; their pairs are read up front and
-  // the next tile's queries while one is computed
+  // the tiles' pairs are read up front, and the next tile's queries while one is
+  // computed
   const int ntile = (end - beg + ppt - 1) / ppt;
-  const int mine = (ntile - wave + kBlockWaves - 1) / kBlockWaves;
-  if (mine <= 0) return;
   int words[kBlockTiles];
 #pragma unroll
   for (int j = 0; j < kBlockTiles; ++j) {
-    const int at = beg + (wave + j * kBlockWaves) * ppt + cp;
+    const int at = beg + j * ppt + cp;
     words[j] = head && at < end ? p.pairs[at] : -1;
   }
   Unit<D, KU> whole;
@@ -552,7 +548,7 @@ __global__ __launch_bounds__(kBlockWaves * 64, WHOLE ? (D == 128 ? 3 : 4) : 2) v
     whole.clear_from(a.N - tok0, grp);
   }
 #pragma unroll 1
-  for (int j = 0; j < mine; ++j) {
+  for (int j = 0; j < ntile; ++j) {
     bf16x8a qt[KS][1];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qt[ks][0] = u4_as_bf16x8(qn[ks]);
@@ -563,7 +559,7 @@ __global__ __launch_bounds__(kBlockWaves * 64, WHOLE ? (D == 128 ? 3 : 4) : 2) v
     const int visible = live ? (a.causal ? min(a.N, t + 1) : a.N) - tok0 : a.C;  // keys of the block
 #pragma unroll
     for (int i = 0; i + 1 < kBlockTiles; ++i) words[i] = words[i + 1];
-    if (j + 1 < mine) gather(words[0]);
+    if (j + 1 < ntile) gather(words[0]);
     uint16_t* dst = nullptr;
     const int64_t pidx = ((static_cast<int64_t>(bh) * p.nrows + rr) * a.K + slot) * a.G + hh;
     if (live) dst = p.part_o + pidx * D + grp * 8;
@@ -796,8 +792,10 @@ static int block_rows(const Shape& s) {
 // Rows per workgroup of the grouping: about 4096 pairs (262144 pairs on 4 KV heads:
 // 28 us, 47 with 1024 rows).
 static int group_rows(const Shape& s) { return std::max(64, 4096 / s.K); }
-// Pairs of one block per workgroup: four tiles for each wavefront.
-static int pair_chunk(const Shape& s) { return 16 / s.G * kBlockWaves * kBlockTiles; }
+// Pairs of one block per wavefront.  Workgroups of one (4096 rows of 8 heads on 8,
+// 16 blocks of 131072 keys: 103 us in this kernel; 4 wavefronts of 4 tiles 150, 2 of
+// 8 113, one of 16 106).
+static int pair_chunk(const Shape& s) { return 16 / s.G * kBlockTiles; }
 struct BlockWs {
   size_t part_o, part_lse, cl, total;
 };
@@ -837,13 +835,13 @@ static hipError_t launch_blocks(const Shape& s, const Geo& geo, const QAttnArgs&
       const unsigned grid = static_cast<unsigned>(
           cluster_max_chunks(s.BH(), geo.M[1], static_cast<int64_t>(s.BH()) * p.nrows * s.K, p.chunk));
       if (s.C == 64)
-        qcache_block_kernel<D, 64, true><<<grid, kBlockWaves * 64, 0, st>>>(p);
+        qcache_block_kernel<D, 64, true><<<grid, 64, 0, st>>>(p);
       else if (s.C == 32)
-        qcache_block_kernel<D, 32, true><<<grid, kBlockWaves * 64, 0, st>>>(p);
+        qcache_block_kernel<D, 32, true><<<grid, 64, 0, st>>>(p);
       else if (ku == 64)
-        qcache_block_kernel<D, 64, false><<<grid, kBlockWaves * 64, 0, st>>>(p);
+        qcache_block_kernel<D, 64, false><<<grid, 64, 0, st>>>(p);
       else
-        qcache_block_kernel<D, 32, false><<<grid, kBlockWaves * 64, 0, st>>>(p);
+        qcache_block_kernel<D, 32, false><<<grid, 64, 0, st>>>(p);
     }
     {
       ProfScope ps("qcache_combine", st);

@@ -10,6 +10,7 @@ if the library has not been built (there is no fallback path).
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -457,6 +458,11 @@ def _take(x, name, dtype, shape, device):
     return x
 
 
+@functools.lru_cache(maxsize=256)
+def _strides(b, h, n):
+    return Strides(b, h, n)
+
+
 def _strided(x, name, dtype, shape, device):
     """The pisa_strides of a [B, heads, rows, d] tensor (None where it is contiguous)."""
     if x.dtype != dtype or x.shape != shape or x.get_device() != device:
@@ -467,7 +473,7 @@ def _strided(x, name, dtype, shape, device):
     if one != 1:
         raise ValueError(f"{name}: its last dimension must be contiguous (strides {x.stride()})")
     # the stride of a dimension of one entry is never used
-    return Strides(b if shape[0] > 1 else 0, h if shape[1] > 1 else 0, n if shape[2] > 1 else 0)
+    return _strides(b if shape[0] > 1 else 0, h if shape[1] > 1 else 0, n if shape[2] > 1 else 0)
 
 
 def make_rope(B, H, Hkv, N, d, rot=None, layout="half", dtype="bf16", base=10000.0, scaling="none", factor=1.0, ctx=4096,
