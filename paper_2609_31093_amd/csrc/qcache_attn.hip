@@ -769,18 +769,19 @@ static size_t al256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 // Does grouping the rows by block pay?  A row alone reads its K blocks, of 2 C D
 // bytes, at about 10 TB/s over all; grouped, a block is read once for many rows,
 // but each (row, slot) writes and reads back a partial of 2 D bytes a head (0.33
-// ns per KB and 64 keys of the block), and the grouping costs 45 us and 4.5 ns per
+// ns per KB and 64 keys of the block), and the grouping costs 32 us and 2.5 ns per
 // block of every KV head.  Measured, alone and grouped (us): 128-wide heads, 16
 // blocks of 64 keys, 32768 keys, 4 heads to a KV head: 2048 rows x KV heads 63 and
-// 69, 4096 112 and 84, 16384 369 and 223; 1 head: 2048 60 and 56, 16384 372 and
-// 94; 8 heads: 8192 213 and 210; 16 heads of 64, 8 blocks: 8192 65 and 140;
-// over 524288 keys, 4 heads: 8192 237 and 299, 16384 455 and 419.
+// 61, 4096 112 and 75, 16384 374 and 226; 1 head: 2048 60 and 52, 16384 367 and
+// 84; 8 heads: 8192 204 and 212; 16 heads of 64, 8 blocks: 8192 64 and 140; over
+// 524288 keys, 4 heads: 16384 457 and 328.  Over 135 shapes of 512 to 16384 rows
+// the mean time is 0.5% above that of the faster choice for each.
 static bool use_blocks(const Shape& s, const Geo& geo) {
   if (!s.bf16 || geo.M[1] > 16384) return false;  // the grouping's LDS histogram
   if (static_cast<int64_t>(s.BH()) * geo.M[1] > (1 << 23)) return false;  // a workgroup per block fits one launch
   const double rows = static_cast<double>(s.BH()) * s.Nq;
   const double saved = rows * s.K * s.D / 1024 * (0.2 * s.C - 1.32 * s.G * std::max(1.0, s.C / 64.0));
-  return saved >= 45000 + 4.5 * s.BH() * geo.M[1];
+  return saved >= 32000 + 2.5 * s.BH() * geo.M[1];
 }
 
 // Rows per pass: their partials take at most 1 GB.
@@ -790,7 +791,7 @@ static int block_rows(const Shape& s) {
   return static_cast<int>(std::min<size_t>(s.Nq, std::max<size_t>(kPartialBytes / per_row, 1)));
 }
 // Rows per workgroup of the grouping: about 4096 pairs (262144 pairs on 4 KV heads:
-// 28 us, 47 with 1024 rows).
+// 28 us for the grouping, 47 with 1024 rows).
 static int group_rows(const Shape& s) { return std::max(64, 4096 / s.K); }
 // Pairs of one block per wavefront.  Workgroups of one (4096 rows of 8 heads on 8,
 // 16 blocks of 131072 keys: 103 us in this kernel; 4 wavefronts of 4 tiles 150, 2 of
