@@ -421,10 +421,13 @@ int pisa_qcache_append(const pisa_problem* p, const pisa_qcache* c, const void* 
                        const void* v_new, const pisa_strides* v_strides, int32_t n_old, float* pyramid,
                        pisa_stream_t stream);
 
-/* pisa_sparse_attn_fwd over the cache: the same result as over keys and values
- * code * scale, up to fp32 rounding order.  Entries of block_idx as there; a row
- * with no visible token gets o = 0 and lse = -inf; tokens that the causal mask or
- * N hides are not used, whatever their codes.  o and lse (nullable) as there. */
+/* pisa_sparse_attn_fwd over the cache, its keys and values being code * scale.
+ * Sums run in fp32; a bf16 problem's weights are rounded to fp16 before they
+ * meet the values (and with many rows each block's result is, before the blocks
+ * of a row are merged), an fp32 problem's are not.  Entries of block_idx as
+ * there; a row with no visible token gets o = 0 and lse = -inf; tokens that the
+ * causal mask or N hides are not used, whatever their codes.  o and lse
+ * (nullable) as there. */
 size_t pisa_qcache_attn_workspace_bytes(const pisa_problem* p);
 int pisa_qcache_attn_fwd(const pisa_problem* p, const pisa_qcache* c, const void* q, const int32_t* block_idx, void* o,
                          float* lse, void* ws, size_t ws_bytes, pisa_stream_t stream);

@@ -204,9 +204,8 @@ size_t qcache_attn_ws(const Shape& s, const Geo& geo);
 hipError_t launch_qcache_attn(const Shape& s, const Geo& geo, const QCache& c, const void* q, const int32_t* idx, void* o,
                               float* lse, void* ws, hipStream_t st);
 
-// Pyramid levels 2 .. Lstore from level 1 (pool.hip): everything above leaf
-// block `leaf` and the blocks after it, for a pyramid whose other nodes are
-// those of the first n_old tokens.
+// Pyramid levels 2 .. Lstore from level 1, which is up to date (pool.hip); the
+// levels above hold the nodes of the first n_old tokens.
 hipError_t launch_pyramid_levels(const Geo& geo, int BH, int D, float* pyr, int n_old, hipStream_t st);
 
 }  // namespace pisa

@@ -9,9 +9,60 @@
 // the mean of its existing children (the last node of a level may be short).
 #include "common.h"
 #include "kernels.h"
-#include "pool.h"
 
 namespace pisa {
+
+// Mean of leaf block `leaf` (rows [leaf*C, min((leaf+1)*C, N))) computed by
+// one wavefront: 16 lanes cover a key row, the 4 row groups take every 4th
+// row; lanes of row group 0 return the D/16 means of their column slice.
+// Both the full build and the decode-cache update use this, so their leaf
+// means agree bit for bit.
+template <typename T, int D>
+__device__ __forceinline__ void leaf_mean(const T* __restrict__ kb, const Geo& geo, int leaf, int sub, int rg,
+                                          float (&m)[D / 16]) {
+  constexpr int DPL = D / 16;
+  const int64_t row0 = static_cast<int64_t>(leaf) * geo.C;
+  const int nrows = min(geo.C, geo.N - static_cast<int>(row0));
+  float acc[DPL];
+#pragma unroll
+  for (int e = 0; e < DPL; ++e) acc[e] = 0.f;
+  const T* base = kb + row0 * D + sub * DPL;
+  int r = rg;
+  for (; r + 12 < nrows; r += 16) {
+    float x0[DPL], x1[DPL], x2[DPL], x3[DPL];
+    load_row_part<T, DPL>(base + static_cast<int64_t>(r) * D, x0);
+    load_row_part<T, DPL>(base + static_cast<int64_t>(r + 4) * D, x1);
+    load_row_part<T, DPL>(base + static_cast<int64_t>(r + 8) * D, x2);
+    load_row_part<T, DPL>(base + static_cast<int64_t>(r + 12) * D, x3);
+#pragma unroll
+    for (int e = 0; e < DPL; ++e) acc[e] += (x0[e] + x1[e]) + (x2[e] + x3[e]);
+  }
+  for (; r < nrows; r += 4) {
+    float x0[DPL];
+    load_row_part<T, DPL>(base + static_cast<int64_t>(r) * D, x0);
+#pragma unroll
+    for (int e = 0; e < DPL; ++e) acc[e] += x0[e];
+  }
+#pragma unroll
+  for (int e = 0; e < DPL; ++e) {
+    acc[e] += __shfl_xor(acc[e], 16);
+    acc[e] += __shfl_xor(acc[e], 32);
+  }
+  const float inv = 1.0f / static_cast<float>(nrows);
+#pragma unroll
+  for (int e = 0; e < DPL; ++e) m[e] = acc[e] * inv;
+}
+
+// Node `node` of level lv (>= 2): the mean of its existing children, summed
+// in index order; `child(ch, col)` reads column col of child ch.
+template <typename F>
+__device__ __forceinline__ float node_mean(const Geo& geo, int lv, int node, int col, F child) {
+  const int c0 = node * geo.g;
+  const int c1 = min(c0 + geo.g, geo.M[lv - 1]);
+  float s = 0.f;
+  for (int ch = c0; ch < c1; ++ch) s += child(ch, col);
+  return s / static_cast<float>(c1 - c0);
+}
 
 // Coarser levels whose nodes lie inside a run of lpb leaves from leaf0 on, whose
 // means are in `src`.

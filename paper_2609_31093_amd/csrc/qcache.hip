@@ -121,7 +121,7 @@ struct Source {
 
 // Lane (sub, rg) of a wavefront: columns sub * D/16 .. of row(i) of CH rows from
 // `base` on: every fourth row for keys (a store covers whole rows, and the mean
-// is summed in leaf_mean_rows' order), CH/4 consecutive ones for values (their
+// is summed in the order of pool.hip's leaf_mean, to the same bits), CH/4 consecutive ones for values (their
 // codes of one column are consecutive bytes).
 template <bool KEYS, int CH>
 __device__ __forceinline__ int row_at(int base, int rg, int i) {

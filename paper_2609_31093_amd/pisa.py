@@ -565,6 +565,23 @@ def make_qcache(p: Problem, device=None):
     return QCache(k, v, *scales, *raw)
 
 
+def grow_qcache(p: Problem, new_cap: int, cache: QCache, pyramid=None):
+    """Allocate a cache for new_cap tokens and move problem p's into it (on the current stream), its pyramid with
+    pisa_cache_grow.  Returns (problem with Ncap = new_cap, cache, pyramid); pyramid is None when not given."""
+    cache.check(p)
+    pn = Problem(*[getattr(p, n) for n, _ in Problem._fields_])
+    pn.Ncap = new_cap
+    if new_cap < (p.Ncap or p.N):
+        raise ValueError(f"new_cap ({new_cap}) is below the current capacity ({p.Ncap or p.N})")
+    new, M = make_qcache(pn), -(-p.N // p.C)
+    for name in ("k", "v", "k_scale", "v_scale"):
+        getattr(new, name)[:, :, :M].copy_(getattr(cache, name)[:, :, :M])
+    if cache.k_open is not None:
+        new.k_open.copy_(cache.k_open)
+        new.v_open.copy_(cache.v_open)
+    return pn, new, None if pyramid is None else grow_cache(p, new_cap, pyramid)[1]
+
+
 def qcache_append(p: Problem, cache: QCache, k_new, v_new, n_old: int, pyramid=None, stream=None):
     """Append rows n_old .. N-1 (k_new, v_new: [B, Hkv, N - n_old, d], views with a contiguous last dimension) to
     the cache, and bring the pyramid with it where one is given."""

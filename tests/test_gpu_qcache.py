@@ -606,6 +606,26 @@ def test_a_sequence_from_prompt_to_tokens():
     assert torch.equal(torch.nan_to_num(pyr, 7.0), torch.nan_to_num(want, 7.0))
 
 
+def test_a_cache_that_grows():
+    """Appends across a growth: as in buffers that were large enough from the start."""
+    B, Hkv, d, C, g, n, cap = 2, 2, 64, 32, 2, 500, 480
+    k, v = normal((B, Hkv, n, d), 1, "bf16"), normal((B, Hkv, n, d), 2, "bf16")
+    p = problem(B, Hkv, Hkv, 1, 470, d, C, g, 4, 1, "bf16", cap)
+    cache, pyr = pisa.make_qcache(p), new_pyramid(p)
+    pisa.qcache_append(p, cache, k[:, :, :470], v[:, :, :470], 0, pyr)
+    bigger = pisa.pisa_cache_capacity(cap, n, C)
+    p, cache, pyr = pisa.grow_qcache(p, bigger, cache, pyr)
+    p = problem(B, Hkv, Hkv, 1, n, d, C, g, 4, 1, "bf16", bigger)
+    pisa.qcache_append(p, cache, k[:, :, 470:], v[:, :, 470:], 470, pyr)
+    check_cache(p, cache, k, v)
+    want = pisa.make_qcache(p), new_pyramid(p)
+    pisa.qcache_append(p, want[0], k, v, 0, want[1])
+    levels = torch.isfinite(want[1])
+    assert torch.equal(pyr[levels], want[1][levels])
+    with pytest.raises(ValueError):
+        pisa.grow_qcache(p, n - 1, cache)
+
+
 def test_graph_replays_match_eager():
     """One generated token (rotary positions, append, attention) captured and replayed on new inputs, with the program's
     own work between the replays."""
