@@ -399,8 +399,8 @@ typedef struct {
   void* v_open;
 } pisa_qcache;
 
-/* Blocks M per (batch, KV head), and bytes of each code buffer (B*Hkv*M*C*d);
- * a negative status, 0 for an invalid problem. */
+/* Blocks M per (batch, KV head), or a negative status for an invalid problem;
+ * bytes of each code buffer (B*Hkv*M*C*d), or 0 for one. */
 int32_t pisa_qcache_blocks(const pisa_problem* p);
 size_t pisa_qcache_bytes(const pisa_problem* p);
 

@@ -501,7 +501,10 @@ def _rope(turn, r: Rope, q, k, positions, q_out, k_out, stream):
     if positions is not None:
         shared = positions.dim() == 1
         _take(positions, "positions", torch.int32, (N,) if shared else (B, N), dev)
-        r.pos_bstride = 0 if shared else N
+        stride = 0 if shared else N
+        if r.pos_bstride != stride:  # in a copy: the caller's may be in use by another thread's call
+            r = Rope.from_buffer_copy(r)
+            r.pos_bstride = stride
     q, qs, q_out, qos = _side(q, q_out, "q", dt, (B, r.H, N, d), dev)
     k, ks, k_out, kos = _side(k, k_out, "k", dt, (B, r.Hkv, N, d), dev)
     turn(r, q, qs, k, ks, positions, q_out, qos, k_out, kos, stream)

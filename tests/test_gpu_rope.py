@@ -199,3 +199,17 @@ def test_another_stream():
     side.synchronize()
     assert torch.equal(out, want)
     assert math.isfinite(out.float().sum().item())
+
+
+def test_positions_leave_the_descriptor_alone():
+    """One descriptor serves calls with positions per batch, shared ones and none, whichever came before."""
+    B, N = 3, 41
+    r = pisa.make_rope(B, 2, 1, N, 64, dtype="bf16", pos0=5)
+    q, before = normal((B, 2, N, 64), 13, "bf16"), bytes(r)
+    own = np.random.default_rng(14).integers(-1000, 1000, (B, N)).astype(np.int32)
+    counted = np.broadcast_to(5 + np.arange(N, dtype=np.int32), (B, N))
+    for pos in (own, own[0], None, own[1], own):
+        given = None if pos is None else torch.from_numpy(pos).cuda()
+        got, _ = pisa.rope_fwd(r, q, positions=given)
+        assert bytes(r) == before
+        check(got, q, counted if pos is None else np.broadcast_to(pos, (B, N)), r, "half", 1, "bf16")
