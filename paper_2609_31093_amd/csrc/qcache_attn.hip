@@ -19,6 +19,10 @@
 // scale is applied to the product in fp32.  Those weights are taken up to 2^14
 // (kHeadroom), so that ones of 2^-28 of the largest are still normal numbers.
 // Sums of weights are not rounded.
+//
+// The running maximum is that of the products S themselves, and the softmax's
+// scale (with log2 e) multiplies differences from it: a large logit that is
+// rounded with its scale first is off by more than fp16's last two octaves. 
 #include <algorithm>
 
 #include "attn_shared.h"
@@ -35,8 +39,8 @@ struct QAttnArgs {
   const int32_t* idx;
   void* o;
   float* lse;
-  // splits > 1: unnormalised sums [rows][splits][G][D], and maximum and sum
-  // [rows][G][splits]
+  // splits > 1: unnormalised sums [rows][splits][G][D], and the largest logit and
+  // sum of weights [rows][G][splits]
   float* part_o;
   float2* part_ml;
   int H, Hkv, G, Nq, N, C, K, causal, M1;
@@ -239,7 +243,8 @@ __device__ __forceinline__ float column_max(const f32x4a (&s)[MT]) {
   mx = fmaxf(mx, __shfl_xor(mx, 16));
   return fmaxf(mx, __shfl_xor(mx, 32));
 }
-// Logits to weights 2^(s * qscale2 - ref), as operands; returns this lane's sum.
+// Logits to weights 2^((s - ref) * qscale2 + headroom), as operands, for ref the
+// largest of them or larger; returns this lane's sum.
 template <int MT, int NT>
 __device__ __forceinline__ float weights(const f32x4a (&s)[MT], float qscale2, float ref, Weights<NT> (&pt)[MT / 2]) {
   float sum = 0.f;
@@ -248,7 +253,7 @@ __device__ __forceinline__ float weights(const f32x4a (&s)[MT], float qscale2, f
     float p[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      p[i] = fast_exp2(fmaf(s[2 * st + i / 4][i % 4], qscale2, -ref));
+      p[i] = fast_exp2(fmaf(s[2 * st + i / 4][i % 4] - ref, qscale2, kHeadroom<NT>));
       sum += p[i];
     }
     pt[st].set(p);
@@ -289,7 +294,7 @@ template <int D, int KU, int NT>
 struct Softmax {
   using U = Unit<D, KU>;
   f32x4a oacc[U::DT];
-  float m = -INFINITY, l = 0.f;  // what the weights are relative to (log2), their sum
+  float m = -INFINITY, l = 0.f;  // largest logit (before its scale), sum of weights
 
   __device__ __forceinline__ Softmax() {
 #pragma unroll
@@ -301,9 +306,9 @@ struct Softmax {
     if (!MIXED && partial) u.clear_from(nkeys, grp);
     f32x4a s[U::MT];
     unit_logits<D, KU, NT>(u, qt, partial, nkeys, grp, s);
-    const float mn = fmaxf(m, column_max<U::MT>(s) * qscale2 - kHeadroom<NT>);
+    const float mn = fmaxf(m, column_max<U::MT>(s));
     const float ref = mn == -INFINITY ? 0.f : mn;
-    const float corr = fast_exp2(m - ref);
+    const float corr = fast_exp2((m - ref) * qscale2);
     m = mn;
     Weights<NT> pt[U::MT / 2];
     l = l * corr + weights<U::MT, NT>(s, qscale2, ref, pt);
@@ -317,6 +322,12 @@ struct Softmax {
     }
   }
 };
+
+// Natural log of a row's sum of exponentials: largest logit, sum of weights.
+template <int NT>
+__device__ __forceinline__ float row_lse(float ref, float sum, float qscale2) {
+  return sum == 0.f ? -INFINITY : fmaf(ref, qscale2, fast_log2(sum) - kHeadroom<NT>) * kLn2;
+}
 
 // One workgroup of NW wavefronts per (row, KV head, split of its key units).
 template <typename T, int D, int KU, int NW>
@@ -410,7 +421,7 @@ __global__ __launch_bounds__(NW * 64, 2) void qcache_attn_kernel(QAttnArgs a) {
 #pragma unroll
     for (int i = 0; i < NW; ++i) {
       const float* r = red + (i * a.G + hh) * W;
-      const float f = fast_exp2(r[D] - ref);
+      const float f = fast_exp2((r[D] - ref) * a.qscale2);
       ll += r[D + 1] * f;
       oo += r[dd] * f;
     }
@@ -421,7 +432,7 @@ __global__ __launch_bounds__(NW * 64, 2) void qcache_attn_kernel(QAttnArgs a) {
         static_cast<uint16_t*>(a.o)[orow * D + dd] = f32_to_bf16_rne(res);
       else
         static_cast<float*>(a.o)[orow * D + dd] = res;
-      if (a.lse && dd == 0) a.lse[orow] = ll == 0.f ? -INFINITY : (ref + fast_log2(ll)) * kLn2;
+      if (a.lse && dd == 0) a.lse[orow] = row_lse<NT>(ref, ll, a.qscale2);
     } else {
       a.part_o[((w * a.splits + split) * a.G + hh) * D + dd] = oo;
       if (dd == 0) a.part_ml[(w * a.G + hh) * a.splits + split] = make_float2(top, ll);
@@ -435,6 +446,7 @@ constexpr int kMaxSplits = 16;
 template <typename T, int D>
 __global__ __launch_bounds__(64) void qcache_merge_kernel(QAttnArgs a) {
   constexpr int E = D / 64;
+  constexpr int NT = sizeof(T) == 4 ? 3 : 1;
   const int64_t w = blockIdx.x;
   const int hh = blockIdx.y, lane = threadIdx.x;
   const float2 ml = lane < a.splits ? a.part_ml[(w * a.G + hh) * a.splits + lane] : make_float2(-INFINITY, 0.f);
@@ -451,7 +463,7 @@ __global__ __launch_bounds__(64) void qcache_merge_kernel(QAttnArgs a) {
 #pragma unroll
   for (int o = 1; o < kMaxSplits; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
   const float ref = top == -INFINITY ? 0.f : top;
-  const float f = fast_exp2(ml.x - ref);
+  const float f = fast_exp2((ml.x - ref) * a.qscale2);
   float ll = ml.y * f;
 #pragma unroll
   for (int o = 1; o < kMaxSplits; o <<= 1) ll += __shfl_xor(ll, o);
@@ -477,7 +489,7 @@ __global__ __launch_bounds__(64) void qcache_merge_kernel(QAttnArgs a) {
     else
       static_cast<float*>(a.o)[orow * D + lane * E + e] = oo[e] * inv;
   }
-  if (a.lse && lane == 0) a.lse[orow] = ll == 0.f ? -INFINITY : (ref + fast_log2(ll)) * kLn2;
+  if (a.lse && lane == 0) a.lse[orow] = row_lse<NT>(ref, ll, a.qscale2);
 }
 
 // Many rows (bf16): the (row, slot) pairs are grouped by key block, and a
@@ -485,7 +497,8 @@ __global__ __launch_bounds__(64) void qcache_merge_kernel(QAttnArgs a) {
 // one row's G heads: the block's codes are read once and turned into operands
 // once for all of them.  Each pair leaves its own softmax of the block, normalised,
 // in units of the values' scale (so at most 448) and rounded to fp16 (relative
-// 2^-11; its log sum stays in fp32), and qcache_combine_kernel merges a row's K.
+// 2^-11; its largest logit and sum stay in fp32, apart: the logarithm of the sum
+// would be lost in a large logit), and qcache_combine_kernel merges a row's K.
 //   part_o [BH][rows][K][G][D], within each 32 dimensions in the order
 //   [grp][dimension tile 0..1][4], so that a lane stores 16 bytes at a time
 constexpr int kBlockTiles = 8;  // tiles of a wavefront, at most
@@ -495,7 +508,7 @@ struct QBlockArgs {
   const int32_t *offs, *toffs, *pairs;  // launch_cluster
   int64_t ncl;
   uint16_t* part_o;
-  float* part_lse;
+  float2* part_ml;  // [BH][rows][K][G]: largest logit, sum of weights
   int nrows;  // rows of this launch, from a.row0 on
   int chunk;  // pairs of one block per workgroup, at most
 };
@@ -585,7 +598,7 @@ __global__ __launch_bounds__(64, WHOLE ? (D == 128 ? 3 : 4) : 2) void qcache_blo
       const bool partial = __any(nkeys < KU);
       f32x4a s[KU / 16];
       unit_logits<D, KU, 1>(whole, qt, partial, nkeys, grp, s);
-      m = column_max<KU / 16>(s) * a.qscale2 - kHeadroom<1>;
+      m = column_max<KU / 16>(s);
       Weights<1> pt[KU / 32];
       l = weights<KU / 16, 1>(s, a.qscale2, m == -INFINITY ? 0.f : m, pt);
       close();
@@ -613,7 +626,7 @@ __global__ __launch_bounds__(64, WHOLE ? (D == 128 ? 3 : 4) : 2) void qcache_blo
 #pragma unroll
       for (int dj = 0; dj < DT / 2; ++dj) store(dj, sm.oacc[2 * dj], sm.oacc[2 * dj + 1], inv);
     }
-    if (live && grp == 0) p.part_lse[pidx] = l == 0.f ? -INFINITY : m + fast_log2(l);
+    if (live && grp == 0) p.part_ml[pidx] = make_float2(m, l);
   }
 }
 
@@ -638,37 +651,45 @@ __global__ __launch_bounds__(256) void qcache_combine_kernel(QBlockArgs p) {
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = 0.f;
   for (int s0 = grp; s0 < a.K; s0 += 4 * SPL) {
-    float ls[SPL], sc[SPL], x[SPL][E];
+    int blk[SPL];
 #pragma unroll
     for (int i = 0; i < SPL; ++i) {
-      const int slot = s0 + 4 * i;
-      const int blk = slot < a.K ? sel[slot] : -1;
-      const bool have = static_cast<uint32_t>(blk) < static_cast<uint32_t>(a.M1);  // padding left no partial
-      ls[i] = have ? p.part_lse[(base + slot) * a.G + hh] : -INFINITY;
-      sc[i] = have ? a.c.v_scale[static_cast<int64_t>(bh) * a.c.M + blk] : 0.f;
+      const int b = s0 + 4 * i < a.K ? sel[s0 + 4 * i] : -1;
+      blk[i] = static_cast<uint32_t>(b) < static_cast<uint32_t>(a.M1) ? b : -1;  // padding left no partial
+    }
+    float2 ml[SPL];
+    float sc[SPL];
+    uint32_t raw[SPL][E / 2];  // converted when all of them are asked for
 #pragma unroll
-      for (int e = 0; e < E; ++e) x[i][e] = 0.f;
-      if (have) {
-        _Float16 raw[E];
-        __builtin_memcpy(raw, __builtin_assume_aligned(p.part_o + ((base + slot) * a.G + hh) * D + sub * E, 2 * E), 2 * E);
+    for (int i = 0; i < SPL; ++i) {
+      ml[i] = make_float2(-INFINITY, 0.f);
+      sc[i] = 0.f;
 #pragma unroll
-        for (int e = 0; e < E; ++e) x[i][e] = static_cast<float>(raw[e]);
+      for (int e = 0; e < E / 2; ++e) raw[i][e] = 0;
+      if (blk[i] >= 0) {
+        const int64_t at = (base + s0 + 4 * i) * a.G + hh;
+        ml[i] = p.part_ml[at];
+        sc[i] = a.c.v_scale[static_cast<int64_t>(bh) * a.c.M + blk[i]];
+        __builtin_memcpy(raw[i], __builtin_assume_aligned(p.part_o + at * D + sub * E, 2 * E), 2 * E);
       }
     }
     float top = m;
 #pragma unroll
-    for (int i = 0; i < SPL; ++i) top = fmaxf(top, ls[i]);
+    for (int i = 0; i < SPL; ++i) top = fmaxf(top, ml[i].x);
     const float ref = top == -INFINITY ? 0.f : top;
-    const float f = fast_exp2(m - ref);
+    const float f = fast_exp2((m - ref) * a.qscale2);
     l *= f;
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] *= f;
 #pragma unroll
     for (int i = 0; i < SPL; ++i) {
-      const float w = fast_exp2(ls[i] - ref);
+      const float w = ml[i].y * fast_exp2((ml[i].x - ref) * a.qscale2);
       l += w;
 #pragma unroll
-      for (int e = 0; e < E; ++e) o[e] = fmaf(w * sc[i], x[i][e], o[e]);
+      for (int e = 0; e < E; ++e) {
+        const _Float16 x = __builtin_bit_cast(f16x2a, raw[i][e / 2])[e % 2];
+        o[e] = fmaf(w * sc[i], static_cast<float>(x), o[e]);
+      }
     }
     m = top;
   }
@@ -676,7 +697,7 @@ __global__ __launch_bounds__(256) void qcache_combine_kernel(QBlockArgs p) {
   for (int msk = 16; msk <= 32; msk <<= 1) {
     const float m2 = __shfl_xor(m, msk), l2 = __shfl_xor(l, msk);
     const float top = fmaxf(m, m2), ref = top == -INFINITY ? 0.f : top;
-    const float f = fast_exp2(m - ref), f2 = fast_exp2(m2 - ref);
+    const float f = fast_exp2((m - ref) * a.qscale2), f2 = fast_exp2((m2 - ref) * a.qscale2);
     l = l * f + l2 * f2;
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] = o[e] * f + __shfl_xor(o[e], msk) * f2;
@@ -693,7 +714,7 @@ __global__ __launch_bounds__(256) void qcache_combine_kernel(QBlockArgs p) {
       const int d = pos / 32 * 32 + (pos & 4) * 4 + (pos % 32) / 8 * 4;
       *reinterpret_cast<uint2*>(dst + d) = make_uint2(pack2_bf16(o[e] * inv, o[e + 1] * inv), pack2_bf16(o[e + 2] * inv, o[e + 3] * inv));
     }
-    if (a.lse && sub == 0) a.lse[orow] = l == 0.f ? -INFINITY : (m + fast_log2(l)) * kLn2;
+    if (a.lse && sub == 0) a.lse[orow] = row_lse<1>(m, l, a.qscale2);
   }
 }
 
@@ -784,7 +805,7 @@ static bool use_blocks(const Shape& s, const Geo& geo) {
   return saved >= 32000 + 2.5 * s.BH() * geo.M[1];
 }
 
-// Rows per pass: their partials take at most 1 GB.
+// Rows per pass: their partials take about 1 GB.
 constexpr size_t kPartialBytes = size_t(1) << 30;
 static int block_rows(const Shape& s) {
   const size_t per_row = static_cast<size_t>(s.BH()) * s.K * s.G * (s.D * 2 + 4);
@@ -798,14 +819,14 @@ static int group_rows(const Shape& s) { return std::max(64, 4096 / s.K); }
 // 8 113, one of 16 106).
 static int pair_chunk(const Shape& s) { return 16 / s.G * kBlockTiles; }
 struct BlockWs {
-  size_t part_o, part_lse, cl, total;
+  size_t part_o, part_ml, cl, total;
 };
 static BlockWs block_layout(const Shape& s, const Geo& geo) {
   const int rows = block_rows(s);
   const size_t np = static_cast<size_t>(s.BH()) * rows * s.K;
   BlockWs w{};
-  w.part_lse = al256(np * s.G * s.D * 2);
-  w.cl = w.part_lse + al256(np * s.G * 4);
+  w.part_ml = al256(np * s.G * s.D * 2);
+  w.cl = w.part_ml + al256(np * s.G * sizeof(float2));
   w.total = w.cl + al256(cluster_ws(s.BH(), geo.M[1], static_cast<int64_t>(np), rows, group_rows(s)));
   return w;
 }
@@ -817,7 +838,7 @@ static hipError_t launch_blocks(const Shape& s, const Geo& geo, const QAttnArgs&
   QBlockArgs p{};
   p.a = a;
   p.part_o = reinterpret_cast<uint16_t*>(base + w.part_o);
-  p.part_lse = reinterpret_cast<float*>(base + w.part_lse);
+  p.part_ml = reinterpret_cast<float2*>(base + w.part_ml);
   for (int row0 = 0; row0 < s.Nq; row0 += rows) {
     p.a.row0 = row0;
     p.nrows = std::min(rows, s.Nq - row0);
