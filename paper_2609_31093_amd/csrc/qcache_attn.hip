@@ -22,7 +22,9 @@
 //
 // The running maximum is that of the products S themselves, and the softmax's
 // scale (with log2 e) multiplies differences from it: a large logit that is
-// rounded with its scale first is off by more than fp16's last two octaves. 
+// rounded with its scale first is off by more than fp16's last two octaves.  The
+// sums over a row are held in units of kRowUnit, so that values up to the type's
+// largest do not overflow before they are divided by the weights' sum.
 #include <algorithm>
 
 #include "attn_shared.h"
@@ -86,6 +88,13 @@ __device__ __forceinline__ void split_terms(const float (&x)[8], bf16x8a (&t)[NT
 // log2 of the largest weight.
 template <int NT>
 constexpr float kHeadroom = NT == 1 ? 14.f : 0.f;
+
+// A row's sums of weights times values, and of weights before they divide them,
+// are taken times this: 1 / (the largest weight times a row's 128 * 256 tokens at
+// most).  A power of two, so nothing is rounded by it; the least value, 2^-109,
+// leaves a sum of 2^-124, which still has all its bits.
+template <int NT>
+constexpr float kRowUnit = NT == 1 ? 0x1p-29f : 0x1p-15f;
 
 // Weights as the values' operands: fp16, or with NT = 3 bf16 terms, and four
 // codes (unscaled) to go with them.
@@ -289,7 +298,8 @@ __device__ __forceinline__ f32x4a value_tile_by_column(const Unit<D, KU>& u, int
 
 // Running softmax of a wavefront's 16 columns over key units.  MIXED: the
 // columns' visible keys differ (otherwise the hidden values' codes are cleared),
-// and the units are of one block, whose values' scale is left to the caller.
+// and the units are of one block, whose values' scale is left to the caller;
+// otherwise the values' sums are in units of kRowUnit.
 template <int D, int KU, int NT>
 struct Softmax {
   using U = Unit<D, KU>;
@@ -313,7 +323,7 @@ struct Softmax {
     Weights<NT> pt[U::MT / 2];
     l = l * corr + weights<U::MT, NT>(s, qscale2, ref, pt);
     const bool by_column = MIXED && partial && u.nan_value();
-    const float scale = MIXED ? 1.f : u.vsc;
+    const float scale = MIXED ? 1.f : u.vsc * kRowUnit<NT>;
 #pragma unroll
     for (int dt = 0; dt < U::DT; ++dt) {
       const f32x4a x = MIXED && by_column ? value_tile_by_column<D, KU, NT>(u, dt, pt, nkeys, grp) : value_tile<D, KU, NT>(u, dt, pt);
@@ -427,7 +437,7 @@ __global__ __launch_bounds__(NW * 64, 2) void qcache_attn_kernel(QAttnArgs a) {
     }
     if (a.splits == 1) {
       const int64_t orow = (static_cast<int64_t>(b) * a.H + h * a.G + hh) * a.Nq + row;
-      const float res = ll == 0.f ? 0.f : oo / ll;
+      const float res = ll == 0.f ? 0.f : oo / (ll * kRowUnit<NT>);
       if constexpr (sizeof(T) == 2)
         static_cast<uint16_t*>(a.o)[orow * D + dd] = f32_to_bf16_rne(res);
       else
@@ -468,7 +478,7 @@ __global__ __launch_bounds__(64) void qcache_merge_kernel(QAttnArgs a) {
 #pragma unroll
   for (int o = 1; o < kMaxSplits; o <<= 1) ll += __shfl_xor(ll, o);
   ll = __shfl(ll, 0);
-  const float inv = ll == 0.f ? 0.f : 1.f / ll;
+  const float inv = ll == 0.f ? 0.f : 1.f / (ll * kRowUnit<NT>);
   float oo[E] = {};
 #pragma unroll
   for (int i = 0; i < kMaxSplits; ++i) {
@@ -688,7 +698,7 @@ __global__ __launch_bounds__(256) void qcache_combine_kernel(QBlockArgs p) {
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         const _Float16 x = __builtin_bit_cast(f16x2a, raw[i][e / 2])[e % 2];
-        o[e] = fmaf(w * sc[i], static_cast<float>(x), o[e]);
+        o[e] = fmaf(w * (sc[i] * kRowUnit<1>), static_cast<float>(x), o[e]);
       }
     }
     m = top;
@@ -704,7 +714,7 @@ __global__ __launch_bounds__(256) void qcache_combine_kernel(QBlockArgs p) {
     m = top;
   }
   if (grp == 0) {
-    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const float inv = l == 0.f ? 0.f : 1.f / (l * kRowUnit<1>);
     const int64_t orow = (static_cast<int64_t>(b) * a.H + hq) * a.Nq + row;
     uint16_t* dst = static_cast<uint16_t*>(a.o) + orow * D;
     // value i of this lane's part is at position sub*E + i of the stored order

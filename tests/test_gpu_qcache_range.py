@@ -1,4 +1,4 @@
-"""Attention over the 8-bit cache with logits of any size that its types hold.
+"""Attention over the 8-bit cache with logits and values of any size that its types hold.
 
 Large logits.  Only dimension 0 of keys and queries is not 0, so every logit is one product of a power of two and a code:
 exact in 32 bits, and equal for many keys.  The rows' weights are then those of the largest logits alone, equal ones, up
@@ -7,6 +7,8 @@ to the error of what is computed from exact differences: 2^-21 of a weight (2 ul
 twice for sums of n terms, 2^-8 of the result (bf16) or 2^-23.  Keys that are not the largest are at least 2^a / 16 / 12
 below it (2^12 and more), so their weights are 0.  lse = (largest logit) + log(number of them): 2^-22 of it, 2^-20 of a
 sum and n 2^-24.
+
+Large and small values: the bounds of test_gpu_qcache, which scale with the values.
 """
 import math
 
@@ -88,3 +90,21 @@ def test_large_logits(form, power):
                 assert (abs(o[b, h, r] - want) <= tol).all(), (b, h, r, abs(o[b, h, r] - want).max())
                 want = z.max() / math.sqrt(d) + math.log(len(top))
                 assert abs(lse[b, h, r] - want) <= 2.0 ** -22 * abs(want) + 2.0 ** -20 + n * 2.0 ** -24, (b, h, r)
+
+
+@pytest.mark.parametrize("power", [-106, -60, 110, 125, 127])
+@pytest.mark.parametrize("form", FORMS, ids=str)
+def test_values_of_any_size(form, power):
+    """Values of one sign near 2^power: their weighted sums, before the division by the weights' sum, would not be finite."""
+    B, H, Hkv, Nq, N, d, C, g, K, causal, dtype = form
+    p = base.problem(*form)
+    k, q = base.normal((B, Hkv, N, d), 1, dtype, 0.5), base.normal((B, H, Nq, d), 3, dtype)
+    v = torch.rand((B, Hkv, N, d), generator=torch.Generator("cuda").manual_seed(2), device="cuda") * 0.5 + 0.5
+    cache = filled(p, k, (v * 2.0 ** power).to(base.TYPES[dtype]))
+    idx = selection(p)
+    o, lse = pisa.qcache_attn_fwd(p, cache, q, idx)
+    assert torch.isfinite(o).all()
+    if grouped(p):
+        base.check_grouped(p, cache, q, idx, o, lse, base.sample(p, 5))
+    else:
+        base.check_attention(p, cache, q, idx, o, lse, base.sample(p, 5) if Nq > 97 else None)
