@@ -9,6 +9,7 @@ if the library has not been built (there is no fallback path).
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import functools
 import os
@@ -369,12 +370,37 @@ def _workspace(nbytes: int, device):
     return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
+_HERE = contextlib.nullcontext()
+
+
+def _elsewhere(stream):
+    return stream is not None and _stream(stream) != _stream(None)
+
+
+def _on(stream, device):
+    """Context in which what a call on `stream` uses is allocated: memory of the current stream's would be handed to its
+    next allocations while `stream` still works on it, and may be in use there when `stream` begins."""
+    if not _elsewhere(stream):
+        return _HERE
+    return torch.cuda.stream(torch.cuda.ExternalStream(_stream(stream), device=device))
+
+
+def _results(stream, *tensors):
+    """Outputs allocated under _on, which the caller's stream reads: not handed on before it has."""
+    if _elsewhere(stream):
+        for x in tensors:
+            if x is not None:
+                x.record_stream(torch.cuda.current_stream(x.device))
+    return tensors if len(tensors) > 1 else tensors[0]
+
+
 def build_pyramid(p: Problem, k, stream=None):
     """Allocate [B, Hkv, R, d] float32 and fill it with pisa_build_pyramid."""
     _, R = pisa_pyramid_layout(p)
-    pyr = torch.empty((p.B, p.Hkv, R, p.d), dtype=torch.float32, device=k.device)
+    with _on(stream, k.device):
+        pyr = torch.empty((p.B, p.Hkv, R, p.d), dtype=torch.float32, device=k.device)
     pisa_build_pyramid(p, k, pyr, stream)
-    return pyr
+    return _results(stream, pyr)
 
 
 def grow_cache(p: Problem, new_cap: int, pyramid, k=None, v=None, stream=None):
@@ -384,59 +410,70 @@ def grow_cache(p: Problem, new_cap: int, pyramid, k=None, v=None, stream=None):
     pn = Problem(*[getattr(p, n) for n, _ in Problem._fields_])
     pn.Ncap = new_cap
     _, R = pisa_pyramid_layout(pn)
-    pyr = torch.empty((p.B, p.Hkv, R, p.d), dtype=torch.float32, device=pyramid.device)
     kn = vn = None
-    if k is not None:
-        kn = torch.empty((p.B, p.Hkv, new_cap, p.d), dtype=k.dtype, device=k.device)
-        vn = torch.empty((p.B, p.Hkv, new_cap, p.d), dtype=v.dtype, device=v.device)
+    with _on(stream, pyramid.device):
+        pyr = torch.empty((p.B, p.Hkv, R, p.d), dtype=torch.float32, device=pyramid.device)
+        if k is not None:
+            kn = torch.empty((p.B, p.Hkv, new_cap, p.d), dtype=k.dtype, device=k.device)
+            vn = torch.empty((p.B, p.Hkv, new_cap, p.d), dtype=v.dtype, device=v.device)
     pisa_cache_grow(p, new_cap, pyramid, pyr, k, kn, v, vn, stream)
-    return pn, pyr, kn, vn
+    return pn, *_results(stream, pyr, kn, vn)
 
 
 def select(p: Problem, q, k, pyramid, with_score=False, stream=None):
     """Allocate outputs and workspace, run pisa_select; returns idx (and scores)."""
-    idx = torch.empty((p.B, p.Hkv, p.Nq, p.K), dtype=torch.int32, device=q.device)
-    sc = torch.empty((p.B, p.Hkv, p.Nq, p.K), dtype=torch.float32, device=q.device) if with_score else None
     nb = pisa_select_workspace_bytes(p)
-    ws = _workspace(nb, q.device)
+    with _on(stream, q.device):
+        idx = torch.empty((p.B, p.Hkv, p.Nq, p.K), dtype=torch.int32, device=q.device)
+        sc = torch.empty((p.B, p.Hkv, p.Nq, p.K), dtype=torch.float32, device=q.device) if with_score else None
+        ws = _workspace(nb, q.device)
     pisa_select(p, q, k, pyramid, idx, sc, ws, nb, stream)
+    _results(stream, idx, sc)
     return (idx, sc) if with_score else idx
 
 
 def select_flat_bsa(p: Problem, q, pyramid, stream=None):
-    idx = torch.empty((p.B, p.Hkv, p.Nq, p.K), dtype=torch.int32, device=q.device)
     nb = pisa_bsa_workspace_bytes(p)
-    pisa_select_flat_bsa(p, q, pyramid, idx, _workspace(nb, q.device), nb, stream)
-    return idx
+    with _on(stream, q.device):
+        idx = torch.empty((p.B, p.Hkv, p.Nq, p.K), dtype=torch.int32, device=q.device)
+        ws = _workspace(nb, q.device)
+    pisa_select_flat_bsa(p, q, pyramid, idx, ws, nb, stream)
+    return _results(stream, idx)
 
 
 def sparse_attn_fwd(p: Problem, q, k, v, block_idx, stream=None):
-    o = torch.empty_like(q)
-    lse = torch.empty((p.B, p.H, p.Nq), dtype=torch.float32, device=q.device)
     nb = pisa_attn_workspace_bytes(p)
-    pisa_sparse_attn_fwd(p, q, k, v, block_idx, o, lse, _workspace(nb, q.device), nb, stream)
-    return o, lse
+    with _on(stream, q.device):
+        o = torch.empty_like(q)
+        lse = torch.empty((p.B, p.H, p.Nq), dtype=torch.float32, device=q.device)
+        ws = _workspace(nb, q.device)
+    pisa_sparse_attn_fwd(p, q, k, v, block_idx, o, lse, ws, nb, stream)
+    return _results(stream, o, lse)
 
 
 def selection_quality(p: Problem, q, k, block_idx, rows, stream=None):
     """Allocate outputs and workspace, run pisa_selection_quality on the listed
     rows (a device int32 tensor); returns (metrics [B,Hkv,n,3], ref [B,Hkv,n,K])."""
     n = int(rows.numel())
-    met = torch.empty((p.B, p.Hkv, n, 3), dtype=torch.float32, device=q.device)
-    ref = torch.empty((p.B, p.Hkv, n, p.K), dtype=torch.int32, device=q.device)
     nb = pisa_quality_workspace_bytes(p, n)
-    pisa_selection_quality(p, q, k, block_idx, rows, n, met, ref, _workspace(nb, q.device), nb, stream)
-    return met, ref
+    with _on(stream, q.device):
+        met = torch.empty((p.B, p.Hkv, n, 3), dtype=torch.float32, device=q.device)
+        ref = torch.empty((p.B, p.Hkv, n, p.K), dtype=torch.int32, device=q.device)
+        ws = _workspace(nb, q.device)
+    pisa_selection_quality(p, q, k, block_idx, rows, n, met, ref, ws, nb, stream)
+    return _results(stream, met, ref)
 
 
 def sparse_attn_bwd(p: Problem, q, k, v, block_idx, o, lse, d_o, stream=None):
     """Allocate gradients and workspace, run pisa_sparse_attn_bwd; returns (dq, dk, dv)."""
-    dq = torch.empty_like(q)
-    dk = torch.empty_like(k)
-    dv = torch.empty_like(v)
     nb = pisa_attn_bwd_workspace_bytes(p)
-    pisa_sparse_attn_bwd(p, q, k, v, block_idx, o, lse, d_o, dq, dk, dv, _workspace(nb, q.device), nb, stream)
-    return dq, dk, dv
+    with _on(stream, q.device):
+        dq = torch.empty_like(q)
+        dk = torch.empty_like(k)
+        dv = torch.empty_like(v)
+        ws = _workspace(nb, q.device)
+    pisa_sparse_attn_bwd(p, q, k, v, block_idx, o, lse, d_o, dq, dk, dv, ws, nb, stream)
+    return _results(stream, dq, dk, dv)
 
 
 # ------------------------------------------------- rotary positions, 8-bit cache ---
@@ -484,7 +521,7 @@ def make_rope(B, H, Hkv, N, d, rot=None, layout="half", dtype="bf16", base=10000
     return r
 
 
-def _side(x, y, name, dtype, shape, device):
+def _side(x, y, name, dtype, shape, device, stream):
     """(x, its strides, output, its strides) of one side of a rotation, the output allocated where y is None."""
     if x is None:
         if y is not None:
@@ -492,7 +529,9 @@ def _side(x, y, name, dtype, shape, device):
         return None, None, None, None
     xs = _strided(x, name, dtype, shape, device)
     if y is None:
-        return x, xs, torch.empty(shape, dtype=dtype, device=x.device), None
+        with _on(stream, x.device):
+            y = torch.empty(shape, dtype=dtype, device=x.device)
+        return x, xs, _results(stream, y), None
     return x, xs, y, _strided(y, name + "_out", dtype, shape, device)
 
 
@@ -505,8 +544,8 @@ def _rope(turn, r: Rope, q, k, positions, q_out, k_out, stream):
         if r.pos_bstride != stride:  # in a copy: the caller's may be in use by another thread's call
             r = Rope.from_buffer_copy(r)
             r.pos_bstride = stride
-    q, qs, q_out, qos = _side(q, q_out, "q", dt, (B, r.H, N, d), dev)
-    k, ks, k_out, kos = _side(k, k_out, "k", dt, (B, r.Hkv, N, d), dev)
+    q, qs, q_out, qos = _side(q, q_out, "q", dt, (B, r.H, N, d), dev, stream)
+    k, ks, k_out, kos = _side(k, k_out, "k", dt, (B, r.Hkv, N, d), dev, stream)
     turn(r, q, qs, k, ks, positions, q_out, qos, k_out, kos, stream)
     return q_out, k_out
 
@@ -604,8 +643,10 @@ def qcache_attn_fwd(p: Problem, cache: QCache, q, block_idx, stream=None):
     dev = cache.device
     _take(q, "q", _TORCH[p.dtype], (p.B, p.H, p.Nq, p.d), dev)
     _take(block_idx, "block_idx", torch.int32, (p.B, p.Hkv, p.Nq, p.K), dev)
-    o = torch.empty_like(q)
-    lse = torch.empty((p.B, p.H, p.Nq), dtype=torch.float32, device=q.device)
     nb = pisa_qcache_attn_workspace_bytes(p)
-    pisa_qcache_attn_fwd(p, cache, q, block_idx, o, lse, _workspace(nb, q.device), nb, stream)
-    return o, lse
+    with _on(stream, q.device):
+        o = torch.empty_like(q)
+        lse = torch.empty((p.B, p.H, p.Nq), dtype=torch.float32, device=q.device)
+        ws = _workspace(nb, q.device)
+    pisa_qcache_attn_fwd(p, cache, q, block_idx, o, lse, ws, nb, stream)
+    return _results(stream, o, lse)
