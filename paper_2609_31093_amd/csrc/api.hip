@@ -325,6 +325,32 @@ int static_scratch(void** out) {
   return PISA_OK;
 }
 
+// Are there two rows of d values less than d apart?  They are `off` plus, for each
+// dimension from `at` on (largest stride first), its stride times a difference of
+// indexes within [lo, hi].  `same`: no difference so far, where a row is not to be
+// compared with itself.  Where no stride is less than what the smaller ones span,
+// each dimension leaves a few differences to look at; after `steps` of them the
+// rows count as meeting.
+struct IndexRange {
+  int64_t stride, lo, hi;
+};
+bool rows_meet(const IndexRange (&dim)[3], int at, __int128 off, int d, bool same, int* steps) {
+  if (at == 3) return off > -d && off < d && !same;
+  __int128 reach = d - 1;  // of the dimensions behind this one
+  for (int i = at + 1; i < 3; ++i) reach += static_cast<__int128>(dim[i].stride) * std::max(-dim[i].lo, dim[i].hi);
+  const int64_t st = dim[at].stride;
+  int64_t lo = dim[at].lo, hi = dim[at].hi;
+  if (st > 0) {
+    auto floor_div = [&](__int128 x) { return x >= 0 ? x / st : -((-x + st - 1) / st); };
+    lo = static_cast<int64_t>(std::max<__int128>(lo, -floor_div(reach + off)));
+    hi = static_cast<int64_t>(std::min<__int128>(hi, floor_div(reach - off)));
+  }
+  for (int64_t i = lo; i <= hi; ++i)
+    if (--*steps < 0 || rows_meet(dim, at + 1, off + static_cast<__int128>(st) * i, d, same && i == 0, steps)) return true;
+  return false;
+}
+constexpr int kMeetSteps = 10000;
+
 // Strides of a [B, heads, rows, d] tensor (the contiguous ones where NULL).
 // Written tensors keep their rows apart.
 int check_strides(const pisa_strides* in, const char* name, int64_t B, int64_t heads, int64_t rows, int d, int dtype,
@@ -338,8 +364,12 @@ int check_strides(const pisa_strides* in, const char* name, int64_t B, int64_t h
     if (x < 0 || x % unit != 0)
       return fail(PISA_ERR_INVALID_ARG, "strides of %s must be non-negative multiples of 16 bytes (got %lld elements)", name,
                   static_cast<long long>(x));
-  if (written && ((B > 1 && in->b < d) || (heads > 1 && in->h < d) || (rows > 1 && in->n < d)))
-    return fail(PISA_ERR_INVALID_ARG, "strides of %s make its rows overlap", name);
+  if (written) {
+    IndexRange dim[3] = {{in->b, 1 - B, B - 1}, {in->h, 1 - heads, heads - 1}, {in->n, 1 - rows, rows - 1}};
+    std::sort(dim, dim + 3, [](const IndexRange& x, const IndexRange& y) { return x.stride > y.stride; });
+    int steps = kMeetSteps;
+    if (rows_meet(dim, 0, 0, d, true, &steps)) return fail(PISA_ERR_INVALID_ARG, "strides of %s make its rows overlap", name);
+  }
   *out = *in;
   return PISA_OK;
 }
