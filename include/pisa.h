@@ -359,7 +359,10 @@ int pisa_rope_frequencies(pisa_rope* r, double base, int32_t scaling, double fac
 
 /* Turns q and k (either may be NULL together with its output) in one launch.
  * An output may be its own input (same pointer and strides); otherwise outputs
- * overlap neither inputs nor each other.  Arithmetic in float32, rounded once. */
+ * overlap neither inputs nor each other, nor their own rows (PISA_ERR_INVALID_ARG;
+ * tensors of the same strides, as the parts of a packed projection, are compared
+ * value by value, others by what lies between their first value and their last).
+ * Arithmetic in float32, rounded once. */
 int pisa_rope_fwd(const pisa_rope* r, const void* q, const pisa_strides* q_strides, const void* k,
                   const pisa_strides* k_strides, const int32_t* positions, void* q_out,
                   const pisa_strides* q_out_strides, void* k_out, const pisa_strides* k_out_strides,

@@ -340,7 +340,10 @@ bool rows_meet(const IndexRange (&dim)[3], int at, __int128 off, int d, bool sam
   for (int i = at + 1; i < 3; ++i) reach += static_cast<__int128>(dim[i].stride) * std::max(-dim[i].lo, dim[i].hi);
   const int64_t st = dim[at].stride;
   int64_t lo = dim[at].lo, hi = dim[at].hi;
-  if (st > 0) {
+  if (reach + (off < 0 ? -off : off) < st) {  // the usual case, without divisions
+    lo = std::max<int64_t>(lo, 0);
+    hi = std::min<int64_t>(hi, 0);
+  } else if (st > 0) {
     auto floor_div = [&](__int128 x) { return x >= 0 ? x / st : -((-x + st - 1) / st); };
     lo = static_cast<int64_t>(std::max<__int128>(lo, -floor_div(reach + off)));
     hi = static_cast<int64_t>(std::min<__int128>(hi, floor_div(reach - off)));
@@ -413,6 +416,34 @@ int check_rope_side(const pisa_rope* r, const char* name, int heads, const void*
   return PISA_OK;
 }
 
+// A [B, heads, rows, d] tensor where it lies.
+struct Placed {
+  const void* ptr;
+  pisa_strides s;
+  int64_t B, heads, rows;
+};
+// Do two tensors share memory?  Those whose spans meet but whose strides are
+// alike (two parts of a packed projection) are compared row by row as rows_meet
+// does; other strides count as sharing.
+bool share(const Placed& x, const Placed& y, int d, int64_t esz) {
+  auto span = [&](const Placed& t) {
+    return (static_cast<__int128>(t.B - 1) * t.s.b + static_cast<__int128>(t.heads - 1) * t.s.h +
+            static_cast<__int128>(t.rows - 1) * t.s.n + d) * esz;
+  };
+  const __int128 at = static_cast<__int128>(reinterpret_cast<uintptr_t>(y.ptr)) - reinterpret_cast<uintptr_t>(x.ptr);
+  if (at >= span(x) || -at >= span(y)) return false;
+  IndexRange dim[3];
+  const int64_t ex[3] = {x.B, x.heads, x.rows}, ey[3] = {y.B, y.heads, y.rows};
+  const int64_t sx[3] = {x.s.b, x.s.h, x.s.n}, sy[3] = {y.s.b, y.s.h, y.s.n};
+  for (int i = 0; i < 3; ++i) {
+    if (ex[i] > 1 && ey[i] > 1 && sx[i] != sy[i]) return true;
+    dim[i] = {ex[i] > 1 ? sx[i] : sy[i], 1 - ex[i], ey[i] - 1};
+  }
+  std::sort(dim, dim + 3, [](const IndexRange& a, const IndexRange& b) { return a.stride > b.stride; });
+  int steps = kMeetSteps;
+  return rows_meet(dim, 0, at / esz, d, false, &steps);
+}
+
 int run_rope(const pisa_rope* r, const void* q, const pisa_strides* qs, const void* k, const pisa_strides* ks,
              const int32_t* positions, void* qo, const pisa_strides* qos, void* ko, const pisa_strides* kos, float sign,
              pisa_stream_t stream, const char* who) {
@@ -423,6 +454,22 @@ int run_rope(const pisa_rope* r, const void* q, const pisa_strides* qs, const vo
   if (!q && !k) return fail(PISA_ERR_INVALID_ARG, "neither q nor k given");
   if (positions && (reinterpret_cast<uintptr_t>(positions) & 3u))
     return fail(PISA_ERR_INVALID_ARG, "positions is not 4-byte aligned");
+  // rows are read and written in one launch, in any order
+  auto placed = [&](const void* ptr, int64_t b, int64_t h, int64_t n, int heads) {
+    return Placed{ptr, pisa_strides{b, h, n}, r->B, heads, r->N};
+  };
+  const Placed in[2] = {placed(a.q.in, a.q.ib, a.q.ih, a.q.in_n, r->H), placed(a.k.in, a.k.ib, a.k.ih, a.k.in_n, r->Hkv)};
+  const Placed out[2] = {placed(a.q.out, a.q.ob, a.q.oh, a.q.on, r->H), placed(a.k.out, a.k.ob, a.k.oh, a.k.on, r->Hkv)};
+  const char* const names[2] = {"q", "k"};
+  const int64_t esz = r->dtype == PISA_DTYPE_BF16 ? 2 : 4;
+  for (int i = 0; i < 2; ++i) {
+    if (!out[i].ptr) continue;
+    for (int j = 0; j < 2; ++j) {
+      if (in[j].ptr && !(i == j && in[j].ptr == out[i].ptr) && share(out[i], in[j], r->d, esz))
+        return fail(PISA_ERR_INVALID_ARG, "%s (output) overlaps %s", names[i], names[j]);
+    }
+  }
+  if (q && k && share(out[0], out[1], r->d, esz)) return fail(PISA_ERR_INVALID_ARG, "q (output) overlaps k (output)");
   a.positions = positions;
   a.pos_bstride = r->pos_bstride;
   a.B = r->B;

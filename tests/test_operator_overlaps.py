@@ -33,3 +33,28 @@ def test_written_rows_that_overlap(name, b, h, n):
     if h >= D:  # the same for keys of as many heads
         assert rotate(name, kos=S(b, h, n), Hkv=H) == INVALID
         assert "k (output)" in pisa.pisa_last_error() and "overlap" in pisa.pisa_last_error()
+
+
+@pytest.mark.parametrize("name", ["pisa_rope_fwd", "pisa_rope_bwd"])
+def test_outputs_that_overlap_inputs_or_each_other(name):
+    def refused(what, **kw):
+        assert rotate(name, **kw) == INVALID and what in pisa.pisa_last_error(), (kw, pisa.pisa_last_error())
+    q_bytes, k_bytes, row = B * H * N * D * 2, B * HKV * N * D * 2, D * 2
+    for at in (0, row, q_bytes - row, -k_bytes + row, q_bytes - 16):
+        refused("q (output) overlaps k", ko=KO, k=QO + at)
+        refused("q (output) overlaps k (output)", ko=QO + at)
+    for at in (0, row, k_bytes - row, -q_bytes + row):
+        refused("k (output) overlaps q", q=KO + at)
+    for at in (row, -row, 16, q_bytes - row):  # not in place, but on its own input
+        refused("q (output) overlaps q", qo=Q + at)
+    refused("k (output) overlaps k", ko=K + row)
+    # parts of one packed projection [B, N, heads, d]: the same memory only where heads are shared
+    packed = S(N * 16 * D, D, 16 * D)
+    refused("q (output) overlaps k", q=Q, qs=packed, qo=Q, qos=packed, k=Q + 3 * row, ks=packed)
+    refused("q (output) overlaps k", q=Q, qs=packed, qo=Q, qos=packed, k=Q + (16 * (N - 1) + 3) * row, ks=packed)
+    refused("k (output) overlaps q", q=Q, qs=packed, qo=QO, k=Q + 2 * row, ks=packed, ko=Q + 2 * row, kos=packed)
+    refused("q (output) overlaps k (output)", qo=QO, qos=packed, ko=QO + 3 * row, kos=packed)
+    # spans that meet under other strides
+    refused("q (output) overlaps k", q=Q, qs=packed, qo=Q, qos=packed, k=Q + 8 * row)
+    # a row that is read for every head
+    refused("q (output) overlaps k", ks=S(0, 0, D), k=QO + 5 * row)
