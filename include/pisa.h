@@ -417,8 +417,8 @@ size_t pisa_qcache_bytes(const pisa_problem* p);
  * The result equals one append of all N rows bit for bit.  pyramid (nullable):
  * the mean pyramid of the raw keys for the same fanout and Ncap, brought from
  * n_old to N, bit for bit as pisa_build_pyramid has it.  k_new and v_new, from
- * their first value to their last, must not overlap the codes or the raw rows
- * (PISA_ERR_INVALID_ARG).  0 <= n_old <= N; n_old = N does nothing.  No
+ * their first value to their last, must not overlap the codes, the scales, the raw
+ * rows or the pyramid (PISA_ERR_INVALID_ARG).  0 <= n_old <= N; n_old = N does nothing.  No
  * workspace; one launch where a single block changes and no level is new. */
 int pisa_qcache_append(const pisa_problem* p, const pisa_qcache* c, const void* k_new, const pisa_strides* k_strides,
                        const void* v_new, const pisa_strides* v_strides, int32_t n_old, float* pyramid,

@@ -844,13 +844,17 @@ int pisa_qcache_append(const pisa_problem* p, const pisa_qcache* c, const void* 
   auto span = [&](const pisa_strides& x) {  // bytes from a tensor's first value to its last
     return ((p->B - 1) * x.b + (p->Hkv - 1) * x.h + (p->N - n_old - 1) * x.n + p->d) * static_cast<int64_t>(esz);
   };
-  const struct { const void* ptr; size_t bytes; const char* name; } fresh[] = {{k_new, static_cast<size_t>(span(ks)), "k_new"},
-                                                                                {v_new, static_cast<size_t>(span(vs)), "v_new"}},
-      held[] = {{c->k, codes, ""}, {c->v, codes, ""}, {c->k_open, open, ""}, {c->v_open, open, ""}};
+  const size_t scales = static_cast<size_t>(s.BH()) * a.c.M * sizeof(float);
+  const size_t levels = static_cast<size_t>(s.BH()) * g.R * s.D * sizeof(float);
+  const struct { const void* ptr; size_t bytes; const char* name; } fresh[] = {
+      {k_new, static_cast<size_t>(span(ks)), "k_new"}, {v_new, static_cast<size_t>(span(vs)), "v_new"}};
+  const struct { const void* ptr; size_t bytes; const char* name; } held[] = {
+      {c->k, codes, "cache"},        {c->v, codes, "cache"},        {c->k_open, open, "cache"}, {c->v_open, open, "cache"},
+      {c->k_scale, scales, "cache"}, {c->v_scale, scales, "cache"}, {pyramid, pyramid ? levels : 0, "pyramid"}};
   for (const auto& x : fresh) {
     for (const auto& y : held) {
       const uintptr_t u = reinterpret_cast<uintptr_t>(x.ptr), w = reinterpret_cast<uintptr_t>(y.ptr);
-      if (u < w + y.bytes && w < u + x.bytes) return fail(PISA_ERR_INVALID_ARG, "%s overlaps the cache", x.name);
+      if (u < w + y.bytes && w < u + x.bytes) return fail(PISA_ERR_INVALID_ARG, "%s overlaps the %s", x.name, y.name);
     }
   }
   a.k_new = k_new;

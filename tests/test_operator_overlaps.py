@@ -58,3 +58,18 @@ def test_outputs_that_overlap_inputs_or_each_other(name):
     refused("q (output) overlaps k", q=Q, qs=packed, qo=Q, qos=packed, k=Q + 8 * row)
     # a row that is read for every head
     refused("q (output) overlaps k", ks=S(0, 0, D), k=QO + 5 * row)
+
+
+def test_appended_rows_that_overlap_scales_or_pyramid():
+    p = pisa.make_problem(1, 4, 2, 256, 1024, 128, 64, 2, 4, 1, "bf16", Ncap=2048)
+    names = [n for n, _ in pisa.QCacheBuffers._fields_]
+    c = pisa.QCacheBuffers(*[(10 + i) << 30 for i in range(len(names))])
+    pyramid, rows = 20 << 30, 2 * 1024 * 128 * 2
+
+    def call(k=K, v=Q, pyr=pyramid):
+        return LIB.pisa_qcache_append(ctypes.byref(p), ctypes.byref(c), k, None, v, None, 0, pyr, None)
+    for what, at, size in (("cache", c.k_scale, 2 * 32 * 4), ("cache", c.v_scale, 2 * 32 * 4),
+                           ("pyramid", pyramid, pisa.pisa_pyramid_bytes(p))):
+        for x in (at, at + size - 16, at - rows + 16):  # the same place, on its last values, its own last values on the first
+            assert call(k=x) == INVALID and f"k_new overlaps the {what}" in pisa.pisa_last_error(), (what, x)
+            assert call(v=x) == INVALID and f"v_new overlaps the {what}" in pisa.pisa_last_error(), (what, x)
