@@ -338,7 +338,9 @@ enum {
  * pos0 + n, or where the call has `positions` (device int32) at
  * positions[b * pos_bstride + n]; pos_bstride = 0 shares one list among the
  * batch.  Positions may be negative.  Angles are computed in 64 bits and
- * reduced before the sine, so far positions lose nothing. */
+ * reduced before the sine: the angle of T turns is off by at most 2^-26 turns for
+ * any position, and by 2^-51 T more (less than a quarter of that up to 2^23
+ * turns; 2^-22 turns at 2^29, position 2^31 with a frequency of 1.6). */
 typedef struct {
   int32_t B, H, Hkv, N, d;
   int32_t rot;

@@ -9,7 +9,10 @@
 //
 // The angle is taken in turns: t * (freq / 2 pi) in 64 bits, its fraction in
 // 32.  Position 2^20 times a frequency of 1 would lose 2^-4 radians in 32 bits;
-// here the fraction is off by at most 2^-26 turns.
+// here the fraction is off by at most 2^-26 turns, and by 2^-51 of all the turns
+// (2^-28 after 2^23 of them) that the roundings in 64 bits leave.  With 32 bits
+// the sines stay 32-bit ones; fp32 results are then 5.6e-8 from the exact ones
+// (relative, 8192 positions from 2^20 on), where 64-bit sines leave 4.2e-8.
 #include "common.h"
 #include "kernels.h"
 
