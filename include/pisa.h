@@ -383,7 +383,13 @@ int pisa_rope_bwd(const pisa_rope* r, const void* d_q_out, const pisa_strides* d
  * is the smallest power of two 2^e, e >= -100, with max|x| <= 448 * 2^e over the
  * block's finite values, so scaling never rounds and code * scale is exact in
  * bf16; the code is x / 2^e rounded to nearest even.  Infinities and NaN become
- * the NaN code.  Half the bytes of a bf16 cache.
+ * the NaN code.  (Values from 0.96875 * 2^128 on round to 2^128 and read as
+ * infinite.)  Half the bytes of a bf16 cache where nothing else is kept:
+ * pisa_select_flat_bsa selects from the pyramid alone, but pisa_select also reads
+ * raw keys for its leaf scores, and a caller that selects with it keeps those
+ * beside the cache (2 bytes a value in bf16: as much again as codes of both).
+ * A call has one N for the whole batch; sequences of other lengths are calls of
+ * their own.
  *
  * With M = ceil(Ncap / C) blocks (Ncap = 0 means N):
  *   k        [B, Hkv, M, C, d]  codes
@@ -421,7 +427,15 @@ size_t pisa_qcache_bytes(const pisa_problem* p);
  * n_old to N, bit for bit as pisa_build_pyramid has it.  k_new and v_new, from
  * their first value to their last, must not overlap the codes, the scales, the raw
  * rows or the pyramid (PISA_ERR_INVALID_ARG).  0 <= n_old <= N; n_old = N does nothing.  No
- * workspace; one launch where a single block changes and no level is new. */
+ * workspace; one launch where a single block changes and no level is new.
+ *
+ * Rows are taken back (drafted tokens that were not accepted) by an append with a
+ * smaller n_old, which replaces everything from that row on.  The call cannot see
+ * which block k_open and v_open belong to: they serve an n_old in the last block
+ * or on any block's border.  Before a draft that may pass a border keep a copy of
+ * both, and put it back to return to the block that the draft began in.  Until
+ * that append the mean and the scale of n_old's block still count the rows that
+ * were taken back. */
 int pisa_qcache_append(const pisa_problem* p, const pisa_qcache* c, const void* k_new, const pisa_strides* k_strides,
                        const void* v_new, const pisa_strides* v_strides, int32_t n_old, float* pyramid,
                        pisa_stream_t stream);

@@ -626,7 +626,9 @@ def grow_qcache(p: Problem, new_cap: int, cache: QCache, pyramid=None):
 
 def qcache_append(p: Problem, cache: QCache, k_new, v_new, n_old: int, pyramid=None, stream=None):
     """Append rows n_old .. N-1 (k_new, v_new: [B, Hkv, N - n_old, d], views with a contiguous last dimension) to
-    the cache, and bring the pyramid with it where one is given."""
+    the cache, and bring the pyramid with it where one is given.  A smaller n_old than before takes rows back: in the last
+    block or on a block's border as it is; after a draft that passed a border only with cache.k_open and cache.v_open put
+    back as they were before it."""
     cache.check(p, appending=True)
     shape, dt, dev = (p.B, p.Hkv, p.N - n_old, p.d), _TORCH[p.dtype], cache.device
     ks, vs = _strided(k_new, "k_new", dt, shape, dev), _strided(v_new, "v_new", dt, shape, dev)
