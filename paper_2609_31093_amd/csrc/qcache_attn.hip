@@ -509,7 +509,7 @@ __global__ __launch_bounds__(64) void qcache_merge_kernel(QAttnArgs a) {
 // in units of the values' scale (so at most 448) and rounded to fp16 (relative
 // 2^-11; its largest logit and sum stay in fp32, apart: the logarithm of the sum
 // would be lost in a large logit), and qcache_combine_kernel merges a row's K.
-//   part_o [BH][rows][K][G][D], within each 32 dimensions in the order
+//   part_o [KV heads of the pass][its rows][K][G][D], within each 32 dimensions in the order
 //   [grp][dimension tile 0..1][4], so that a lane stores 16 bytes at a time
 constexpr int kBlockTiles = 8;  // tiles of a wavefront, at most
 
@@ -518,8 +518,9 @@ struct QBlockArgs {
   const int32_t *offs, *toffs, *pairs;  // launch_cluster
   int64_t ncl;
   uint16_t* part_o;
-  float2* part_ml;  // [BH][rows][K][G]: largest logit, sum of weights
-  int nrows;  // rows of this launch, from a.row0 on
+  float2* part_ml;  // [KV heads][rows][K][G]: largest logit, sum of weights
+  int nrows;  // rows of this pass, from a.row0 on
+  int bh0;    // its first KV head of [0, BH)
   int chunk;  // pairs of one block per workgroup, at most
 };
 
@@ -535,7 +536,8 @@ __global__ __launch_bounds__(64, WHOLE ? (D == 128 ? 3 : 4) : 2) void qcache_blo
   int64_t cl;
   int beg, end;
   if (!cluster_chunk(p.offs, p.toffs, p.ncl, blockIdx.x, p.chunk, cl, beg, end)) return;
-  const int bh = static_cast<int>(cl / a.M1), blk = static_cast<int>(cl - static_cast<int64_t>(bh) * a.M1);
+  const int pbh = static_cast<int>(cl / a.M1), blk = static_cast<int>(cl - static_cast<int64_t>(pbh) * a.M1);
+  const int bh = p.bh0 + pbh;
   const int b = bh / a.Hkv, h = bh - b * a.Hkv;
   const int col = threadIdx.x & 15, grp = threadIdx.x >> 4;
   const int ppt = 16 / a.G;                // pairs of a tile
@@ -584,7 +586,7 @@ __global__ __launch_bounds__(64, WHOLE ? (D == 128 ? 3 : 4) : 2) void qcache_blo
     for (int i = 0; i + 1 < kBlockTiles; ++i) words[i] = words[i + 1];
     if (j + 1 < ntile) gather(words[0]);
     uint16_t* dst = nullptr;
-    const int64_t pidx = ((static_cast<int64_t>(bh) * p.nrows + rr) * a.K + slot) * a.G + hh;
+    const int64_t pidx = ((static_cast<int64_t>(pbh) * p.nrows + rr) * a.K + slot) * a.G + hh;
     if (live) dst = p.part_o + pidx * D + grp * 8;
     auto store = [&](int j, f32x4a x, f32x4a y, float inv) {  // dimension tiles 2j and 2j + 1
       uint4 w;
@@ -652,11 +654,11 @@ __global__ __launch_bounds__(256) void qcache_combine_kernel(QBlockArgs p) {
   const int rr = static_cast<int>(e / a.G), hh = static_cast<int>(e - static_cast<int64_t>(rr) * a.G);
   if (rr >= p.nrows) return;
   const int grp = lane >> 4, sub = lane & 15;
-  const int bh = blockIdx.y, b = bh / a.Hkv;
+  const int bh = p.bh0 + static_cast<int>(blockIdx.y), b = bh / a.Hkv;
   const int hq = (bh - b * a.Hkv) * a.G + hh;
   const int row = a.row0 + rr;
   const int32_t* sel = a.idx + (static_cast<int64_t>(bh) * a.Nq + row) * a.K;
-  const int64_t base = (static_cast<int64_t>(bh) * p.nrows + rr) * a.K;
+  const int64_t base = (static_cast<int64_t>(blockIdx.y) * p.nrows + rr) * a.K;
   float m = -INFINITY, l = 0.f, o[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = 0.f;
@@ -797,30 +799,50 @@ hipError_t launch_nw(const Shape& s, const QAttnArgs& a, int nw, hipStream_t st)
 
 static size_t al256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
+// Partials of one pass take about 1 GB.  A pass takes all rows of some KV heads,
+// so that their blocks are grouped once, and only where those of one KV head are
+// more than that does it take a part of them.  (Passes over a part of the rows of
+// every KV head group all blocks each time: 2048 rows of 32 x 8 KV heads over
+// 131072 keys took 26.5 ms that way, 7.4 this way.)
+constexpr size_t kPartialBytes = size_t(1) << 30;
+struct BlockPass {
+  int heads, rows;       // of a pass, at most
+  int hpasses, rpasses;  // passes over KV heads, and over the rows of each
+};
+static BlockPass block_pass(const Shape& s) {
+  const size_t row = static_cast<size_t>(s.K) * s.G * (s.D * 2 + 4);  // a KV head's row
+  const int most = static_cast<int>(std::max<size_t>(kPartialBytes / row, 1));
+  auto div_up = [](int x, int y) { return (x + y - 1) / y; };
+  BlockPass b{};
+  b.rpasses = div_up(s.Nq, most);
+  b.rows = div_up(s.Nq, b.rpasses);
+  b.hpasses = div_up(s.BH(), std::max(1, most / s.Nq));
+  b.heads = div_up(s.BH(), b.hpasses);
+  return b;
+}
+
 // Does grouping the rows by block pay?  A row alone reads its K blocks, of 2 C D
 // bytes, at about 10 TB/s over all; grouped, a block is read once for many rows,
-// but each (row, slot) writes and reads back a partial of 2 D bytes a head (0.33
-// ns per KB and 64 keys of the block), and the grouping costs 32 us and 2.5 ns per
-// block of every KV head.  Measured, alone and grouped (us): 128-wide heads, 16
-// blocks of 64 keys, 32768 keys, 4 heads to a KV head: 2048 rows x KV heads 63 and
-// 61, 4096 112 and 75, 16384 374 and 226; 1 head: 2048 60 and 52, 16384 367 and
-// 84; 8 heads: 8192 204 and 212; 16 heads of 64, 8 blocks: 8192 64 and 140; over
-// 524288 keys, 4 heads: 16384 457 and 328.  Over 135 shapes of 512 to 16384 rows
-// the mean time is 0.5% above that of the faster choice for each.
+// but each (row, slot) writes and reads back a partial of 2 D bytes a head (0.25
+// ns per KB and 64 keys of the block), a pass costs 36 us, and the grouping 2.5 ns
+// per block of every KV head, again for each part of its rows.  Measured, alone
+// and grouped (us): 128-wide heads, 16 blocks of 64 keys, 32768 keys, 4 heads to a
+// KV head: 2048 rows x KV heads 62 and 56, 4096 109 and 69, 16384 373 and 203; 1
+// head: 2048 58 and 51, 16384 367 and 78; 8 heads: 2048 63 and 67, 8192 207 and
+// 187; 16 heads of 64, 8 blocks: 8192 61 and 131; over 524288 keys, 4 heads: 4096
+// 135 and 194, 16384 481 and 317.  Several passes, 4 heads, 131072 keys: 2048 rows
+// of 32 x 8 KV heads (9 passes) 21105 and 7436, 512 of 64 x 8 (5) 11620 and 7746,
+// 32768 of 8 (8) 6066 and 3221.  Over 177 shapes of 256 to 524288 rows the mean
+// time is 0.3% above that of the faster choice for each.
 static bool use_blocks(const Shape& s, const Geo& geo) {
   if (!s.bf16 || geo.M[1] > 16384) return false;  // the grouping's LDS histogram
   if (static_cast<int64_t>(s.BH()) * geo.M[1] > (1 << 23)) return false;  // a workgroup per block fits one launch
   const double rows = static_cast<double>(s.BH()) * s.Nq;
-  const double saved = rows * s.K * s.D / 1024 * (0.2 * s.C - 1.32 * s.G * std::max(1.0, s.C / 64.0));
-  return saved >= 32000 + 2.5 * s.BH() * geo.M[1];
+  const double saved = rows * s.K * s.D / 1024 * (0.2 * s.C - s.G * std::max(1.0, s.C / 64.0));
+  const BlockPass b = block_pass(s);
+  return saved >= b.rpasses * (36000.0 * b.hpasses + 2.5 * s.BH() * geo.M[1]);
 }
 
-// Rows per pass: their partials take about 1 GB.
-constexpr size_t kPartialBytes = size_t(1) << 30;
-static int block_rows(const Shape& s) {
-  const size_t per_row = static_cast<size_t>(s.BH()) * s.K * s.G * (s.D * 2 + 4);
-  return static_cast<int>(std::min<size_t>(s.Nq, std::max<size_t>(kPartialBytes / per_row, 1)));
-}
 // Rows per workgroup of the grouping: about 4096 pairs (262144 pairs on 4 KV heads:
 // 28 us for the grouping, 47 with 1024 rows).
 static int group_rows(const Shape& s) { return std::max(64, 4096 / s.K); }
@@ -832,54 +854,59 @@ struct BlockWs {
   size_t part_o, part_ml, cl, total;
 };
 static BlockWs block_layout(const Shape& s, const Geo& geo) {
-  const int rows = block_rows(s);
-  const size_t np = static_cast<size_t>(s.BH()) * rows * s.K;
+  const BlockPass b = block_pass(s);
+  const size_t np = static_cast<size_t>(b.heads) * b.rows * s.K;
   BlockWs w{};
   w.part_ml = al256(np * s.G * s.D * 2);
   w.cl = w.part_ml + al256(np * s.G * sizeof(float2));
-  w.total = w.cl + al256(cluster_ws(s.BH(), geo.M[1], static_cast<int64_t>(np), rows, group_rows(s)));
+  w.total = w.cl + al256(cluster_ws(b.heads, geo.M[1], static_cast<int64_t>(np), b.rows, group_rows(s)));
   return w;
 }
 
 template <int D>
 static hipError_t launch_blocks(const Shape& s, const Geo& geo, const QAttnArgs& a, char* base, int ku, hipStream_t st) {
   const BlockWs w = block_layout(s, geo);
-  const int rows = block_rows(s);
+  const BlockPass bp = block_pass(s);
   QBlockArgs p{};
   p.a = a;
   p.part_o = reinterpret_cast<uint16_t*>(base + w.part_o);
   p.part_ml = reinterpret_cast<float2*>(base + w.part_ml);
-  for (int row0 = 0; row0 < s.Nq; row0 += rows) {
-    p.a.row0 = row0;
-    p.nrows = std::min(rows, s.Nq - row0);
-    ClusterArgs ca{a.idx, nullptr, s.K, s.Nq, s.N, s.C, s.K, s.causal, geo.M[1], kClusterAttn, row0, p.nrows, s.g};
-    ca.chunk_rows = group_rows(s);
-    p.chunk = pair_chunk(s);
-    ClusterOut co{};
-    hipError_t e = launch_cluster(ca, s.BH(), base + w.cl, &co, st, p.chunk);
-    if (e != hipSuccess) return e;
-    p.offs = co.offs;
-    p.toffs = co.toffs;
-    p.pairs = co.pairs;
-    p.ncl = co.ncl;
-    {
-      ProfScope ps("qcache_block", st);
-      const unsigned grid = static_cast<unsigned>(
-          cluster_max_chunks(s.BH(), geo.M[1], static_cast<int64_t>(s.BH()) * p.nrows * s.K, p.chunk));
-      if (s.C == 64)
-        qcache_block_kernel<D, 64, true><<<grid, 64, 0, st>>>(p);
-      else if (s.C == 32)
-        qcache_block_kernel<D, 32, true><<<grid, 64, 0, st>>>(p);
-      else if (ku == 64)
-        qcache_block_kernel<D, 64, false><<<grid, 64, 0, st>>>(p);
-      else
-        qcache_block_kernel<D, 32, false><<<grid, 64, 0, st>>>(p);
+  p.chunk = pair_chunk(s);
+  for (int bh0 = 0; bh0 < s.BH(); bh0 += bp.heads) {
+    const int heads = std::min(bp.heads, s.BH() - bh0);
+    p.bh0 = bh0;
+    for (int row0 = 0; row0 < s.Nq; row0 += bp.rows) {
+      p.a.row0 = row0;
+      p.nrows = std::min(bp.rows, s.Nq - row0);
+      ClusterArgs ca{a.idx + static_cast<int64_t>(bh0) * s.Nq * s.K, nullptr, s.K, s.Nq, s.N, s.C, s.K, s.causal, geo.M[1],
+                     kClusterAttn, row0, p.nrows, s.g};
+      ca.chunk_rows = group_rows(s);
+      ClusterOut co{};
+      hipError_t e = launch_cluster(ca, heads, base + w.cl, &co, st, p.chunk);
+      if (e != hipSuccess) return e;
+      p.offs = co.offs;
+      p.toffs = co.toffs;
+      p.pairs = co.pairs;
+      p.ncl = co.ncl;
+      {
+        ProfScope ps("qcache_block", st);
+        const unsigned grid = static_cast<unsigned>(
+            cluster_max_chunks(heads, geo.M[1], static_cast<int64_t>(heads) * p.nrows * s.K, p.chunk));
+        if (s.C == 64)
+          qcache_block_kernel<D, 64, true><<<grid, 64, 0, st>>>(p);
+        else if (s.C == 32)
+          qcache_block_kernel<D, 32, true><<<grid, 64, 0, st>>>(p);
+        else if (ku == 64)
+          qcache_block_kernel<D, 64, false><<<grid, 64, 0, st>>>(p);
+        else
+          qcache_block_kernel<D, 32, false><<<grid, 64, 0, st>>>(p);
+      }
+      {
+        ProfScope ps("qcache_combine", st);
+        qcache_combine_kernel<D><<<dim3(static_cast<unsigned>((static_cast<int64_t>(p.nrows) * s.G + 3) / 4), heads), 256, 0, st>>>(p);
+      }
+      if ((e = hipGetLastError()) != hipSuccess) return e;
     }
-    {
-      ProfScope ps("qcache_combine", st);
-      qcache_combine_kernel<D><<<dim3(static_cast<unsigned>((static_cast<int64_t>(p.nrows) * s.G + 3) / 4), s.BH()), 256, 0, st>>>(p);
-    }
-    if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   return hipSuccess;
 }
