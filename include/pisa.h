@@ -445,7 +445,8 @@ int pisa_qcache_append(const pisa_problem* p, const pisa_qcache* c, const void* 
  * meet the values (and with many rows each block's result is, before the blocks
  * of a row are merged), an fp32 problem's are not.  Entries of block_idx as
  * there; a row with no visible token gets o = 0 and lse = -inf; tokens that the
- * causal mask or N hides are not used, whatever their codes.  o and lse
+ * causal mask or N hides are not used, whatever their codes.  Logits and values may
+ * be as large as fp32 holds the products q . k and the type o.  o and lse
  * (nullable) as there. */
 size_t pisa_qcache_attn_workspace_bytes(const pisa_problem* p);
 int pisa_qcache_attn_fwd(const pisa_problem* p, const pisa_qcache* c, const void* q, const int32_t* block_idx, void* o,

@@ -524,11 +524,12 @@ struct QBlockArgs {
   int chunk;  // pairs of one block per workgroup, at most
 };
 
-// WHOLE: a unit is a block, whose codes stay in registers (152 of them, three
+// WHOLE: a unit is a block, whose codes stay in registers (158 in all, three
 // wavefronts on a SIMD; with the operands there instead, 256 and two, 4096 rows of
-// 16 heads on 4 took 157 us in this kernel against 126); otherwise its units are
-// read again, from the cache, for every tile.  What bounds it there (119 us) is the
-// partials' 268 MB out and the queries' 268 MB in, 4.5 TB/s.
+// 16 heads on 4 took 157 us in this kernel against 126 at that time); otherwise its
+// units are read again, from the cache, for every tile.  What bounds it there (120
+// us) is the partials' 268 MB out and the queries' 268 MB in, 4.5 TB/s; the vector
+// units are busy 45% of that time and the matrix cores 12%.
 template <int D, int KU, bool WHOLE>
 __global__ __launch_bounds__(64, WHOLE ? (D == 128 ? 3 : 4) : 2) void qcache_block_kernel(QBlockArgs p) {
   constexpr int KS = D / 32, DT = D / 16;
@@ -643,7 +644,9 @@ __global__ __launch_bounds__(64, WHOLE ? (D == 128 ? 3 : 4) : 2) void qcache_blo
 }
 
 // One wavefront per (row, head): 16 lanes hold a partial (8 values each for
-// d = 128), so four slots at a time.
+// d = 128), so four slots at a time, and SPL rounds of them asked for before the
+// first is used (4096 rows of 16 heads, 16 blocks: 64 us, 277 MB; with each
+// round's values converted as they came, and so waited for, 89).
 template <int D>
 __global__ __launch_bounds__(256) void qcache_combine_kernel(QBlockArgs p) {
   constexpr int E = D / 16;
@@ -844,7 +847,7 @@ static bool use_blocks(const Shape& s, const Geo& geo) {
 }
 
 // Rows per workgroup of the grouping: about 4096 pairs (262144 pairs on 4 KV heads:
-// 28 us for the grouping, 47 with 1024 rows).
+// 21 us for the grouping, 35 with 1024 rows).
 static int group_rows(const Shape& s) { return std::max(64, 4096 / s.K); }
 // Pairs of one block per wavefront.  Workgroups of one (4096 rows of 8 heads on 8,
 // 16 blocks of 131072 keys: 103 us in this kernel; 4 wavefronts of 4 tiles 150, 2 of
