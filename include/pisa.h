@@ -426,7 +426,7 @@ size_t pisa_qcache_bytes(const pisa_problem* p);
  * the mean pyramid of the raw keys for the same fanout and Ncap, brought from
  * n_old to N, bit for bit as pisa_build_pyramid has it.  k_new and v_new, from
  * their first value to their last, must not overlap the codes, the scales, the raw
- * rows or the pyramid (PISA_ERR_INVALID_ARG).  0 <= n_old <= N; n_old = N does nothing.  No
+ * rows or the pyramid, nor those each other (PISA_ERR_INVALID_ARG).  0 <= n_old <= N; n_old = N does nothing.  No
  * workspace; one launch where a single block changes and no level is new.
  *
  * Rows are taken back (drafted tokens that were not accepted) by an append with a

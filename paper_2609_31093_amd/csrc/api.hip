@@ -8,6 +8,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <iterator>
 #include <mutex>
 
 #include "../../include/pisa.h"
@@ -851,11 +852,17 @@ int pisa_qcache_append(const pisa_problem* p, const pisa_qcache* c, const void* 
   const struct { const void* ptr; size_t bytes; const char* name; } held[] = {
       {c->k, codes, "cache"},        {c->v, codes, "cache"},        {c->k_open, open, "cache"}, {c->v_open, open, "cache"},
       {c->k_scale, scales, "cache"}, {c->v_scale, scales, "cache"}, {pyramid, pyramid ? levels : 0, "pyramid"}};
+  auto meet = [](const auto& x, const auto& y) {
+    const uintptr_t u = reinterpret_cast<uintptr_t>(x.ptr), w = reinterpret_cast<uintptr_t>(y.ptr);
+    return u < w + y.bytes && w < u + x.bytes;
+  };
   for (const auto& x : fresh) {
-    for (const auto& y : held) {
-      const uintptr_t u = reinterpret_cast<uintptr_t>(x.ptr), w = reinterpret_cast<uintptr_t>(y.ptr);
-      if (u < w + y.bytes && w < u + x.bytes) return fail(PISA_ERR_INVALID_ARG, "%s overlaps the %s", x.name, y.name);
-    }
+    for (const auto& y : held)
+      if (meet(x, y)) return fail(PISA_ERR_INVALID_ARG, "%s overlaps the %s", x.name, y.name);
+  }
+  for (size_t i = 1; i < std::size(held); ++i) {
+    for (size_t j = 0; j < i; ++j)
+      if (meet(held[i], held[j])) return fail(PISA_ERR_INVALID_ARG, "buffers of the cache or the pyramid overlap");
   }
   a.k_new = k_new;
   a.v_new = v_new;

@@ -73,3 +73,20 @@ def test_appended_rows_that_overlap_scales_or_pyramid():
         for x in (at, at + size - 16, at - rows + 16):  # the same place, on its last values, its own last values on the first
             assert call(k=x) == INVALID and f"k_new overlaps the {what}" in pisa.pisa_last_error(), (what, x)
             assert call(v=x) == INVALID and f"v_new overlaps the {what}" in pisa.pisa_last_error(), (what, x)
+
+
+def test_cache_buffers_that_overlap_each_other():
+    p = pisa.make_problem(1, 4, 2, 256, 1024, 64, 64, 2, 4, 1, "bf16", Ncap=2048)  # codes of keys and values: same shape
+    names = [n for n, _ in pisa.QCacheBuffers._fields_]
+    at = {n: (10 + i) << 30 for i, n in enumerate([*names, "pyramid"])}
+    codes, raw = 2 * 32 * 64 * 64, 2 * 64 * 64 * 2
+    size = dict(k=codes, v=codes, k_scale=2 * 32 * 4, v_scale=2 * 32 * 4, k_open=raw, v_open=raw, pyramid=pisa.pisa_pyramid_bytes(p))
+    for x in at:
+        for y in at:
+            if x == y:
+                continue
+            for off in (0, size[y] - 16):
+                given = {**at, x: at[y] + off}
+                c = pisa.QCacheBuffers(*[given[n] for n in names])
+                st = LIB.pisa_qcache_append(ctypes.byref(p), ctypes.byref(c), K, None, Q, None, 0, given["pyramid"], None)
+                assert st == INVALID and "overlap" in pisa.pisa_last_error(), (x, y, off)
