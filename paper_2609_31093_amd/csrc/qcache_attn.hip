@@ -333,10 +333,14 @@ struct Softmax {
   }
 };
 
-// Natural log of a row's sum of exponentials: largest logit, sum of weights.
+// Natural log of a row's sum of exponentials: largest logit, sum of weights.  The
+// headroom leaves the sum before its logarithm, which is then that of a number from
+// 1 on and keeps its bits.
 template <int NT>
 __device__ __forceinline__ float row_lse(float ref, float sum, float qscale2) {
-  return sum == 0.f ? -INFINITY : fmaf(ref, qscale2, fast_log2(sum) - kHeadroom<NT>) * kLn2;
+  constexpr float unit = NT == 1 ? 0x1p-14f : 1.f;
+  static_assert(unit * (1 << static_cast<int>(kHeadroom<NT>)) == 1.f);
+  return sum == 0.f ? -INFINITY : fmaf(ref, qscale2, fast_log2(sum * unit)) * kLn2;
 }
 
 // One workgroup of NW wavefronts per (row, KV head, split of its key units).
@@ -669,8 +673,8 @@ __global__ __launch_bounds__(256) void qcache_combine_kernel(QBlockArgs p) {
     int blk[SPL];
 #pragma unroll
     for (int i = 0; i < SPL; ++i) {
-      const int b = s0 + 4 * i < a.K ? sel[s0 + 4 * i] : -1;
-      blk[i] = static_cast<uint32_t>(b) < static_cast<uint32_t>(a.M1) ? b : -1;  // padding left no partial
+      const int x = s0 + 4 * i < a.K ? sel[s0 + 4 * i] : -1;
+      blk[i] = static_cast<uint32_t>(x) < static_cast<uint32_t>(a.M1) ? x : -1;  // padding left no partial
     }
     float2 ml[SPL];
     float sc[SPL];
