@@ -18,7 +18,10 @@
 // exact one as rounding it does), in which value codes are exact too; the values'
 // scale is applied to the product in fp32.  Those weights are taken up to 2^14
 // (kHeadroom), so that ones of 2^-28 of the largest are still normal numbers.
-// Sums of weights are not rounded.
+// Sums of weights are not rounded.  (A second fp16 term for what the first leaves
+// of a weight brings a token's result over 131072 to what rounding it to bf16
+// alone leaves, 1.666e-3 from the exact one instead of 1.673e-3, and took 7.80 us
+// instead of 7.57, 8 drafted rows over 524288 10.2 instead of 9.65.)
 //
 // The running maximum is that of the products S themselves, and the softmax's
 // scale (with log2 e) multiplies differences from it: a large logit that is
