@@ -597,7 +597,7 @@ class QCache:
 
 
 def make_qcache(p: Problem, device=None):
-    """An empty cache for problem p (reserving Ncap tokens)."""
+    """An empty cache for problem p (reserving Ncap tokens), cleared on the current stream."""
     M, dev = pisa_qcache_blocks(p), torch.device("cuda", torch.cuda.current_device()) if device is None else device
     new = dict(device=dev)
     k = torch.zeros((p.B, p.Hkv, M, p.C, p.d), dtype=torch.uint8, **new)
