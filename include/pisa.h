@@ -376,6 +376,44 @@ int pisa_rope_bwd(const pisa_rope* r, const void* d_q_out, const pisa_strides* d
                   const pisa_strides* d_k_out_strides, const int32_t* positions, void* d_q,
                   const pisa_strides* d_q_strides, void* d_k, const pisa_strides* d_k_strides, pisa_stream_t stream);
 
+/* ---- Norms of queries and keys with their positions ------------------------
+ *
+ * Each head of a row is divided by its root mean square and multiplied by learned
+ * weights before it is turned:
+ *   y = R (x / sqrt(mean(x^2) + eps) * (w + offset))
+ * with R the rotation of pisa_rope_fwd (dimensions from `rot` on are normed but not
+ * turned).  Sums and products in fp32, rounded once; the sum of a head's squares is
+ * held in fp32, so a head whose mean square is past its range comes out as 0. */
+typedef struct {
+  const void* q_weight; /* [d] in weight_dtype, one for every head; NULL: all 1, without offset */
+  const void* k_weight;
+  int32_t weight_dtype; /* pisa_dtype of both           */
+  int32_t reserved;     /* 0                            */
+  double eps;           /* in [1e-30, 1e30]             */
+  double offset;        /* 1 for weights stored around 0 */
+} pisa_qk_norm;
+
+/* Norms and turns q and k in one launch; tensors, sides and outputs as in
+ * pisa_rope_fwd. */
+int pisa_norm_rope_fwd(const pisa_rope* r, const pisa_qk_norm* m, const void* q, const pisa_strides* q_strides, const void* k,
+                       const pisa_strides* k_strides, const int32_t* positions, void* q_out,
+                       const pisa_strides* q_out_strides, void* k_out, const pisa_strides* k_out_strides,
+                       pisa_stream_t stream);
+
+/* Gradients of pisa_norm_rope_fwd from its inputs q, k and the gradients of its
+ * outputs: d_q, d_k, and the weights' d_q_weight, d_k_weight (float32 [d], summed
+ * over every row and head in a fixed order; nullable, and NULL for a side that is
+ * left out).  A side has its input, its output's gradient and its gradient, or none
+ * of them.  d_q may be d_q_out and d_k d_k_out (same pointer and strides); nothing
+ * that is written overlaps anything else (PISA_ERR_INVALID_ARG).  Workspace:
+ * pisa_norm_rope_bwd_workspace_bytes(r), needed where a weight's gradient is wanted. */
+size_t pisa_norm_rope_bwd_workspace_bytes(const pisa_rope* r);
+int pisa_norm_rope_bwd(const pisa_rope* r, const pisa_qk_norm* m, const void* q, const pisa_strides* q_strides, const void* k,
+                       const pisa_strides* k_strides, const void* d_q_out, const pisa_strides* d_q_out_strides,
+                       const void* d_k_out, const pisa_strides* d_k_out_strides, const int32_t* positions, void* d_q,
+                       const pisa_strides* d_q_strides, void* d_k, const pisa_strides* d_k_strides, float* d_q_weight,
+                       float* d_k_weight, void* ws, size_t ws_bytes, pisa_stream_t stream);
+
 /* ---- 8-bit key/value cache --------------------------------------------------
  *
  * Keys and values in e4m3 (4 exponent, 3 mantissa bits, largest 448), one scale
@@ -451,6 +489,74 @@ int pisa_qcache_append(const pisa_problem* p, const pisa_qcache* c, const void* 
 size_t pisa_qcache_attn_workspace_bytes(const pisa_problem* p);
 int pisa_qcache_attn_fwd(const pisa_problem* p, const pisa_qcache* c, const void* q, const int32_t* block_idx, void* o,
                          float* lse, void* ws, size_t ws_bytes, pisa_stream_t stream);
+
+/* ---- Drafted tokens ---------------------------------------------------------
+ *
+ * T drafted tokens per sequence, a tree (or several) that continues its n cached
+ * ones.  Their keys and values stay out of the cache until they are accepted, so
+ * there is nothing to take back: rows k_new, v_new [B, Hkv, T, d] in the problem
+ * dtype (strides as in pisa_strides).  With a problem of Nq = T, N = n + T (and room
+ * for them, Ncap >= N):
+ *   pisa_draft_layout       masks, and positions for pisa_rope_fwd, from the parents
+ *   pisa_select, pisa_select_flat_bsa
+ *                           as for T rows after n: those blocks that hold drafted
+ *                           rows are forced, so that neither call reads them (T <= C)
+ *   pisa_draft_attn_fwd, pisa_qcache_draft_attn_fwd
+ *   pisa_cache_append_rows, pisa_qcache_append_rows
+ *                           the accepted rows, with a problem of N = n + accepted */
+#define PISA_DRAFT_MAX 1024
+
+/* parents: device int32 [B, T], the drafted token that each one follows; -1 (or T and
+ * more): the last cached one; below -1: none, a token that pads the tree.  Parents
+ * may come behind their children.
+ * mask: uint64 [B, T, W], W = ceil(T / 64): bit j % 64 of word j / 64 of row i is set
+ * where j is i or an ancestor of i (no bit for a token that pads).
+ * positions: nullable int32 [B, T], n + the number of i's ancestors (n for one that
+ * pads).  A token whose ancestors run in a circle has those of the circle, and a
+ * position of n + T - 1.  B <= 65535, 1 <= T <= PISA_DRAFT_MAX, n + T < 2^31. */
+int pisa_draft_layout(int32_t B, int32_t T, const int32_t* parents, int32_t n, uint64_t* mask, int32_t* positions,
+                      pisa_stream_t stream);
+
+/* Attention of the Nq drafted rows: for every row and query head, softmax over the
+ * cached tokens (the first N - Nq rows of k, v) of its KV head's selected blocks and
+ * over the drafted rows of its mask, applied to their values.  The cached tokens all
+ * come before the drafted ones, so p->causal is not read.  block_idx as in
+ * pisa_sparse_attn_fwd: entries outside [0, ceil((N - Nq) / C)), among them blocks that
+ * hold drafted rows alone, contribute nothing; distinct entries in any order.  mask:
+ * [B, Nq, W] words of pisa_draft_layout, or any others (bits from Nq on are not read);
+ * mask_bstride words lie between two sequences, 0 shares one mask among the batch.
+ * Rows that nothing selects or masks in are hidden whatever their values.  Writes o
+ * [B, H, Nq, d] and lse (nullable); a row that sees nothing gets o = 0 and lse = -inf.
+ * Sums in fp32, weights rounded to bf16 (fp16 for 8-bit values, not at all in fp32
+ * problems) before they meet the values.  Nq <= PISA_DRAFT_MAX; N = Nq is an empty
+ * cache.  o, lse and the workspace must not overlap anything else (PISA_ERR_INVALID_ARG). */
+size_t pisa_draft_attn_workspace_bytes(const pisa_problem* p);
+int pisa_draft_attn_fwd(const pisa_problem* p, const void* q, const void* k, const void* v, const int32_t* block_idx,
+                        const void* k_new, const pisa_strides* k_strides, const void* v_new, const pisa_strides* v_strides,
+                        const uint64_t* mask, int64_t mask_bstride, void* o, float* lse, void* ws, size_t ws_bytes,
+                        pisa_stream_t stream);
+
+/* The same over the 8-bit cache, its keys and values being code * scale. */
+size_t pisa_qcache_draft_attn_workspace_bytes(const pisa_problem* p);
+int pisa_qcache_draft_attn_fwd(const pisa_problem* p, const pisa_qcache* c, const void* q, const int32_t* block_idx,
+                               const void* k_new, const pisa_strides* k_strides, const void* v_new,
+                               const pisa_strides* v_strides, const uint64_t* mask, int64_t mask_bstride, void* o, float* lse,
+                               void* ws, size_t ws_bytes, pisa_stream_t stream);
+
+/* Appends accepted rows to a cache k, v [B, Hkv, Ncap, d] of n_old rows: row n_old + i
+ * of sequence b becomes row rows[b * (N - n_old) + i] of k_new, v_new [B, Hkv, n_rows, d],
+ * for i < N - n_old (any rows, in any order; an entry outside [0, n_rows) is read as the
+ * nearest one inside).  rows NULL: the first N - n_old of them, so that the call also
+ * writes a prompt.  pyramid (nullable): as in pisa_qcache_append.  k_new, v_new and rows
+ * must not overlap the cache or the pyramid (PISA_ERR_INVALID_ARG). */
+int pisa_cache_append_rows(const pisa_problem* p, void* k, void* v, const void* k_new, const pisa_strides* k_strides,
+                           const void* v_new, const pisa_strides* v_strides, const int32_t* rows, int32_t n_rows,
+                           int32_t n_old, float* pyramid, pisa_stream_t stream);
+
+/* pisa_qcache_append of such rows: the same cache as an append of them in order. */
+int pisa_qcache_append_rows(const pisa_problem* p, const pisa_qcache* c, const void* k_new, const pisa_strides* k_strides,
+                            const void* v_new, const pisa_strides* v_strides, const int32_t* rows, int32_t n_rows,
+                            int32_t n_old, float* pyramid, pisa_stream_t stream);
 
 /* Per-kernel timing for benchmarks (not needed for computing anything).
  * pisa_profile_enable(1) makes every later call bracket each kernel it

@@ -445,6 +445,49 @@ bool share(const Placed& x, const Placed& y, int d, int64_t esz) {
   return rows_meet(dim, 0, at / esz, d, false, &steps);
 }
 
+// What a rotation's kernels take from its descriptor; sides are filled in already.
+void fill_rope(const pisa_rope* r, const int32_t* positions, float sign, pisa::RopeArgs* a) {
+  a->positions = positions;
+  a->pos_bstride = r->pos_bstride;
+  a->B = r->B;
+  a->H = a->q.in ? r->H : 0;
+  a->HH = a->H + (a->k.in ? r->Hkv : 0);
+  a->N = r->N;
+  a->d = r->d;
+  a->rot = r->rot;
+  a->pos0 = r->pos0;
+  a->amplitude = static_cast<float>(r->amplitude);
+  a->sign = sign;
+  for (int i = 0; i < r->rot / 2; ++i) a->turn[i] = r->freq[i] / 6.283185307179586476925286766559;
+}
+
+// Rows are read and written in one launch, in any order: an output (side i's) meets
+// no input, but its own in place, and no other output.
+int check_rope_overlaps(const pisa_rope* r, const pisa::RopeSide (&side)[2], const char* const (&names)[2]) {
+  const int heads[2] = {r->H, r->Hkv};
+  const int64_t esz = r->dtype == PISA_DTYPE_BF16 ? 2 : 4;
+  Placed in[2], out[2];
+  for (int i = 0; i < 2; ++i) {
+    in[i] = Placed{side[i].in, pisa_strides{side[i].ib, side[i].ih, side[i].in_n}, r->B, heads[i], r->N};
+    out[i] = Placed{side[i].out, pisa_strides{side[i].ob, side[i].oh, side[i].on}, r->B, heads[i], r->N};
+  }
+  for (int i = 0; i < 2; ++i) {
+    if (!out[i].ptr) continue;
+    for (int j = 0; j < 2; ++j) {
+      if (in[j].ptr && !(i == j && in[j].ptr == out[i].ptr) && share(out[i], in[j], r->d, esz))
+        return fail(PISA_ERR_INVALID_ARG, "%s (output) overlaps %s", names[i], names[j]);
+    }
+  }
+  if (out[0].ptr && out[1].ptr && share(out[0], out[1], r->d, esz))
+    return fail(PISA_ERR_INVALID_ARG, "%s (output) overlaps %s (output)", names[0], names[1]);
+  return PISA_OK;
+}
+
+int check_positions(const int32_t* positions) {
+  if (reinterpret_cast<uintptr_t>(positions) & 3u) return fail(PISA_ERR_INVALID_ARG, "positions is not 4-byte aligned");
+  return PISA_OK;
+}
+
 int run_rope(const pisa_rope* r, const void* q, const pisa_strides* qs, const void* k, const pisa_strides* ks,
              const int32_t* positions, void* qo, const pisa_strides* qos, void* ko, const pisa_strides* kos, float sign,
              pisa_stream_t stream, const char* who) {
@@ -453,39 +496,64 @@ int run_rope(const pisa_rope* r, const void* q, const pisa_strides* qs, const vo
   PISA_TRY(check_rope_side(r, "q", r->H, q, qs, qo, qos, &a.q));
   PISA_TRY(check_rope_side(r, "k", r->Hkv, k, ks, ko, kos, &a.k));
   if (!q && !k) return fail(PISA_ERR_INVALID_ARG, "neither q nor k given");
-  if (positions && (reinterpret_cast<uintptr_t>(positions) & 3u))
-    return fail(PISA_ERR_INVALID_ARG, "positions is not 4-byte aligned");
-  // rows are read and written in one launch, in any order
-  auto placed = [&](const void* ptr, int64_t b, int64_t h, int64_t n, int heads) {
-    return Placed{ptr, pisa_strides{b, h, n}, r->B, heads, r->N};
-  };
-  const Placed in[2] = {placed(a.q.in, a.q.ib, a.q.ih, a.q.in_n, r->H), placed(a.k.in, a.k.ib, a.k.ih, a.k.in_n, r->Hkv)};
-  const Placed out[2] = {placed(a.q.out, a.q.ob, a.q.oh, a.q.on, r->H), placed(a.k.out, a.k.ob, a.k.oh, a.k.on, r->Hkv)};
-  const char* const names[2] = {"q", "k"};
-  const int64_t esz = r->dtype == PISA_DTYPE_BF16 ? 2 : 4;
-  for (int i = 0; i < 2; ++i) {
-    if (!out[i].ptr) continue;
-    for (int j = 0; j < 2; ++j) {
-      if (in[j].ptr && !(i == j && in[j].ptr == out[i].ptr) && share(out[i], in[j], r->d, esz))
-        return fail(PISA_ERR_INVALID_ARG, "%s (output) overlaps %s", names[i], names[j]);
-    }
-  }
-  if (q && k && share(out[0], out[1], r->d, esz)) return fail(PISA_ERR_INVALID_ARG, "q (output) overlaps k (output)");
-  a.positions = positions;
-  a.pos_bstride = r->pos_bstride;
-  a.B = r->B;
-  a.H = q ? r->H : 0;
-  a.HH = a.H + (k ? r->Hkv : 0);
-  a.N = r->N;
-  a.d = r->d;
-  a.rot = r->rot;
-  a.pos0 = r->pos0;
-  a.amplitude = static_cast<float>(r->amplitude);
-  a.sign = sign;
-  for (int i = 0; i < r->rot / 2; ++i) a.turn[i] = r->freq[i] / 6.283185307179586476925286766559;
+  PISA_TRY(check_positions(positions));
+  PISA_TRY(check_rope_overlaps(r, {a.q, a.k}, {"q", "k"}));
+  fill_rope(r, positions, sign, &a);
   return device_status(pisa::launch_rope(a, r->dtype == PISA_DTYPE_BF16, r->layout == PISA_ROPE_HALF,
                                          static_cast<hipStream_t>(stream)),
                        who);
+}
+
+// A norm's descriptor for a rotation of these sides.
+int check_norm(const pisa_rope* r, const pisa_qk_norm* m, pisa::NormArgs* out) {
+  if (!m) return fail(PISA_ERR_INVALID_ARG, "norm is NULL");
+  PISA_TRY(check_ptr(m->q_weight, "q_weight", true));
+  PISA_TRY(check_ptr(m->k_weight, "k_weight", true));
+  if (m->weight_dtype != PISA_DTYPE_F32 && m->weight_dtype != PISA_DTYPE_BF16)
+    return fail(PISA_ERR_INVALID_ARG, "unknown weight_dtype %d", m->weight_dtype);
+  if (m->reserved != 0) return fail(PISA_ERR_INVALID_ARG, "reserved of the norm must be 0");
+  if (!(m->eps >= 1e-30 && m->eps <= 1e30)) return fail(PISA_ERR_INVALID_ARG, "eps must be in [1e-30, 1e30]");
+  if (!(fabs(m->offset) <= 1e30)) return fail(PISA_ERR_INVALID_ARG, "offset is not a number within 10^30");
+  *out = pisa::NormArgs{m->q_weight, m->k_weight, nullptr, nullptr, nullptr, static_cast<float>(m->eps),
+                        static_cast<float>(m->offset), m->weight_dtype == PISA_DTYPE_BF16};
+  return PISA_OK;
+}
+
+// Bytes from a tensor's first value to its last.
+size_t span_of(const pisa_strides& x, int64_t B, int64_t heads, int64_t rows, int d, size_t esz) {
+  return static_cast<size_t>((B - 1) * x.b + (heads - 1) * x.h + (rows - 1) * x.n + d) * esz;
+}
+
+struct Region {
+  const void* ptr;
+  size_t bytes;
+  const char* name;
+};
+bool meet(const Region& x, const Region& y) {
+  const uintptr_t u = reinterpret_cast<uintptr_t>(x.ptr), w = reinterpret_cast<uintptr_t>(y.ptr);
+  return x.bytes && y.bytes && u < w + y.bytes && w < u + x.bytes;
+}
+
+// Rows that an append reads, against what it writes.
+int check_append_regions(const Region* fresh, int nfresh, const Region* held, int nheld, const char* clash) {
+  for (int i = 0; i < nfresh; ++i) {
+    for (int j = 0; j < nheld; ++j)
+      if (meet(fresh[i], held[j])) return fail(PISA_ERR_INVALID_ARG, "%s overlaps the %s", fresh[i].name, held[j].name);
+  }
+  for (int i = 1; i < nheld; ++i) {
+    for (int j = 0; j < i; ++j)
+      if (meet(held[i], held[j])) return fail(PISA_ERR_INVALID_ARG, "%s", clash);
+  }
+  return PISA_OK;
+}
+
+// The list of rows of an append: which of n_rows each of the appended ones is.
+int check_rows(const int32_t* rows, int32_t n_rows, int32_t appended) {
+  if (n_rows < 1) return fail(PISA_ERR_INVALID_ARG, "n_rows must be >= 1 (got %d)", n_rows);
+  if (reinterpret_cast<uintptr_t>(rows) & 3u) return fail(PISA_ERR_INVALID_ARG, "rows is not 4-byte aligned");
+  if (!rows && n_rows < appended)
+    return fail(PISA_ERR_INVALID_ARG, "without rows, n_rows (%d) must be >= N - n_old (%d)", n_rows, appended);
+  return PISA_OK;
 }
 
 int check_qcache(const pisa_qcache* c, const pisa::Geo& g, pisa::QCache* out) {
@@ -497,6 +565,180 @@ int check_qcache(const pisa_qcache* c, const pisa::Geo& g, pisa::QCache* out) {
   *out = pisa::QCache{static_cast<uint8_t*>(c->k), static_cast<uint8_t*>(c->v), c->k_scale, c->v_scale,
                       (g.Nkv + g.C - 1) / g.C};
   return PISA_OK;
+}
+
+int check_n_old(const pisa_problem* p, int32_t n_old) {
+  if (n_old < 0 || n_old > p->N) return fail(PISA_ERR_INVALID_ARG, "need 0 <= n_old <= N (got %d, N=%d)", n_old, p->N);
+  return PISA_OK;
+}
+
+int run_qcache_append(const pisa_problem* p, const pisa_qcache* c, const void* k_new, const pisa_strides* k_strides,
+                      const void* v_new, const pisa_strides* v_strides, const int32_t* rows, int32_t n_rows, int32_t n_old,
+                      float* pyramid, pisa_stream_t stream, const char* who) {
+  pisa::Shape s{};
+  pisa::Geo g{};
+  pisa::QAppend a{};
+  PISA_TRY(check_problem(p, &s, &g));
+  PISA_TRY(check_qcache(c, g, &a.c));
+  PISA_TRY(check_ptr(c->k_open, "k_open"));
+  PISA_TRY(check_ptr(c->v_open, "v_open"));
+  PISA_TRY(check_ptr(pyramid, "pyramid", true));
+  PISA_TRY(check_n_old(p, n_old));
+  PISA_TRY(check_rows(rows, n_rows, p->N - n_old));
+  if (n_old == p->N) return PISA_OK;
+  PISA_TRY(check_ptr(k_new, "k_new"));
+  PISA_TRY(check_ptr(v_new, "v_new"));
+  const int32_t have = rows ? n_rows : p->N - n_old;  // rows that may be read
+  // without a list the contiguous layout is that of the rows that are appended
+  const int32_t wide = n_rows == INT32_MAX ? have : n_rows;
+  pisa_strides ks, vs;
+  PISA_TRY(check_strides(k_strides, "k_new", p->B, p->Hkv, wide, p->d, p->dtype, false, &ks));
+  PISA_TRY(check_strides(v_strides, "v_new", p->B, p->Hkv, wide, p->d, p->dtype, false, &vs));
+  // the appended rows are read while the cache is written
+  const size_t esz = s.bf16 ? 2 : 4, codes = pisa_qcache_bytes(p), open = static_cast<size_t>(s.BH()) * s.C * s.D * esz;
+  const size_t scales = static_cast<size_t>(s.BH()) * a.c.M * sizeof(float);
+  const size_t levels = static_cast<size_t>(s.BH()) * g.R * s.D * sizeof(float);
+  const Region fresh[] = {{k_new, span_of(ks, p->B, p->Hkv, have, p->d, esz), "k_new"},
+                          {v_new, span_of(vs, p->B, p->Hkv, have, p->d, esz), "v_new"},
+                          {rows, rows ? static_cast<size_t>(p->B) * (p->N - n_old) * 4 : 0, "rows"}};
+  const Region held[] = {{c->k, codes, "cache"},        {c->v, codes, "cache"},        {c->k_open, open, "cache"},
+                         {c->v_open, open, "cache"},    {c->k_scale, scales, "cache"}, {c->v_scale, scales, "cache"},
+                         {pyramid, pyramid ? levels : 0, "pyramid"}};
+  PISA_TRY(check_append_regions(fresh, 3, held, 7, "buffers of the cache or the pyramid overlap"));
+  a.k_new = k_new;
+  a.v_new = v_new;
+  a.ksb = ks.b;
+  a.ksh = ks.h;
+  a.ksn = ks.n;
+  a.vsb = vs.b;
+  a.vsh = vs.h;
+  a.vsn = vs.n;
+  a.k_open = c->k_open;
+  a.v_open = c->v_open;
+  a.pyr = pyramid;
+  a.Hkv = p->Hkv;
+  a.n_old = n_old;
+  a.rows = rows;
+  a.n_rows = n_rows;
+  pisa::Geo g_old{};
+  if (n_old > 0) compute_geo(n_old, p->C, p->fanout, &g_old, g.Nkv);
+  return device_status(pisa::launch_qcache_append(g, g_old, s.BH(), s.D, s.bf16, a, static_cast<hipStream_t>(stream)), who);
+}
+
+// The input of one side of a norm's gradient.
+int check_rope_input(const pisa_rope* r, const char* name, int heads, const void* in, const pisa_strides* is, pisa::RopeSide* side) {
+  if (!in) return PISA_OK;
+  PISA_TRY(check_ptr(in, name));
+  pisa_strides si;
+  PISA_TRY(check_strides(is, name, r->B, heads, r->N, r->d, r->dtype, false, &si));
+  *side = pisa::RopeSide{in, nullptr, si.b, si.h, si.n, 0, 0, 0};
+  return PISA_OK;
+}
+
+// A norm's gradient reads its inputs while the gradients are written.
+int check_inputs_apart(const pisa_rope* r, const pisa::RopeSide (&x)[2], const pisa::RopeSide (&d)[2]) {
+  const int heads[2] = {r->H, r->Hkv};
+  const char* const names[2] = {"q", "k"};
+  const int64_t esz = r->dtype == PISA_DTYPE_BF16 ? 2 : 4;
+  for (int i = 0; i < 2; ++i) {
+    for (int j = 0; j < 2; ++j) {
+      if (!x[i].in || !d[j].out) continue;
+      const Placed in{x[i].in, pisa_strides{x[i].ib, x[i].ih, x[i].in_n}, r->B, heads[i], r->N};
+      const Placed out{d[j].out, pisa_strides{d[j].ob, d[j].oh, d[j].on}, r->B, heads[j], r->N};
+      if (share(out, in, r->d, esz)) return fail(PISA_ERR_INVALID_ARG, "d_%s overlaps %s", names[j], names[i]);
+    }
+  }
+  return PISA_OK;
+}
+
+// Weights, their gradients and the workspace against each other and against what is
+// written (by what lies between a tensor's first value and its last).
+int check_norm_overlaps(const pisa_rope* r, const pisa_qk_norm* m, const pisa::RopeSide (&side)[2], const float* d_q_weight,
+                        const float* d_k_weight, const void* ws, size_t ws_bytes) {
+  const size_t w = static_cast<size_t>(r->d) * (m->weight_dtype == PISA_DTYPE_BF16 ? 2 : 4), dw = static_cast<size_t>(r->d) * 4;
+  const size_t esz = r->dtype == PISA_DTYPE_BF16 ? 2 : 4;
+  auto bytes = [](const void* p, size_t n) { return p ? n : 0; };
+  const Region weights[] = {{m->q_weight, bytes(m->q_weight, w), "q_weight"}, {m->k_weight, bytes(m->k_weight, w), "k_weight"}};
+  Region out[5] = {{d_q_weight, bytes(d_q_weight, dw), "d_q_weight"}, {d_k_weight, bytes(d_k_weight, dw), "d_k_weight"},
+                   {ws, bytes(ws, ws_bytes), "workspace"}, {nullptr, 0, "q (output)"}, {nullptr, 0, "k (output)"}};
+  const int heads[2] = {r->H, r->Hkv};
+  for (int i = 0; i < 2; ++i) {
+    out[3 + i].ptr = side[i].out;
+    if (side[i].out) out[3 + i].bytes = span_of({side[i].ob, side[i].oh, side[i].on}, r->B, heads[i], r->N, r->d, esz);
+  }
+  for (int j = 0; j < 5; ++j) {
+    for (const Region& x : weights)
+      if (meet(x, out[j])) return fail(PISA_ERR_INVALID_ARG, "%s overlaps %s", out[j].name, x.name);
+    for (int i = 0; i < std::min(j, 3); ++i)
+      if (meet(out[i], out[j])) return fail(PISA_ERR_INVALID_ARG, "%s overlaps %s", out[j].name, out[i].name);
+  }
+  return PISA_OK;
+}
+
+// Drafted rows of a problem with Nq of them behind N - Nq cached ones.
+int check_draft(const pisa_problem* p, pisa::Shape* s, pisa::Geo* g) {
+  PISA_TRY(check_problem(p, s, g));
+  if (p->Nq > PISA_DRAFT_MAX) return fail(PISA_ERR_UNSUPPORTED, "%d drafted rows (supported: <= %d)", p->Nq, PISA_DRAFT_MAX);
+  return PISA_OK;
+}
+
+size_t draft_ws(const pisa_problem* p, bool q8) {
+  pisa::Shape s{};
+  pisa::Geo g{};
+  return check_draft(p, &s, &g) == PISA_OK ? pisa::draft_attn_ws(s, q8) : 0;
+}
+
+// What both attentions of drafted rows check and launch alike; d has the cache, held
+// its buffers.
+int run_draft_attn(const pisa_problem* p, const pisa::Shape& s, pisa::DraftAttn d, const Region* held, int nheld,
+                   const void* q, const int32_t* block_idx, const void* k_new, const pisa_strides* k_strides, const void* v_new,
+                   const pisa_strides* v_strides, const uint64_t* mask, int64_t mask_bstride, void* o, float* lse, void* ws,
+                   size_t ws_bytes, pisa_stream_t stream, const char* who) {
+  PISA_TRY(check_ptr(q, "q"));
+  PISA_TRY(check_ptr(block_idx, "block_idx"));
+  PISA_TRY(check_ptr(k_new, "k_new"));
+  PISA_TRY(check_ptr(v_new, "v_new"));
+  PISA_TRY(check_ptr(mask, "mask"));
+  PISA_TRY(check_ptr(o, "o"));
+  PISA_TRY(check_ptr(lse, "lse", true));
+  const int64_t W = (p->Nq + 63) / 64;
+  if (mask_bstride != 0 && mask_bstride < p->Nq * W)
+    return fail(PISA_ERR_INVALID_ARG, "mask_bstride must be 0 (one mask) or >= Nq * ceil(Nq / 64) (got %lld)",
+                static_cast<long long>(mask_bstride));
+  pisa_strides ks, vs;
+  PISA_TRY(check_strides(k_strides, "k_new", p->B, p->Hkv, p->Nq, p->d, p->dtype, false, &ks));
+  PISA_TRY(check_strides(v_strides, "v_new", p->B, p->Hkv, p->Nq, p->d, p->dtype, false, &vs));
+  const size_t need = pisa::draft_attn_ws(s, d.k == nullptr);
+  PISA_TRY(check_ws(ws, ws_bytes, need));
+  // what is written against what is read meanwhile
+  const size_t esz = s.bf16 ? 2 : 4, rows = static_cast<size_t>(p->B) * p->H * p->Nq;
+  const Region out[] = {{o, rows * p->d * esz, "o"}, {lse, lse ? rows * 4 : 0, "lse"}, {ws, need, "workspace"}};
+  const Region in[] = {{q, rows * p->d * esz, "q"},
+                       {block_idx, static_cast<size_t>(s.BH()) * p->Nq * p->K * 4, "block_idx"},
+                       {k_new, span_of(ks, p->B, p->Hkv, p->Nq, p->d, esz), "k_new"},
+                       {v_new, span_of(vs, p->B, p->Hkv, p->Nq, p->d, esz), "v_new"},
+                       {mask, static_cast<size_t>(mask_bstride * (p->B - 1) + p->Nq * W) * 8, "mask"}};
+  for (int i = 0; i < 3; ++i) {
+    for (const Region& x : in)
+      if (meet(out[i], x)) return fail(PISA_ERR_INVALID_ARG, "%s overlaps %s", out[i].name, x.name);
+    for (int j = 0; j < nheld; ++j)
+      if (meet(out[i], held[j])) return fail(PISA_ERR_INVALID_ARG, "%s overlaps the %s", out[i].name, held[j].name);
+    for (int j = 0; j < i; ++j)
+      if (meet(out[i], out[j])) return fail(PISA_ERR_INVALID_ARG, "%s overlaps %s", out[i].name, out[j].name);
+  }
+  d.k_new = k_new;
+  d.v_new = v_new;
+  d.ksb = ks.b, d.ksh = ks.h, d.ksn = ks.n;
+  d.vsb = vs.b, d.vsh = vs.h, d.vsn = vs.n;
+  d.mask = mask;
+  d.mask_bstride = mask_bstride;
+  return device_status(pisa::launch_draft_attn(s, d, q, block_idx, o, lse, ws, static_cast<hipStream_t>(stream)), who);
+}
+
+// Whichever sides a call has.
+size_t norm_rope_ws(const pisa_rope* r) {
+  return std::max({pisa::norm_rope_bwd_ws(r->B, r->N, r->H, r->Hkv, r->d), pisa::norm_rope_bwd_ws(r->B, r->N, r->H, 0, r->d),
+                   pisa::norm_rope_bwd_ws(r->B, r->N, 0, r->Hkv, r->d)});
 }
 
 }  // namespace
@@ -825,62 +1067,163 @@ size_t pisa_qcache_bytes(const pisa_problem* p) {
 int pisa_qcache_append(const pisa_problem* p, const pisa_qcache* c, const void* k_new, const pisa_strides* k_strides,
                        const void* v_new, const pisa_strides* v_strides, int32_t n_old, float* pyramid,
                        pisa_stream_t stream) {
+  return run_qcache_append(p, c, k_new, k_strides, v_new, v_strides, nullptr, INT32_MAX, n_old, pyramid, stream,
+                           "pisa_qcache_append");
+}
+
+int pisa_qcache_append_rows(const pisa_problem* p, const pisa_qcache* c, const void* k_new, const pisa_strides* k_strides,
+                            const void* v_new, const pisa_strides* v_strides, const int32_t* rows, int32_t n_rows,
+                            int32_t n_old, float* pyramid, pisa_stream_t stream) {
+  return run_qcache_append(p, c, k_new, k_strides, v_new, v_strides, rows, n_rows, n_old, pyramid, stream,
+                           "pisa_qcache_append_rows");
+}
+
+int pisa_cache_append_rows(const pisa_problem* p, void* k, void* v, const void* k_new, const pisa_strides* k_strides,
+                           const void* v_new, const pisa_strides* v_strides, const int32_t* rows, int32_t n_rows,
+                           int32_t n_old, float* pyramid, pisa_stream_t stream) {
   pisa::Shape s{};
   pisa::Geo g{};
-  pisa::QAppend a{};
   PISA_TRY(check_problem(p, &s, &g));
-  PISA_TRY(check_qcache(c, g, &a.c));
-  PISA_TRY(check_ptr(c->k_open, "k_open"));
-  PISA_TRY(check_ptr(c->v_open, "v_open"));
+  PISA_TRY(check_ptr(k, "k"));
+  PISA_TRY(check_ptr(v, "v"));
   PISA_TRY(check_ptr(pyramid, "pyramid", true));
-  if (n_old < 0 || n_old > p->N) return fail(PISA_ERR_INVALID_ARG, "need 0 <= n_old <= N (got %d, N=%d)", n_old, p->N);
+  PISA_TRY(check_n_old(p, n_old));
+  PISA_TRY(check_rows(rows, n_rows, p->N - n_old));
   if (n_old == p->N) return PISA_OK;
   PISA_TRY(check_ptr(k_new, "k_new"));
   PISA_TRY(check_ptr(v_new, "v_new"));
+  const int32_t have = rows ? n_rows : p->N - n_old;  // rows that may be read
   pisa_strides ks, vs;
-  PISA_TRY(check_strides(k_strides, "k_new", p->B, p->Hkv, p->N - n_old, p->d, p->dtype, false, &ks));
-  PISA_TRY(check_strides(v_strides, "v_new", p->B, p->Hkv, p->N - n_old, p->d, p->dtype, false, &vs));
-  // the appended rows are read while the cache is written
-  const size_t esz = s.bf16 ? 2 : 4, codes = pisa_qcache_bytes(p), open = static_cast<size_t>(s.BH()) * s.C * s.D * esz;
-  auto span = [&](const pisa_strides& x) {  // bytes from a tensor's first value to its last
-    return ((p->B - 1) * x.b + (p->Hkv - 1) * x.h + (p->N - n_old - 1) * x.n + p->d) * static_cast<int64_t>(esz);
-  };
-  const size_t scales = static_cast<size_t>(s.BH()) * a.c.M * sizeof(float);
-  const size_t levels = static_cast<size_t>(s.BH()) * g.R * s.D * sizeof(float);
-  const struct { const void* ptr; size_t bytes; const char* name; } fresh[] = {
-      {k_new, static_cast<size_t>(span(ks)), "k_new"}, {v_new, static_cast<size_t>(span(vs)), "v_new"}};
-  const struct { const void* ptr; size_t bytes; const char* name; } held[] = {
-      {c->k, codes, "cache"},        {c->v, codes, "cache"},        {c->k_open, open, "cache"}, {c->v_open, open, "cache"},
-      {c->k_scale, scales, "cache"}, {c->v_scale, scales, "cache"}, {pyramid, pyramid ? levels : 0, "pyramid"}};
-  auto meet = [](const auto& x, const auto& y) {
-    const uintptr_t u = reinterpret_cast<uintptr_t>(x.ptr), w = reinterpret_cast<uintptr_t>(y.ptr);
-    return u < w + y.bytes && w < u + x.bytes;
-  };
-  for (const auto& x : fresh) {
-    for (const auto& y : held)
-      if (meet(x, y)) return fail(PISA_ERR_INVALID_ARG, "%s overlaps the %s", x.name, y.name);
-  }
-  for (size_t i = 1; i < std::size(held); ++i) {
-    for (size_t j = 0; j < i; ++j)
-      if (meet(held[i], held[j])) return fail(PISA_ERR_INVALID_ARG, "buffers of the cache or the pyramid overlap");
-  }
-  a.k_new = k_new;
-  a.v_new = v_new;
-  a.ksb = ks.b;
-  a.ksh = ks.h;
-  a.ksn = ks.n;
-  a.vsb = vs.b;
-  a.vsh = vs.h;
-  a.vsn = vs.n;
-  a.k_open = c->k_open;
-  a.v_open = c->v_open;
-  a.pyr = pyramid;
-  a.Hkv = p->Hkv;
-  a.n_old = n_old;
+  PISA_TRY(check_strides(k_strides, "k_new", p->B, p->Hkv, n_rows, p->d, p->dtype, false, &ks));
+  PISA_TRY(check_strides(v_strides, "v_new", p->B, p->Hkv, n_rows, p->d, p->dtype, false, &vs));
+  const size_t esz = s.bf16 ? 2 : 4, cache = static_cast<size_t>(s.BH()) * g.Nkv * s.D * esz;
+  const Region fresh[] = {{k_new, span_of(ks, p->B, p->Hkv, have, p->d, esz), "k_new"},
+                          {v_new, span_of(vs, p->B, p->Hkv, have, p->d, esz), "v_new"},
+                          {rows, rows ? static_cast<size_t>(p->B) * (p->N - n_old) * 4 : 0, "rows"}};
+  const Region held[] = {{k, cache, "cache"}, {v, cache, "cache"},
+                         {pyramid, pyramid ? static_cast<size_t>(s.BH()) * g.R * s.D * 4 : 0, "pyramid"}};
+  PISA_TRY(check_append_regions(fresh, 3, held, 3, "k, v and the pyramid overlap"));
+  pisa::CacheAppend a{k, v, k_new, v_new, ks.b, ks.h, ks.n, vs.b, vs.h, vs.n, pyramid, p->Hkv, n_old, rows, n_rows};
   pisa::Geo g_old{};
   if (n_old > 0) compute_geo(n_old, p->C, p->fanout, &g_old, g.Nkv);
-  return device_status(pisa::launch_qcache_append(g, g_old, s.BH(), s.D, s.bf16, a, static_cast<hipStream_t>(stream)),
-                       "pisa_qcache_append");
+  return device_status(pisa::launch_cache_append(g, g_old, s.BH(), s.D, s.bf16, a, static_cast<hipStream_t>(stream)),
+                       "pisa_cache_append_rows");
+}
+
+int pisa_draft_layout(int32_t B, int32_t T, const int32_t* parents, int32_t n, uint64_t* mask, int32_t* positions,
+                      pisa_stream_t stream) {
+  if (B < 1 || B > 65535) return fail(PISA_ERR_INVALID_ARG, "B must be in [1, 65535] (got %d)", B);
+  if (T < 1 || T > PISA_DRAFT_MAX) return fail(PISA_ERR_INVALID_ARG, "T must be in [1, %d] (got %d)", PISA_DRAFT_MAX, T);
+  if (n < 0 || n > INT32_MAX - T) return fail(PISA_ERR_INVALID_ARG, "need 0 <= n <= 2^31 - 1 - T (got %d)", n);
+  PISA_TRY(check_ptr(parents, "parents"));
+  PISA_TRY(check_ptr(mask, "mask"));
+  PISA_TRY(check_ptr(positions, "positions", true));
+  const size_t row = static_cast<size_t>(B) * T;
+  const Region r[] = {{parents, row * 4, "parents"}, {mask, row * 8 * ((T + 63) / 64), "mask"},
+                      {positions, positions ? row * 4 : 0, "positions"}};
+  for (int i = 1; i < 3; ++i) {
+    for (int j = 0; j < i; ++j)
+      if (meet(r[i], r[j])) return fail(PISA_ERR_INVALID_ARG, "%s overlaps %s", r[i].name, r[j].name);
+  }
+  return device_status(pisa::launch_draft_layout(parents, B, T, n, mask, positions, static_cast<hipStream_t>(stream)),
+                       "pisa_draft_layout");
+}
+
+size_t pisa_draft_attn_workspace_bytes(const pisa_problem* p) { return draft_ws(p, false); }
+size_t pisa_qcache_draft_attn_workspace_bytes(const pisa_problem* p) { return draft_ws(p, true); }
+
+int pisa_draft_attn_fwd(const pisa_problem* p, const void* q, const void* k, const void* v, const int32_t* block_idx,
+                        const void* k_new, const pisa_strides* k_strides, const void* v_new, const pisa_strides* v_strides,
+                        const uint64_t* mask, int64_t mask_bstride, void* o, float* lse, void* ws, size_t ws_bytes,
+                        pisa_stream_t stream) {
+  pisa::Shape s{};
+  pisa::Geo g{};
+  PISA_TRY(check_draft(p, &s, &g));
+  PISA_TRY(check_ptr(k, "k"));
+  PISA_TRY(check_ptr(v, "v"));
+  pisa::DraftAttn d{};
+  d.k = k;
+  d.v = v;
+  const size_t rows = static_cast<size_t>(s.BH()) * g.Nkv * s.D * (s.bf16 ? 2 : 4);
+  const Region held[] = {{k, rows, "cache"}, {v, rows, "cache"}};
+  return run_draft_attn(p, s, d, held, 2, q, block_idx, k_new, k_strides, v_new, v_strides, mask, mask_bstride, o, lse, ws,
+                        ws_bytes, stream, "pisa_draft_attn_fwd");
+}
+
+int pisa_qcache_draft_attn_fwd(const pisa_problem* p, const pisa_qcache* c, const void* q, const int32_t* block_idx,
+                               const void* k_new, const pisa_strides* k_strides, const void* v_new,
+                               const pisa_strides* v_strides, const uint64_t* mask, int64_t mask_bstride, void* o, float* lse,
+                               void* ws, size_t ws_bytes, pisa_stream_t stream) {
+  pisa::Shape s{};
+  pisa::Geo g{};
+  pisa::DraftAttn d{};
+  PISA_TRY(check_draft(p, &s, &g));
+  PISA_TRY(check_qcache(c, g, &d.c));
+  const size_t codes = pisa_qcache_bytes(p), scales = static_cast<size_t>(s.BH()) * d.c.M * sizeof(float);
+  const Region held[] = {{c->k, codes, "cache"}, {c->v, codes, "cache"}, {c->k_scale, scales, "cache"}, {c->v_scale, scales, "cache"}};
+  return run_draft_attn(p, s, d, held, 4, q, block_idx, k_new, k_strides, v_new, v_strides, mask, mask_bstride, o, lse, ws,
+                        ws_bytes, stream, "pisa_qcache_draft_attn_fwd");
+}
+
+int pisa_norm_rope_fwd(const pisa_rope* r, const pisa_qk_norm* m, const void* q, const pisa_strides* q_strides, const void* k,
+                       const pisa_strides* k_strides, const int32_t* positions, void* q_out,
+                       const pisa_strides* q_out_strides, void* k_out, const pisa_strides* k_out_strides,
+                       pisa_stream_t stream) {
+  PISA_TRY(check_rope(r));
+  pisa::RopeArgs a{};
+  pisa::NormArgs na{};
+  PISA_TRY(check_norm(r, m, &na));
+  PISA_TRY(check_rope_side(r, "q", r->H, q, q_strides, q_out, q_out_strides, &a.q));
+  PISA_TRY(check_rope_side(r, "k", r->Hkv, k, k_strides, k_out, k_out_strides, &a.k));
+  if (!q && !k) return fail(PISA_ERR_INVALID_ARG, "neither q nor k given");
+  PISA_TRY(check_positions(positions));
+  PISA_TRY(check_rope_overlaps(r, {a.q, a.k}, {"q", "k"}));
+  PISA_TRY(check_norm_overlaps(r, m, {a.q, a.k}, nullptr, nullptr, nullptr, 0));
+  fill_rope(r, positions, 1.f, &a);
+  return device_status(pisa::launch_norm_rope(a, na, nullptr, nullptr, r->dtype == PISA_DTYPE_BF16, r->layout == PISA_ROPE_HALF,
+                                              static_cast<hipStream_t>(stream)),
+                       "pisa_norm_rope_fwd");
+}
+
+size_t pisa_norm_rope_bwd_workspace_bytes(const pisa_rope* r) {
+  if (check_rope(r) != PISA_OK) return 0;
+  return norm_rope_ws(r);
+}
+
+int pisa_norm_rope_bwd(const pisa_rope* r, const pisa_qk_norm* m, const void* q, const pisa_strides* q_strides, const void* k,
+                       const pisa_strides* k_strides, const void* d_q_out, const pisa_strides* d_q_out_strides,
+                       const void* d_k_out, const pisa_strides* d_k_out_strides, const int32_t* positions, void* d_q,
+                       const pisa_strides* d_q_strides, void* d_k, const pisa_strides* d_k_strides, float* d_q_weight,
+                       float* d_k_weight, void* ws, size_t ws_bytes, pisa_stream_t stream) {
+  PISA_TRY(check_rope(r));
+  pisa::RopeArgs a{};
+  pisa::NormArgs na{};
+  pisa::RopeSide dq{}, dk{};
+  PISA_TRY(check_norm(r, m, &na));
+  if ((!q) != (!d_q) || (!k) != (!d_k))
+    return fail(PISA_ERR_INVALID_ARG, "a side needs its input, its output's gradient and its gradient, or none of them");
+  PISA_TRY(check_rope_side(r, "d_q_out", r->H, d_q_out, d_q_out_strides, d_q, d_q_strides, &dq));
+  PISA_TRY(check_rope_side(r, "d_k_out", r->Hkv, d_k_out, d_k_out_strides, d_k, d_k_strides, &dk));
+  if (!q && !k) return fail(PISA_ERR_INVALID_ARG, "neither q nor k given");
+  PISA_TRY(check_rope_input(r, "q", r->H, q, q_strides, &a.q));
+  PISA_TRY(check_rope_input(r, "k", r->Hkv, k, k_strides, &a.k));
+  PISA_TRY(check_positions(positions));
+  PISA_TRY(check_ptr(d_q_weight, "d_q_weight", true));
+  PISA_TRY(check_ptr(d_k_weight, "d_k_weight", true));
+  if ((d_q_weight && !q) || (d_k_weight && !k)) return fail(PISA_ERR_INVALID_ARG, "a weight's gradient needs its side");
+  PISA_TRY(check_rope_overlaps(r, {dq, dk}, {"d_q_out", "d_k_out"}));
+  // the inputs against the gradients that are written
+  PISA_TRY(check_inputs_apart(r, {a.q, a.k}, {dq, dk}));
+  const size_t need = d_q_weight || d_k_weight ? norm_rope_ws(r) : 0;
+  PISA_TRY(check_ws(ws, ws_bytes, need));
+  PISA_TRY(check_norm_overlaps(r, m, {dq, dk}, d_q_weight, d_k_weight, need ? ws : nullptr, need));
+  na.d_q_weight = d_q_weight;
+  na.d_k_weight = d_k_weight;
+  na.parts = static_cast<float*>(ws);
+  fill_rope(r, positions, -1.f, &a);
+  return device_status(pisa::launch_norm_rope(a, na, &dq, &dk, r->dtype == PISA_DTYPE_BF16, r->layout == PISA_ROPE_HALF,
+                                              static_cast<hipStream_t>(stream)),
+                       "pisa_norm_rope_bwd");
 }
 
 size_t pisa_qcache_attn_workspace_bytes(const pisa_problem* p) {

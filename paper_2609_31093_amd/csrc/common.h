@@ -162,6 +162,15 @@ __device__ __forceinline__ float xor32_f(float v) {
   return __builtin_bit_cast(float, xor32_i<J>(__builtin_bit_cast(int, v)));
 }
 
+// Entry i of a list of rows to append, within the n rows there are.  It is read for
+// every lane (the empty asm keeps the read out of a branch), so that what follows is
+// a choice between two addresses.
+__device__ __forceinline__ int picked_row(const int32_t* __restrict__ rows, int i, int n) {
+  int j = min(max(rows[i], 0), n - 1);
+  asm volatile("" : "+v"(j));
+  return j;
+}
+
 // Orders LDS traffic among the lanes of one wavefront (no cross-wave effect).
 __device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");

@@ -182,6 +182,20 @@ struct RopeArgs {
 };
 hipError_t launch_rope(const RopeArgs& a, bool bf16, bool half, hipStream_t st);
 
+// Norms of queries and keys in front of their rotation (norm_rope.hip).  Gradients:
+// dq, dk (null forward) hold the outputs' gradients and where the inputs' go; parts:
+// norm_rope_bwd_ws() bytes.
+struct NormArgs {
+  const void *q_weight, *k_weight;  // null: ones
+  float *d_q_weight, *d_k_weight;   // null: not wanted
+  float* parts;
+  float eps, offset;
+  bool w_bf16;
+};
+size_t norm_rope_bwd_ws(int B, int N, int H, int Hkv, int d);  // H or Hkv 0: that side is left out
+hipError_t launch_norm_rope(const RopeArgs& a, const NormArgs& m, const RopeSide* dq, const RopeSide* dk, bool bf16, bool half,
+                            hipStream_t st);
+
 // 8-bit cache (qcache.hip, qcache_attn.hip).
 struct QCache {
   uint8_t* k;
@@ -197,12 +211,40 @@ struct QAppend {
   void *k_open, *v_open;
   float* pyr;
   int Hkv, n_old;
+  const int32_t* rows;  // [B, N - n_old]: which of the n_rows new rows; null: all of them
+  int n_rows;
 };
 hipError_t launch_qcache_append(const Geo& geo, const Geo& geo_old, int BH, int D, bool bf16, const QAppend& a,
                                 hipStream_t st);
 size_t qcache_attn_ws(const Shape& s, const Geo& geo);
 hipError_t launch_qcache_attn(const Shape& s, const Geo& geo, const QCache& c, const void* q, const int32_t* idx, void* o,
                               float* lse, void* ws, hipStream_t st);
+
+// Drafted tokens (drafts.hip, draft_attn.hip).
+hipError_t launch_draft_layout(const int32_t* parents, int B, int T, int n, uint64_t* mask, int32_t* positions, hipStream_t st);
+struct CacheAppend {
+  void *k, *v;
+  const void *k_new, *v_new;
+  int64_t ksb, ksh, ksn, vsb, vsh, vsn;  // strides in elements
+  float* pyr;
+  int Hkv, n_old;
+  const int32_t* rows;  // as in QAppend
+  int n_rows;
+};
+hipError_t launch_cache_append(const Geo& geo, const Geo& geo_old, int BH, int D, bool bf16, const CacheAppend& a,
+                               hipStream_t st);
+
+struct DraftAttn {
+  QCache c;           // where k is null
+  const void *k, *v;  // [BH, Nkv, D]
+  const void *k_new, *v_new;
+  int64_t ksb, ksh, ksn, vsb, vsh, vsn;  // strides in elements
+  const uint64_t* mask;
+  int64_t mask_bstride;  // words
+};
+size_t draft_attn_ws(const Shape& s, bool q8);
+hipError_t launch_draft_attn(const Shape& s, const DraftAttn& d, const void* q, const int32_t* idx, void* o, float* lse, void* ws,
+                             hipStream_t st);
 
 // Pyramid levels 2 .. Lstore from level 1, which is up to date (pool.hip); the
 // levels above hold the nodes of the first n_old tokens.

@@ -7,6 +7,7 @@
 // e4m3, and every later reader (fp32 or bf16) sees the same numbers.
 #include "common.h"
 #include "kernels.h"
+#include "pyramid_path.h"
 
 namespace pisa {
 
@@ -107,15 +108,22 @@ __device__ __forceinline__ uint32_t pack4_e4m3(float a, float b, float c, float 
   return static_cast<uint32_t>(pack2_e4m3<true, ODD>(c, d, inv, pack2_e4m3<false, ODD>(a, b, inv, 0)));
 }
 
-// What a wavefront needs to know of the block it quantises.
-template <typename T, int D>
+// What a wavefront needs to know of the block it quantises.  PICK: the appended rows
+// are those that a list names, of n_rows (an entry outside is read as the nearest).
+template <typename T, int D, bool PICK>
 struct Source {
   const T* open;   // the (batch, KV head)'s raw rows, at this lane's columns
   const T* fresh;  // its appended rows, likewise
   int64_t stride;  // between appended rows
   int tok0, nrows, had, n_old;
+  const int32_t* rows;
+  int n_rows;
+  __device__ __forceinline__ const T* appended(int i) const {
+    return fresh + (PICK ? picked_row(rows, max(i, 0), n_rows) : i) * stride;
+  }
   __device__ __forceinline__ const T* row(int r) const {
-    return r < had ? open + r * D : fresh + (tok0 + r - n_old) * stride;
+    const T* p = appended(tok0 + r - n_old);
+    return r < had ? open + r * D : p;
   }
 };
 
@@ -171,8 +179,8 @@ __device__ __forceinline__ void store_codes(const Rows<T, D, CH / 4>& x, uint8_t
 // the whole block where C <= CH, read once; larger blocks are read twice, the
 // second time from the cache.  Keys: means(m) is called with the means of the
 // raw rows before any code is stored.
-template <typename T, int D, bool KEYS, int CH, typename F>
-__device__ __forceinline__ void quantise_block(const Source<T, D>& src, int C, uint8_t* dst, float* scale, int lane, F means) {
+template <typename T, int D, bool KEYS, int CH, bool PICK, typename F>
+__device__ __forceinline__ void quantise_block(const Source<T, D, PICK>& src, int C, uint8_t* dst, float* scale, int lane, F means) {
   constexpr int DPL = D / 16, R = CH / 4;
   const int sub = lane & 15, rg = lane >> 4;
   Rows<T, D, R> x;
@@ -182,6 +190,7 @@ __device__ __forceinline__ void quantise_block(const Source<T, D>& src, int C, u
     const T* end = src.row(src.nrows - 1);
     x.load([&](int i) {
       const int r = r0 + i * step;
+      if constexpr (PICK) return src.row(min(r, src.nrows - 1));
       const T* p = r < src.had ? src.open + r * D : fresh + i * step * src.stride;
       return r < src.nrows ? p : end;
     });
@@ -251,13 +260,13 @@ __device__ __forceinline__ void quantise_block(const Source<T, D>& src, int C, u
 
 // The rows of the last block that were appended now, into the raw rows.  Called
 // by the wavefront that read the old raw rows, after it used them.
-template <typename T, int D>
-__device__ __forceinline__ void keep_raw(const Source<T, D>& src, T* open, int last0, int N, int lane) {
+template <typename T, int D, bool PICK>
+__device__ __forceinline__ void keep_raw(const Source<T, D, PICK>& src, T* open, int last0, int N, int lane) {
   constexpr int R = 8;
   const int rg = lane >> 4, n = N - last0;
   for (int r0 = max(0, src.n_old - last0); r0 < n; r0 += 4 * R) {
     Rows<T, D, R> x;
-    x.load([&](int i) { return src.fresh + (last0 + min(r0 + rg + 4 * i, n - 1) - src.n_old) * src.stride; });
+    x.load([&](int i) { return src.appended(last0 + min(r0 + rg + 4 * i, n - 1) - src.n_old); });
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       const int r = r0 + rg + 4 * i;
@@ -265,9 +274,6 @@ __device__ __forceinline__ void keep_raw(const Source<T, D>& src, T* open, int l
     }
   }
 }
-
-// Most stored levels: 65535 leaf blocks, two children to a node.
-constexpr int kMaxStored = 16;
 
 }  // namespace
 
@@ -277,7 +283,7 @@ constexpr int kMaxStored = 16;
 // meanwhile, all levels' loads in flight at once, and take the mean up from
 // there (node_mean's order: children by index, the changed one last).  Otherwise
 // four wavefronts on their own: blocks x {keys, values}.
-template <typename T, int D, int CH, bool PATH>
+template <typename T, int D, int CH, bool PATH, bool PICK>
 __global__ __launch_bounds__(256) void qcache_append_kernel(QAppend a, Geo geo) {
   constexpr int DPL = D / 16;
   __shared__ __align__(16) float mean[D];
@@ -292,7 +298,7 @@ __global__ __launch_bounds__(256) void qcache_append_kernel(QAppend a, Geo geo) 
   float* pb = a.pyr + static_cast<int64_t>(bh) * geo.R * D;
 
   if (PATH ? wave < 2 : leaf <= last) {
-    Source<T, D> src;
+    Source<T, D, PICK> src;
     T* open = static_cast<T*>(keys ? a.k_open : a.v_open) + static_cast<int64_t>(bh) * C * D + sub * DPL;
     src.open = open;
     src.fresh = static_cast<const T*>(keys ? a.k_new : a.v_new) + b * (keys ? a.ksb : a.vsb) + h * (keys ? a.ksh : a.vsh) + sub * DPL;
@@ -301,9 +307,11 @@ __global__ __launch_bounds__(256) void qcache_append_kernel(QAppend a, Geo geo) 
     src.nrows = min(C, geo.N - src.tok0);
     src.n_old = a.n_old;
     src.had = max(0, a.n_old - src.tok0);
+    src.rows = PICK ? a.rows + static_cast<int64_t>(b) * (geo.N - a.n_old) : nullptr;
+    src.n_rows = a.n_rows;
     const int64_t blk = static_cast<int64_t>(bh) * a.c.M + leaf;
     if (keys) {
-      quantise_block<T, D, true, CH>(src, C, a.c.k + blk * C * D, a.c.k_scale + blk, lane, [&](const float (&m)[DPL]) {
+      quantise_block<T, D, true, CH, PICK>(src, C, a.c.k + blk * C * D, a.c.k_scale + blk, lane, [&](const float (&m)[DPL]) {
         if (!a.pyr) return;
         if (rg == 0) {
           float* dst = pb + (geo.off[1] + leaf) * D + sub * DPL;
@@ -319,51 +327,24 @@ __global__ __launch_bounds__(256) void qcache_append_kernel(QAppend a, Geo geo) 
     } else {
       if constexpr (PATH)
         if (a.pyr) __syncthreads();
-      quantise_block<T, D, false, CH>(src, C, a.c.v + blk * C * D, a.c.v_scale + blk, lane, [](const float (&)[DPL]) {});
+      quantise_block<T, D, false, CH, PICK>(src, C, a.c.v + blk * C * D, a.c.v_scale + blk, lane, [](const float (&)[DPL]) {});
     }
-    if (leaf == first) keep_raw<T, D>(src, open, last * C, geo.N, lane);
+    if (leaf == first) keep_raw<T, D, PICK>(src, open, last * C, geo.N, lane);
   } else if (PATH && a.pyr) {
-    const int d = threadIdx.x - 128;
-    float sum[kMaxStored + 1], x[kMaxStored + 1];
-#pragma unroll
-    for (int lv = 2; lv <= kMaxStored; ++lv) sum[lv] = 0.f;
-    if (d < D) {
-      for (int j = 0; j < geo.g - 1; ++j) {
-#pragma unroll
-        for (int lv = 2; lv <= kMaxStored; ++lv) {
-          const int c0 = (geo.M[lv] - 1) * geo.g + j;
-          const bool have = lv <= geo.Lstore && c0 < geo.M[lv - 1] - 1;
-          x[lv] = pb[(geo.off[1] + (have ? geo.off[lv - 1] - geo.off[1] + c0 : 0)) * D + d];
-          x[lv] = have ? x[lv] : 0.f;
-        }
-#pragma unroll
-        for (int lv = 2; lv <= kMaxStored; ++lv) sum[lv] += x[lv];
-      }
-    }
-    __syncthreads();
-    if (d < D) {
-      float v = mean[d];
-#pragma unroll
-      for (int lv = 2; lv <= kMaxStored; ++lv) {
-        if (lv <= geo.Lstore) {
-          v = (sum[lv] + v) / static_cast<float>(geo.M[lv - 1] - (geo.M[lv] - 1) * geo.g);
-          pb[(geo.off[lv] + geo.M[lv] - 1) * D + d] = v;
-        }
-      }
-    }
+    path_levels<D>(geo, pb, mean, threadIdx.x - 128);
   }
 }
 
-template <typename T, int D, int CH>
+template <typename T, int D, int CH, bool PICK>
 static hipError_t launch_append(const Geo& geo, const Geo& geo_old, int BH, const QAppend& a, hipStream_t st) {
   const int first = a.n_old / geo.C, nleaf = geo.M[1] - first;
   const bool path = a.n_old > 0 && nleaf == 1 && geo_old.Lstore == geo.Lstore;
   {
     ProfScope ps("qcache_append", st);
     if (path) {
-      qcache_append_kernel<T, D, CH, true><<<dim3(1, BH), 256, 0, st>>>(a, geo);
+      qcache_append_kernel<T, D, CH, true, PICK><<<dim3(1, BH), 256, 0, st>>>(a, geo);
     } else {
-      qcache_append_kernel<T, D, CH, false><<<dim3((nleaf + 1) / 2, BH), 256, 0, st>>>(a, geo);
+      qcache_append_kernel<T, D, CH, false, PICK><<<dim3((nleaf + 1) / 2, BH), 256, 0, st>>>(a, geo);
     }
   }
   const hipError_t e = hipGetLastError();
@@ -376,8 +357,9 @@ static hipError_t launch_append(const Geo& geo, const Geo& geo_old, int BH, cons
 template <typename T, int D>
 static hipError_t launch_append_ch(const Geo& geo, const Geo& geo_old, int BH, const QAppend& a, hipStream_t st) {
   if constexpr (sizeof(T) == 2)
-    if (geo.C > 64) return launch_append<T, D, 128>(geo, geo_old, BH, a, st);
-  return launch_append<T, D, 64>(geo, geo_old, BH, a, st);
+    if (geo.C > 64)
+      return a.rows ? launch_append<T, D, 128, true>(geo, geo_old, BH, a, st) : launch_append<T, D, 128, false>(geo, geo_old, BH, a, st);
+  return a.rows ? launch_append<T, D, 64, true>(geo, geo_old, BH, a, st) : launch_append<T, D, 64, false>(geo, geo_old, BH, a, st);
 }
 
 hipError_t launch_qcache_append(const Geo& geo, const Geo& geo_old, int BH, int D, bool bf16, const QAppend& a,

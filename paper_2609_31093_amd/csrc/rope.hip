@@ -15,40 +15,9 @@
 // (relative, 8192 positions from 2^20 on), where 64-bit sines leave 4.2e-8.
 #include "common.h"
 #include "kernels.h"
+#include "rope_shared.h"
 
 namespace pisa {
-
-namespace {
-
-// 8 consecutive values from an address that may be aligned to the element only.
-template <typename T>
-__device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
-  T raw[8];
-  __builtin_memcpy(raw, p, sizeof(raw));
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    if constexpr (sizeof(T) == 2) x[i] = bf16_to_f32(raw[i]);
-    else x[i] = raw[i];
-  }
-}
-
-template <typename T>
-__device__ __forceinline__ void store8(T* p, const float (&x)[8]) {
-  if constexpr (sizeof(T) == 2) {
-    const uint4 w = make_uint4(pack2_bf16(x[0], x[1]), pack2_bf16(x[2], x[3]), pack2_bf16(x[4], x[5]), pack2_bf16(x[6], x[7]));
-    __builtin_memcpy(p, &w, 16);
-  } else {
-    __builtin_memcpy(p, x, 32);
-  }
-}
-
-template <typename T>
-__device__ __forceinline__ void store1(T* p, float x) {
-  if constexpr (sizeof(T) == 2) *p = static_cast<T>(pack2_bf16(x, x));
-  else *p = x;
-}
-
-}  // namespace
 
 template <typename T, bool HALF>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
@@ -61,15 +30,7 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   const int pairs = a.rot / 2;
 
   float c[8], s[8];
-  const int64_t t = a.positions ? static_cast<int64_t>(a.positions[b * a.pos_bstride + n]) : static_cast<int64_t>(a.pos0) + n;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const double turns = static_cast<double>(t) * a.turn[min(8 * u + i, pairs - 1)];
-    float sn, cs;
-    sincospif(2.f * static_cast<float>(turns - rint(turns)), &sn, &cs);
-    c[i] = a.amplitude * cs;
-    s[i] = a.amplitude * sn * a.sign;
-  }
+  rope_angles(a, b, n, 8 * u, pairs, c, s);
 
   const int h1 = min(a.HH, (static_cast<int>(blockIdx.y) + 1) * a.heads);
   for (int hh = blockIdx.y * a.heads; hh < h1; ++hh) {

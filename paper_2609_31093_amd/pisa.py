@@ -35,6 +35,7 @@ PISA_ROPE_SCALE_LINEAR = 1
 PISA_ROPE_SCALE_BASE = 2
 PISA_ROPE_SCALE_PARTS = 3
 PISA_ROPE_MAX_PAIRS = 64
+PISA_DRAFT_MAX = 1024
 
 PISA_OK = 0
 PISA_ERR_INVALID_ARG = -1
@@ -50,8 +51,12 @@ EXPORTS = (
     "pisa_attn_bwd_workspace_bytes", "pisa_sparse_attn_bwd",
     "pisa_quality_workspace_bytes", "pisa_selection_quality",
     "pisa_rope_frequencies", "pisa_rope_fwd", "pisa_rope_bwd",
+    "pisa_norm_rope_fwd", "pisa_norm_rope_bwd_workspace_bytes", "pisa_norm_rope_bwd",
     "pisa_qcache_blocks", "pisa_qcache_bytes", "pisa_qcache_append",
     "pisa_qcache_attn_workspace_bytes", "pisa_qcache_attn_fwd",
+    "pisa_draft_layout", "pisa_draft_attn_workspace_bytes", "pisa_draft_attn_fwd",
+    "pisa_qcache_draft_attn_workspace_bytes", "pisa_qcache_draft_attn_fwd",
+    "pisa_cache_append_rows", "pisa_qcache_append_rows",
     "pisa_profile_enable", "pisa_profile_report", "pisa_status_string", "pisa_last_error",
 )
 
@@ -82,6 +87,12 @@ class Rope(ctypes.Structure):
     _fields_ = ([(n, ctypes.c_int32) for n in ("B", "H", "Hkv", "N", "d", "rot", "layout", "dtype", "pos0", "reserved")]
                 + [("pos_bstride", ctypes.c_int64), ("amplitude", ctypes.c_double),
                    ("freq", ctypes.c_double * PISA_ROPE_MAX_PAIRS)])
+
+
+class QKNorm(ctypes.Structure):
+    """Mirror of ``pisa_qk_norm``."""
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("weight_dtype", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("eps", ctypes.c_double), ("offset", ctypes.c_double)]
 
 
 class QCacheBuffers(ctypes.Structure):
@@ -131,11 +142,21 @@ def _load():
                                                  ctypes.c_double, ctypes.c_double]),
         "pisa_rope_fwd": (ctypes.c_int, [ctypes.POINTER(Rope), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]),
         "pisa_rope_bwd": (ctypes.c_int, [ctypes.POINTER(Rope), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]),
+        "pisa_norm_rope_fwd": (ctypes.c_int, [ctypes.POINTER(Rope), ctypes.POINTER(QKNorm)] + [vp] * 10),
+        "pisa_norm_rope_bwd_workspace_bytes": (sz, [ctypes.POINTER(Rope)]),
+        "pisa_norm_rope_bwd": (ctypes.c_int, [ctypes.POINTER(Rope), ctypes.POINTER(QKNorm)] + [vp] * 16 + [sz, vp]),
         "pisa_qcache_blocks": (ctypes.c_int32, [P]),
         "pisa_qcache_bytes": (sz, [P]),
         "pisa_qcache_append": (ctypes.c_int, [P, vp, vp, vp, vp, vp, i32, vp, vp]),
         "pisa_qcache_attn_workspace_bytes": (sz, [P]),
         "pisa_qcache_attn_fwd": (ctypes.c_int, [P, vp, vp, vp, vp, vp, vp, sz, vp]),
+        "pisa_draft_layout": (ctypes.c_int, [i32, i32, vp, i32, vp, vp, vp]),
+        "pisa_draft_attn_workspace_bytes": (sz, [P]),
+        "pisa_draft_attn_fwd": (ctypes.c_int, [P] + [vp] * 9 + [ctypes.c_int64, vp, vp, vp, sz, vp]),
+        "pisa_qcache_draft_attn_workspace_bytes": (sz, [P]),
+        "pisa_qcache_draft_attn_fwd": (ctypes.c_int, [P] + [vp] * 8 + [ctypes.c_int64, vp, vp, vp, sz, vp]),
+        "pisa_cache_append_rows": (ctypes.c_int, [P, vp, vp, vp, vp, vp, vp, vp, i32, i32, vp, vp]),
+        "pisa_qcache_append_rows": (ctypes.c_int, [P, vp, vp, vp, vp, vp, vp, i32, i32, vp, vp]),
         "pisa_profile_enable": (ctypes.c_int, [ctypes.c_int]),
         "pisa_profile_report": (ctypes.c_int, [ctypes.c_char_p, sz]),
         "pisa_status_string": (ctypes.c_char_p, [ctypes.c_int]),
@@ -309,6 +330,27 @@ def pisa_rope_bwd(r: Rope, d_q_out, d_q_out_strides, d_k_out, d_k_out_strides, p
                       d_k, d_k_strides, stream)
 
 
+def pisa_norm_rope_fwd(r: Rope, m: QKNorm, q, q_strides, k, k_strides, positions, q_out, q_out_strides, k_out,
+                       k_out_strides, stream=None) -> int:
+    return _check(_lib.pisa_norm_rope_fwd(ctypes.byref(r), ctypes.byref(m), _ptr(q), _at(q_strides), _ptr(k), _at(k_strides),
+                                          _ptr(positions), _ptr(q_out), _at(q_out_strides), _ptr(k_out), _at(k_out_strides),
+                                          _stream(stream)), "pisa_norm_rope_fwd")
+
+
+def pisa_norm_rope_bwd_workspace_bytes(r: Rope) -> int:
+    return _lib.pisa_norm_rope_bwd_workspace_bytes(ctypes.byref(r))
+
+
+def pisa_norm_rope_bwd(r: Rope, m: QKNorm, q, q_strides, k, k_strides, d_q_out, d_q_out_strides, d_k_out, d_k_out_strides,
+                       positions, d_q, d_q_strides, d_k, d_k_strides, d_q_weight=None, d_k_weight=None, ws=None, ws_bytes=0,
+                       stream=None) -> int:
+    return _check(_lib.pisa_norm_rope_bwd(ctypes.byref(r), ctypes.byref(m), _ptr(q), _at(q_strides), _ptr(k), _at(k_strides),
+                                          _ptr(d_q_out), _at(d_q_out_strides), _ptr(d_k_out), _at(d_k_out_strides),
+                                          _ptr(positions), _ptr(d_q), _at(d_q_strides), _ptr(d_k), _at(d_k_strides),
+                                          _ptr(d_q_weight), _ptr(d_k_weight), _ptr(ws), ws_bytes, _stream(stream)),
+                  "pisa_norm_rope_bwd")
+
+
 def pisa_qcache_blocks(p: Problem) -> int:
     M = _lib.pisa_qcache_blocks(ctypes.byref(p))
     return _check(M, "pisa_qcache_blocks") if M < 0 else M
@@ -331,6 +373,48 @@ def pisa_qcache_attn_workspace_bytes(p: Problem) -> int:
 def pisa_qcache_attn_fwd(p: Problem, cache, q, block_idx, o, lse=None, ws=None, ws_bytes=0, stream=None) -> int:
     return _check(_lib.pisa_qcache_attn_fwd(ctypes.byref(p), cache.address, _ptr(q), _ptr(block_idx), _ptr(o), _ptr(lse),
                                             _ptr(ws), ws_bytes, _stream(stream)), "pisa_qcache_attn_fwd")
+
+
+def pisa_draft_layout(B: int, T: int, parents, n: int, mask, positions=None, stream=None) -> int:
+    return _check(_lib.pisa_draft_layout(B, T, _ptr(parents), n, _ptr(mask), _ptr(positions), _stream(stream)),
+                  "pisa_draft_layout")
+
+
+def pisa_draft_attn_workspace_bytes(p: Problem) -> int:
+    return _lib.pisa_draft_attn_workspace_bytes(ctypes.byref(p))
+
+
+def pisa_draft_attn_fwd(p: Problem, q, k, v, block_idx, k_new, k_strides, v_new, v_strides, mask, mask_bstride: int, o, lse=None,
+                        ws=None, ws_bytes=0, stream=None) -> int:
+    return _check(_lib.pisa_draft_attn_fwd(ctypes.byref(p), _ptr(q), _ptr(k), _ptr(v), _ptr(block_idx), _ptr(k_new),
+                                           _at(k_strides), _ptr(v_new), _at(v_strides), _ptr(mask), mask_bstride, _ptr(o),
+                                           _ptr(lse), _ptr(ws), ws_bytes, _stream(stream)), "pisa_draft_attn_fwd")
+
+
+def pisa_qcache_draft_attn_workspace_bytes(p: Problem) -> int:
+    return _lib.pisa_qcache_draft_attn_workspace_bytes(ctypes.byref(p))
+
+
+def pisa_qcache_draft_attn_fwd(p: Problem, cache, q, block_idx, k_new, k_strides, v_new, v_strides, mask, mask_bstride: int, o,
+                               lse=None, ws=None, ws_bytes=0, stream=None) -> int:
+    return _check(_lib.pisa_qcache_draft_attn_fwd(ctypes.byref(p), cache.address, _ptr(q), _ptr(block_idx), _ptr(k_new),
+                                                  _at(k_strides), _ptr(v_new), _at(v_strides), _ptr(mask), mask_bstride,
+                                                  _ptr(o), _ptr(lse), _ptr(ws), ws_bytes, _stream(stream)),
+                  "pisa_qcache_draft_attn_fwd")
+
+
+def pisa_cache_append_rows(p: Problem, k, v, k_new, k_strides, v_new, v_strides, rows, n_rows: int, n_old: int, pyramid=None,
+                           stream=None) -> int:
+    return _check(_lib.pisa_cache_append_rows(ctypes.byref(p), _ptr(k), _ptr(v), _ptr(k_new), _at(k_strides), _ptr(v_new),
+                                              _at(v_strides), _ptr(rows), n_rows, n_old, _ptr(pyramid), _stream(stream)),
+                  "pisa_cache_append_rows")
+
+
+def pisa_qcache_append_rows(p: Problem, cache, k_new, k_strides, v_new, v_strides, rows, n_rows: int, n_old: int, pyramid=None,
+                            stream=None) -> int:
+    return _check(_lib.pisa_qcache_append_rows(ctypes.byref(p), cache.address, _ptr(k_new), _at(k_strides), _ptr(v_new),
+                                               _at(v_strides), _ptr(rows), n_rows, n_old, _ptr(pyramid), _stream(stream)),
+                  "pisa_qcache_append_rows")
 
 
 def pisa_attn_union_min_tiles(n: int) -> int:
@@ -562,6 +646,66 @@ def rope_bwd(r: Rope, d_q_out, d_k_out=None, positions=None, d_q=None, d_k=None,
     return _rope(pisa_rope_bwd, r, d_q_out, d_k_out, positions, d_q, d_k, stream)
 
 
+class _Norm(QKNorm):
+    """A pisa_qk_norm that keeps its weights alive."""
+
+
+def make_qk_norm(r: Rope, q_weight=None, k_weight=None, eps=1e-6, offset=0.0):
+    """A pisa_qk_norm for rotations like r; the weights are [d] on the current device, bf16 or float32 (both alike), or
+    None for all ones."""
+    given = [w for w in (q_weight, k_weight) if w is not None]
+    dt = given[0].dtype if given else torch.float32
+    if dt not in _DTYPES:
+        raise ValueError(f"weights are bfloat16 or float32, got {dt}")
+    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if w is not None:
+            _take(w, name, dt, (r.d,), torch.cuda.current_device())
+    m = _Norm(_ptr(q_weight), _ptr(k_weight), _DTYPES[dt], 0, eps, offset)
+    m.weights, m.device = (q_weight, k_weight), torch.cuda.current_device() if given else None
+    return m
+
+
+def _norm_here(m, r: Rope, device):
+    if m.device not in (None, device):
+        raise ValueError(f"the norm's weights are on cuda:{m.device}, the current device is cuda:{device}")
+    for w in m.weights:
+        if w is not None and w.shape[0] != r.d:
+            raise ValueError(f"the norm's weights {tuple(w.shape)} do not fit heads of {r.d}")
+
+
+def norm_rope_fwd(r: Rope, m, q, k=None, positions=None, q_out=None, k_out=None, stream=None):
+    """Norm each head of q and k (make_qk_norm) and turn them as rope_fwd does, in one pass; tensors and results as
+    there."""
+    def turn(r, q, qs, k, ks, positions, q_out, qos, k_out, kos, stream):
+        pisa_norm_rope_fwd(r, m, q, qs, k, ks, positions, q_out, qos, k_out, kos, stream)
+    _norm_here(m, r, torch.cuda.current_device())
+    return _rope(turn, r, q, k, positions, q_out, k_out, stream)
+
+
+def norm_rope_bwd(r: Rope, m, q, k, d_q_out, d_k_out=None, positions=None, d_q=None, d_k=None, stream=None):
+    """The gradients of norm_rope_fwd's inputs and weights from those of its outputs, the inputs q and k as they were:
+    (d_q, d_k, d_q_weight, d_k_weight), the weights' in float32 (None where there is no weight or no side)."""
+    dev = torch.cuda.current_device()
+    _norm_here(m, r, dev)
+    if (q is None) != (d_q_out is None) or (k is None) != (d_k_out is None):
+        raise ValueError("a side comes with its input and its output's gradient, or with neither")
+    dt, like = _TORCH[r.dtype], q if q is not None else k
+    if like is None:
+        raise ValueError("neither q nor k given")
+    qs = None if q is None else _strided(q, "q", dt, (r.B, r.H, r.N, r.d), dev)
+    ks = None if k is None else _strided(k, "k", dt, (r.B, r.Hkv, r.N, r.d), dev)
+    want = [x is not None and w is not None for x, w in zip((q, k), m.weights)]
+    nb = pisa_norm_rope_bwd_workspace_bytes(r) if any(want) else 0
+    with _on(stream, like.device):
+        dw = [torch.empty(r.d, dtype=torch.float32, device=like.device) if x else None for x in want]
+        ws = _workspace(nb, like.device)
+
+    def turn(r, gq, gqs, gk, gks, positions, d_q, dqs, d_k, dks, stream):
+        pisa_norm_rope_bwd(r, m, q, qs, k, ks, gq, gqs, gk, gks, positions, d_q, dqs, d_k, dks, *dw, ws, nb, stream)
+    d_q, d_k = _rope(turn, r, d_q_out, d_k_out, positions, d_q, d_k, stream)
+    return d_q, d_k, *_results(stream, *dw)
+
+
 class QCache:
     """The buffers of an 8-bit key/value cache (pisa_qcache): uint8 codes k [B, Hkv, M, C, d] and v [B, Hkv, M, d, C],
     float32 scales [B, Hkv, M], and for appending the raw rows of the last block, [B, Hkv, C, d]."""
@@ -652,3 +796,92 @@ def qcache_attn_fwd(p: Problem, cache: QCache, q, block_idx, stream=None):
         ws = _workspace(nb, q.device)
     pisa_qcache_attn_fwd(p, cache, q, block_idx, o, lse, ws, nb, stream)
     return _results(stream, o, lse)
+
+
+# ------------------------------------------------------------- drafted tokens ---
+
+def draft_layout(parents, n: int, stream=None):
+    """(mask, positions) of trees of drafted tokens after n cached ones, from each token's parent (int32 [B, T]; -1: the
+    last cached token, below -1: padding): mask int64 [B, T, ceil(T / 64)], bit j of row i set where j is i or an ancestor
+    of i; positions int32 [B, T]."""
+    if parents.dim() != 2:
+        raise ValueError(f"parents: expected [B, T], got {tuple(parents.shape)}")
+    B, T = parents.shape
+    _take(parents, "parents", torch.int32, (B, T), torch.cuda.current_device())
+    with _on(stream, parents.device):
+        mask = torch.empty((B, T, (T + 63) // 64), dtype=torch.int64, device=parents.device)
+        positions = torch.empty((B, T), dtype=torch.int32, device=parents.device)
+    pisa_draft_layout(B, T, parents, n, mask, positions, stream)
+    return _results(stream, mask, positions)
+
+
+def _draft_attn(call, nb, p: Problem, q, block_idx, k_new, v_new, mask, o, lse, ws, stream, dev):
+    dt, T = _TORCH[p.dtype], p.Nq
+    _take(q, "q", dt, (p.B, p.H, T, p.d), dev)
+    _take(block_idx, "block_idx", torch.int32, (p.B, p.Hkv, T, p.K), dev)
+    shape = (p.B, p.Hkv, T, p.d)
+    ks, vs = _strided(k_new, "k_new", dt, shape, dev), _strided(v_new, "v_new", dt, shape, dev)
+    W = (T + 63) // 64
+    shared = mask.dim() == 2
+    _take(mask, "mask", torch.int64, (T, W) if shared else (p.B, T, W), dev)
+    with _on(stream, q.device):
+        mine = [torch.empty_like(q) if o is None else None,
+                torch.empty((p.B, p.H, T), dtype=torch.float32, device=q.device) if lse is None else None]
+        ws = _workspace(nb, q.device) if ws is None else ws
+    _results(stream, *mine)
+    o = mine[0] if o is None else _take(o, "o", dt, (p.B, p.H, T, p.d), dev)
+    lse = mine[1] if lse is None else _take(lse, "lse", torch.float32, (p.B, p.H, T), dev)
+    call(k_new, ks, v_new, vs, mask, 0 if shared else T * W, o, lse, ws, 0 if ws is None else ws.numel() * ws.element_size(), stream)
+    return o, lse
+
+
+def draft_attn_fwd(p: Problem, q, k, v, block_idx, k_new, v_new, mask, o=None, lse=None, ws=None, stream=None):
+    """Attention of the Nq drafted rows of p over their selected blocks of the N - Nq rows that the cache k, v
+    [B, Hkv, Ncap, d] holds, and over the drafted rows k_new, v_new [B, Hkv, Nq, d] (views with a contiguous last dimension)
+    of their mask (draft_layout's, or one [Nq, W] for the batch).  Returns (o, lse), allocated with the workspace where not
+    given."""
+    dev, shape = torch.cuda.current_device(), (p.B, p.Hkv, p.Ncap or p.N, p.d)
+    _take(k, "k", _TORCH[p.dtype], shape, dev)
+    _take(v, "v", _TORCH[p.dtype], shape, dev)
+    return _draft_attn(lambda *a: pisa_draft_attn_fwd(p, q, k, v, block_idx, *a), pisa_draft_attn_workspace_bytes(p), p, q,
+                       block_idx, k_new, v_new, mask, o, lse, ws, stream, dev)
+
+
+def qcache_draft_attn_fwd(p: Problem, cache: QCache, q, block_idx, k_new, v_new, mask, o=None, lse=None, ws=None, stream=None):
+    """draft_attn_fwd over the 8-bit cache."""
+    cache.check(p)
+    return _draft_attn(lambda *a: pisa_qcache_draft_attn_fwd(p, cache, q, block_idx, *a),
+                       pisa_qcache_draft_attn_workspace_bytes(p), p, q, block_idx, k_new, v_new, mask, o, lse, ws, stream,
+                       cache.device)
+
+
+def _append_args(p: Problem, k_new, v_new, rows, n_old, pyramid, dev):
+    """Strides of the new rows, and how many there are, of an append of chosen rows."""
+    n_rows = k_new.shape[2] if k_new.dim() == 4 else 0
+    shape, dt = (p.B, p.Hkv, n_rows, p.d), _TORCH[p.dtype]
+    ks, vs = _strided(k_new, "k_new", dt, shape, dev), _strided(v_new, "v_new", dt, shape, dev)
+    if rows is not None:
+        _take(rows, "rows", torch.int32, (p.B, p.N - n_old), dev)
+    if pyramid is not None:
+        _take(pyramid, "pyramid", torch.float32, (p.B, p.Hkv, pyramid.shape[2], p.d), dev)
+        if pyramid.numel() * 4 != pisa_pyramid_bytes(p):
+            raise ValueError(f"pyramid: {tuple(pyramid.shape)} does not fit {p}")
+    return ks, vs, n_rows
+
+
+def cache_append_rows(p: Problem, k, v, k_new, v_new, rows, n_old: int, pyramid=None, stream=None):
+    """Rows n_old .. N-1 of the cache k, v [B, Hkv, Ncap, d] from chosen rows of k_new, v_new [B, Hkv, T, d] (views with a
+    contiguous last dimension): rows int32 [B, N - n_old] names them, None takes the first; the pyramid with them where one
+    is given."""
+    dev, shape = torch.cuda.current_device(), (p.B, p.Hkv, p.Ncap or p.N, p.d)
+    _take(k, "k", _TORCH[p.dtype], shape, dev)
+    _take(v, "v", _TORCH[p.dtype], shape, dev)
+    ks, vs, n_rows = _append_args(p, k_new, v_new, rows, n_old, pyramid, dev)
+    pisa_cache_append_rows(p, k, v, k_new, ks, v_new, vs, rows, n_rows, n_old, pyramid, stream)
+
+
+def qcache_append_rows(p: Problem, cache: QCache, k_new, v_new, rows, n_old: int, pyramid=None, stream=None):
+    """qcache_append of chosen rows, as in cache_append_rows."""
+    cache.check(p, appending=True)
+    ks, vs, n_rows = _append_args(p, k_new, v_new, rows, n_old, pyramid, cache.device)
+    pisa_qcache_append_rows(p, cache, k_new, ks, v_new, vs, rows, n_rows, n_old, pyramid, stream)

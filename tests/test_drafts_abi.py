@@ -1,0 +1,208 @@
+"""Norms with rotary positions and drafted tokens at the C ABI, without a GPU: workspace sizes and every refusal (exact
+status, a detail that names the argument) before anything is launched."""
+import ctypes
+
+import pytest
+
+pisa = pytest.importorskip("paper_2609_31093_amd.pisa", reason="libpisa.so not built")
+
+FAKE = 1 << 20  # aligned, non-null addresses far apart; never dereferenced because validation fails first
+INVALID, UNSUPPORTED, WORKSPACE = pisa.PISA_ERR_INVALID_ARG, pisa.PISA_ERR_UNSUPPORTED, pisa.PISA_ERR_WORKSPACE
+LIB = pisa.library()
+AT = {n: (i + 1) << 32 for i, n in enumerate(
+    ("q", "k", "d_q_out", "d_k_out", "d_q", "d_k", "d_q_weight", "d_k_weight", "ws", "w", "v", "idx", "k_new", "v_new", "mask", "o",
+     "lse", "ck", "cv", "cks", "cvs", "cko", "cvo", "pyr", "rows", "parents", "positions"))}
+S = pisa.Strides
+
+
+def at(x):
+    return None if x is None else ctypes.addressof(x)
+
+
+def error():
+    return pisa.pisa_last_error()
+
+
+# ------------------------------------------------------------- norms ---
+
+def rope(**kw):
+    return pisa.make_rope(**{**dict(B=2, H=4, Hkv=2, N=100, d=128), **kw})
+
+
+def norm(q=AT["w"], k=AT["w"] + 4096, dtype=pisa.PISA_DTYPE_BF16, eps=1e-6, offset=0.0, reserved=0):
+    return pisa.QKNorm(q, k, dtype, reserved, eps, offset)
+
+
+def fwd(r=None, m=None, **kw):
+    a = {**dict(q=AT["q"], qs=None, k=AT["k"], ks=None, pos=None, qo=AT["d_q"], qos=None, ko=AT["d_k"], kos=None), **kw}
+    r, m = rope() if r is None else r, norm() if m is None else m
+    return LIB.pisa_norm_rope_fwd(ctypes.byref(r), None if m == "none" else ctypes.byref(m), a["q"], at(a["qs"]), a["k"], at(a["ks"]),
+                                  a["pos"], a["qo"], at(a["qos"]), a["ko"], at(a["kos"]), None)
+
+
+def bwd(r=None, m=None, **kw):
+    a = {**{n: AT[n] for n in ("q", "k", "d_q_out", "d_k_out", "d_q", "d_k", "d_q_weight", "d_k_weight", "ws")}, "nb": 1 << 30, "pos": None}
+    s = {n: None for n in ("q", "k", "d_q_out", "d_k_out", "d_q", "d_k")}
+    for n, x in kw.items():
+        if n.endswith("_s"):
+            s[n[:-2]] = x
+        else:
+            a[n] = x
+    r, m = rope() if r is None else r, norm() if m is None else m
+    return LIB.pisa_norm_rope_bwd(ctypes.byref(r), ctypes.byref(m), a["q"], at(s["q"]), a["k"], at(s["k"]), a["d_q_out"], at(s["d_q_out"]),
+                                  a["d_k_out"], at(s["d_k_out"]), a["pos"], a["d_q"], at(s["d_q"]), a["d_k"], at(s["d_k"]),
+                                  a["d_q_weight"], a["d_k_weight"], a["ws"], a["nb"], None)
+
+
+@pytest.mark.parametrize("call", [fwd, bwd])
+def test_norm_refuses_bad_descriptors(call):
+    for kw in (dict(eps=0.0), dict(eps=-1.0), dict(eps=float("nan")), dict(eps=1e31), dict(offset=float("inf")), dict(dtype=2),
+               dict(reserved=1), dict(q=AT["w"] + 2)):
+        assert call(m=norm(**kw)) == INVALID and error(), kw
+    r = rope()
+    r.rot = 3
+    assert call(r=r) == INVALID
+    assert call(r=rope(d=64), m=norm(dtype=7)) == INVALID
+
+
+def test_norm_fwd_refuses_bad_tensors():
+    assert fwd(m="none") == INVALID
+    assert fwd(q=None) == INVALID and "q" in error()
+    assert fwd(q=None, k=None, qo=None, ko=None) == INVALID
+    assert fwd(pos=AT["positions"] + 2) == INVALID and "positions" in error()
+    assert fwd(qo=AT["w"]) == INVALID and "q_weight" in error()          # weights that are overwritten
+    assert fwd(qo=AT["k"]) == INVALID and "overlaps" in error()
+    assert fwd(qo=AT["d_q"], ko=AT["d_q"] + 256) == INVALID and "overlaps" in error()
+    assert fwd(qos=S(0, 100 * 128, 128)) == INVALID and "overlap" in error()
+    assert fwd(qs=S(4, 4, 4)) == INVALID and "strides" in error()
+    # one side whose weights lie in the other's unused output
+    assert fwd(k=None, ko=AT["d_k"]) == INVALID
+
+
+def test_norm_bwd_refuses_bad_tensors():
+    for side in ("q", "k"):
+        for n in (side, f"d_{side}_out", f"d_{side}"):
+            assert bwd(**{n: None}) == INVALID and error(), n
+        assert bwd(**{side: None, f"d_{side}_out": None, f"d_{side}": None}) == INVALID and "weight" in error()
+    assert bwd(nb=pisa.pisa_norm_rope_bwd_workspace_bytes(rope()) - 1) == WORKSPACE
+    assert bwd(ws=None) == WORKSPACE
+    assert bwd(ws=AT["ws"] + 16) == INVALID
+    assert bwd(d_q=AT["q"]) == INVALID and "d_q overlaps q" in error()
+    assert bwd(d_q=AT["k"] + 256) == INVALID and "d_q overlaps k" in error()
+    assert bwd(d_q=AT["d_k"]) == INVALID
+    assert bwd(d_q_weight=AT["w"]) == INVALID and "q_weight" in error()
+    assert bwd(d_k_weight=AT["d_q_weight"] + 256) == INVALID
+    assert bwd(ws=AT["d_q"]) == INVALID and "workspace" in error()
+    assert bwd(d_q_weight=AT["d_q"] + 1024) == INVALID
+    assert bwd(d_q=AT["d_q_out"], d_q_s=S(4 * 128 * 100, 128, 4 * 128)) == INVALID and "in place" in error()
+
+
+def test_norm_workspace_serves_every_choice_of_sides():
+    """One size for both sides, or one of them: never less than the partial sums of any of them."""
+    for kw in (dict(), dict(B=1, H=1, Hkv=1, N=1), dict(B=1, H=32, Hkv=2, N=5000), dict(B=8, H=16, Hkv=16, N=4096, d=64)):
+        nb = pisa.pisa_norm_rope_bwd_workspace_bytes(rope(**kw))
+        assert 0 < nb <= 64 << 20
+    r = rope()
+    r.rot = 1
+    assert pisa.pisa_norm_rope_bwd_workspace_bytes(r) == 0
+
+
+# ------------------------------------------------------------ drafts ---
+
+def problem(**kw):
+    return pisa.make_problem(**{**dict(B=2, H=4, Hkv=2, Nq=20, N=1020, d=128, C=64, fanout=2, K=4, causal=1, dtype="bf16", Ncap=1024), **kw})
+
+
+def cache(**kw):
+    f = {**dict(k=AT["ck"], v=AT["cv"], k_scale=AT["cks"], v_scale=AT["cvs"], k_open=AT["cko"], v_open=AT["cvo"]), **kw}
+    return pisa.QCacheBuffers(*(f[n] for n in ("k", "v", "k_scale", "v_scale", "k_open", "v_open")))
+
+
+def attend(eight, p=None, c=None, **kw):
+    a = {**{n: AT[n] for n in ("q", "k", "v", "idx", "k_new", "v_new", "mask", "o", "lse", "ws")}, "ks": None, "vs": None, "mb": 20,
+         "nb": 1 << 30, **kw}
+    p = problem() if p is None else p
+    tail = (a["idx"], a["k_new"], at(a["ks"]), a["v_new"], at(a["vs"]), a["mask"], a["mb"], a["o"], a["lse"], a["ws"], a["nb"], None)
+    if eight:
+        c = cache() if c is None else c
+        return LIB.pisa_qcache_draft_attn_fwd(ctypes.byref(p), ctypes.byref(c), a["q"], *tail)
+    return LIB.pisa_draft_attn_fwd(ctypes.byref(p), a["q"], a["k"], a["v"], *tail)
+
+
+@pytest.mark.parametrize("eight", [False, True])
+def test_draft_attention_refuses(eight):
+    for n in ("q", "idx", "k_new", "v_new", "mask", "o") + (() if eight else ("k", "v")):
+        assert attend(eight, **{n: None}) == INVALID and error(), n
+        assert attend(eight, **{n: AT[n] + 8}) == INVALID and "aligned" in error(), n
+    assert attend(eight, lse=AT["lse"] + 4) == INVALID
+    assert attend(eight, p=problem(Nq=1025, N=3000, Ncap=0)) == UNSUPPORTED
+    assert attend(eight, p=problem(d=96)) == UNSUPPORTED
+    assert attend(eight, p=problem(Nq=30, N=20, Ncap=0)) == INVALID
+    for mb in (-1, 1, 19):
+        assert attend(eight, mb=mb) == INVALID and "mask_bstride" in error()
+    assert attend(eight, ks=S(8, 8, 4)) == INVALID and "strides" in error()
+    p = problem(K=64)
+    need = (pisa.pisa_qcache_draft_attn_workspace_bytes if eight else pisa.pisa_draft_attn_workspace_bytes)(p)
+    assert need > 0
+    assert attend(eight, p=p, nb=need - 1) == WORKSPACE
+    assert attend(eight, p=p, ws=None) == WORKSPACE
+    assert attend(eight, p=p, ws=AT["ws"] + 16) == INVALID
+    held = ("ck", "cv", "cks", "cvs") if eight else ("k", "v")
+    for out in ("o", "lse", "ws"):
+        for x in ("q", "idx", "k_new", "v_new", "mask") + held:
+            assert attend(eight, p=p, **{out: AT[x]}) == INVALID and "overlap" in error(), (out, x)
+    assert attend(eight, lse=AT["o"] + 256) == INVALID and attend(eight, p=p, ws=AT["o"]) == INVALID
+    if eight:
+        assert attend(eight, c=cache(k=None)) == INVALID
+        assert attend(eight, c=cache(v_scale=None)) == INVALID
+
+
+def append(eight, p=None, c=None, **kw):
+    a = {**{n: AT[n] for n in ("k", "v", "k_new", "v_new", "rows", "pyr")}, "ks": None, "vs": None, "n": 20, "n_old": 1000, **kw}
+    p = problem(Nq=1) if p is None else p
+    tail = (a["k_new"], at(a["ks"]), a["v_new"], at(a["vs"]), a["rows"], a["n"], a["n_old"], a["pyr"], None)
+    if eight:
+        c = cache() if c is None else c
+        return LIB.pisa_qcache_append_rows(ctypes.byref(p), ctypes.byref(c), *tail)
+    return LIB.pisa_cache_append_rows(ctypes.byref(p), a["k"], a["v"], *tail)
+
+
+@pytest.mark.parametrize("eight", [False, True])
+def test_append_of_rows_refuses(eight):
+    for n_old in (-1, 1021):
+        assert append(eight, n_old=n_old) == INVALID and "n_old" in error()
+    assert append(eight, n_old=1020) == 0  # nothing to append: nothing launched
+    for n in (0, -3):
+        assert append(eight, n=n) == INVALID and "n_rows" in error()
+    assert append(eight, rows=None, n=19) == INVALID and "n_rows" in error()
+    assert append(eight, rows=AT["rows"] + 2) == INVALID and "rows" in error()
+    for n in ("k_new", "v_new") + (() if eight else ("k", "v")):
+        assert append(eight, **{n: None}) == INVALID and n in error()
+    assert append(eight, pyr=AT["pyr"] + 8) == INVALID
+    assert append(eight, ks=S(8, 8, 4)) == INVALID and "strides" in error()
+    held = dict(k="ck", v="cv", pyr="pyr") if eight else dict(k="k", v="v", pyr="pyr")
+    for x in held.values():
+        for n in ("k_new", "v_new", "rows"):
+            assert append(eight, **{n: AT[x] + 256}) == INVALID and n in error(), (n, x)
+    assert append(eight, pyr=AT[held["v"]]) == INVALID and "overlap" in error()
+    # a strided row that reaches into the cache from behind another buffer
+    far = S(0, 0, (AT[held["v"]] - AT["q"]) // 2 // 19)
+    assert append(eight, k_new=AT["q"], ks=far) == INVALID
+    if eight:
+        assert append(eight, c=cache(k_open=None)) == INVALID
+    else:
+        assert append(eight, k=AT["v"]) == INVALID
+
+
+def test_layout_refuses():
+    def call(B=2, T=20, parents=AT["parents"], n=100, mask=AT["mask"], positions=AT["positions"]):
+        return LIB.pisa_draft_layout(B, T, parents, n, mask, positions, None)
+    for kw in (dict(B=0), dict(B=65536), dict(T=0), dict(T=1025), dict(n=-1), dict(n=2**31 - 1), dict(parents=None), dict(mask=None),
+               dict(parents=AT["parents"] + 4), dict(mask=AT["mask"] + 8), dict(positions=AT["positions"] + 4),
+               dict(mask=AT["parents"]), dict(positions=AT["mask"] + 16), dict(positions=AT["parents"])):
+        assert call(**kw) == INVALID and error(), kw
+
+
+def test_draft_workspaces_are_zero_for_bad_problems():
+    for f in (pisa.pisa_draft_attn_workspace_bytes, pisa.pisa_qcache_draft_attn_workspace_bytes):
+        assert f(problem(d=96)) == 0 and f(problem(Nq=1025, N=2000, Ncap=0)) == 0

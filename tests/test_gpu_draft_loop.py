@@ -1,0 +1,120 @@
+"""Drafted trees as a serving loop has them: layout, norm and rotation at the tree's positions, selection from a pyramid
+that does not know the drafts, attention, and the accepted rows into the cache; several rounds, past block borders."""
+import numpy as np
+import pytest
+import torch
+
+import helpers
+import test_gpu_draft_attn as attn
+import test_gpu_norm_rope as norm
+import test_gpu_qcache as base
+
+pytestmark = pytest.mark.gpu
+
+if torch.cuda.is_available():
+    from paper_2609_31093_amd import pisa
+
+
+def random_parents(B, T, rng):
+    return np.array([[-1] + [int(rng.integers(max(0, i - 4), i)) for i in range(1, T)] for _ in range(B)], np.int32)
+
+
+@pytest.mark.parametrize("eight", [False, True], ids=["raw", "8bit"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,H,Hkv,d,C,g,K,n0", [(2, 4, 2, 64, 32, 2, 5, 245), (1, 8, 8, 128, 64, 2, 6, 1000), (1, 4, 1, 64, 32, 4, 4, 2040)])
+def test_rounds(eight, dtype, B, H, Hkv, d, C, g, K, n0):
+    T, rounds, rng = 20, 5, np.random.default_rng(1)
+    cap, n = n0 + 200, n0
+    w = [norm.weights(d, i, dtype, 0.0) for i in (1, 2)]
+    pn = base.problem(B, H, Hkv, 1, n, d, C, g, K, 1, dtype, cap)
+    rope = pisa.make_rope(B, H, Hkv, n0, d, dtype=dtype)
+    qk = pisa.make_qk_norm(rope, *w)
+    # the prompt
+    _, k = pisa.norm_rope_fwd(rope, qk, None, base.normal((B, Hkv, n0, d), 3, dtype))
+    v = base.normal((B, Hkv, n0, d), 4, dtype)
+    kept_k, kept_v = [k], [v]
+    pyr = base.new_pyramid(pn)
+    if eight:
+        cache = pisa.make_qcache(pn)
+        pisa.qcache_append(pn, cache, k, v, 0, pyr)
+    else:
+        cache = tuple(torch.full((B, Hkv, cap, d), float("nan"), dtype=base.TYPES[dtype], device="cuda") for _ in range(2))
+        pisa.cache_append_rows(pn, *cache, k, v, None, 0, pyr)
+    rope = pisa.make_rope(B, H, Hkv, T, d, dtype=dtype)
+    for i in range(rounds):
+        p = base.problem(B, H, Hkv, T, n + T, d, C, g, K, 1, dtype, cap)
+        parents = random_parents(B, T, rng)
+        mask, pos = pisa.draft_layout(torch.from_numpy(parents).cuda(), n)
+        packed = base.normal((B, T, H + 2 * Hkv, d), 10 + i, dtype)
+        q_in, k_in, v_new = (packed[:, :, a:b].transpose(1, 2) for a, b in ((0, H), (H, H + Hkv), (H + Hkv, H + 2 * Hkv)))
+        q, k_new = pisa.norm_rope_fwd(rope, qk, q_in, k_in, pos)
+        at = pos.cpu().numpy()
+        for x, y, ww in ((q_in, q, w[0]), (k_in, k_new, w[1])):
+            want, size, _ = norm.forward(norm.numbers(x), norm.numbers(ww), at, rope, "half", 1e-6)
+            norm.near(y, want, (2.0 ** -19 + 2.0 ** -21) * size, dtype)
+        # nodes that the cached tokens do not reach are NaN, as are the rows: neither is read
+        idx = pisa.select_flat_bsa(p, q, pyr) if eight else pisa.select(p, q, cache[0], pyr)
+        helpers.check_valid_all_rows(idx, n + T, T, C, K, True)
+        clean = torch.nan_to_num(pyr, 0.5)
+        again = pisa.select_flat_bsa(p, q, clean) if eight else pisa.select(p, q, torch.nan_to_num(cache[0], 0.5), clean)
+        assert torch.equal(idx, again)
+        o, lse = attn.attend(p, cache, q, idx, k_new, v_new, mask)
+        attn.check(p, cache, q, idx, k_new, v_new, mask, o, lse)
+        # a path down each tree is accepted: as many tokens of each, by chance of any depth
+        paths = []
+        for b in range(B):
+            path = [int(rng.integers(T // 2, T))]
+            while parents[b, path[0]] >= 0:
+                path.insert(0, int(parents[b, path[0]]))
+            paths.append(path)
+        m = min(len(x) for x in paths)
+        rows = torch.tensor([x[:m] for x in paths], dtype=torch.int32, device="cuda")
+        pm = base.problem(B, H, Hkv, 1, n + m, d, C, g, K, 1, dtype, cap)
+        if eight:
+            pisa.qcache_append_rows(pm, cache, k_new, v_new, rows, n, pyr)
+        else:
+            pisa.cache_append_rows(pm, *cache, k_new, v_new, rows, n, pyr)
+        pick = rows.long()[:, None, :, None].expand(-1, Hkv, -1, d)
+        kept_k.append(k_new.gather(2, pick))
+        kept_v.append(v_new.gather(2, pick))
+        assert bool((pos.gather(1, rows.long()) == n + torch.arange(m, device="cuda")).all()), "positions of what is kept"
+        n += m
+    k, v = torch.cat(kept_k, 2), torch.cat(kept_v, 2)
+    assert n // C > n0 // C, "past a block's border"
+    pm = base.problem(B, H, Hkv, 1, n, d, C, g, K, 1, dtype, cap)
+    want = base.new_pyramid(pm)
+    if eight:
+        base.check_cache(pm, cache, k, v)
+    else:
+        assert torch.equal(cache[0][:, :, :n], k) and torch.equal(cache[1][:, :, :n], v)
+        assert bool(torch.isnan(cache[0][:, :, n:]).all())
+    full = torch.nn.functional.pad(k, (0, 0, 0, cap - n)).contiguous()
+    pisa.pisa_build_pyramid(pm, full, want)
+    used = torch.isfinite(want)
+    assert torch.equal(pyr[used], want[used])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_chain_is_causal_attention(dtype):
+    """A tree without branches attends as the rows of a cache that holds them do."""
+    B, H, Hkv, T, n, d, C, K = 2, 4, 2, 30, 450, 64, 32, 6
+    p = base.problem(B, H, Hkv, T, n + T, d, C, 2, K, 1, dtype, 0)
+    cache, q, new = attn.make(p, False, 1, dtype), base.normal((B, H, T, d), 3, dtype), attn.drafted(p, 5, dtype)
+    chain = torch.arange(-1, T - 1, dtype=torch.int32, device="cuda").expand(B, T).contiguous()
+    mask, pos = pisa.draft_layout(chain, n)
+    assert torch.equal(pos, torch.arange(n, n + T, device="cuda", dtype=torch.int32).expand(B, T))
+    full = [x.clone() for x in cache]
+    for x, y in zip(full, new):
+        x[:, :, n:] = y
+    # rows that attend every block that holds a draft, and others at random
+    rng = np.random.default_rng(2)
+    last = list(range(n // C, (n + T - 1) // C + 1))
+    idx = np.array([[[last + list(rng.permutation(n // C)[:K - len(last)]) for _ in range(T)] for _ in range(Hkv)] for _ in range(B)])
+    idx = torch.from_numpy(idx.astype(np.int32)).cuda()
+    o, lse = pisa.draft_attn_fwd(p, q, *cache, idx, *new, mask)
+    attn.check(p, cache, q, idx, *new, mask, o, lse)
+    want = pisa.sparse_attn_fwd(p, q, *full, idx)
+    # both within the tolerance of the exact result (sparse_attn_fwd: bf16 weights as here)
+    _, _, tol_o, tol_l = attn.reference(p, cache, q, idx, *new, mask)
+    assert (abs((o.double() - want[0].double()).cpu().numpy()) <= 2 * tol_o).all()
+    assert (abs((lse.double() - want[1].double()).cpu().numpy()) <= 2 * tol_l).all()
