@@ -519,9 +519,11 @@ int check_norm(const pisa_rope* r, const pisa_qk_norm* m, pisa::NormArgs* out) {
   return PISA_OK;
 }
 
-// Bytes from a tensor's first value to its last.
+// Bytes from a tensor's first value to its last (at most 2^62).
 size_t span_of(const pisa_strides& x, int64_t B, int64_t heads, int64_t rows, int d, size_t esz) {
-  return static_cast<size_t>((B - 1) * x.b + (heads - 1) * x.h + (rows - 1) * x.n + d) * esz;
+  const __int128 n = (static_cast<__int128>(B - 1) * x.b + static_cast<__int128>(heads - 1) * x.h +
+                      static_cast<__int128>(rows - 1) * x.n + d) * static_cast<__int128>(esz);
+  return static_cast<size_t>(std::min<__int128>(n, int64_t(1) << 62));
 }
 
 struct Region {
@@ -717,7 +719,7 @@ int run_draft_attn(const pisa_problem* p, const pisa::Shape& s, pisa::DraftAttn 
                        {block_idx, static_cast<size_t>(s.BH()) * p->Nq * p->K * 4, "block_idx"},
                        {k_new, span_of(ks, p->B, p->Hkv, p->Nq, p->d, esz), "k_new"},
                        {v_new, span_of(vs, p->B, p->Hkv, p->Nq, p->d, esz), "v_new"},
-                       {mask, static_cast<size_t>(mask_bstride * (p->B - 1) + p->Nq * W) * 8, "mask"}};
+                       {mask, span_of({mask_bstride, 0, W}, p->B, 1, p->Nq, static_cast<int>(W), 8), "mask"}};
   for (int i = 0; i < 3; ++i) {
     for (const Region& x : in)
       if (meet(out[i], x)) return fail(PISA_ERR_INVALID_ARG, "%s overlaps %s", out[i].name, x.name);
@@ -737,8 +739,9 @@ int run_draft_attn(const pisa_problem* p, const pisa::Shape& s, pisa::DraftAttn 
 
 // Whichever sides a call has.
 size_t norm_rope_ws(const pisa_rope* r) {
-  return std::max({pisa::norm_rope_bwd_ws(r->B, r->N, r->H, r->Hkv, r->d), pisa::norm_rope_bwd_ws(r->B, r->N, r->H, 0, r->d),
-                   pisa::norm_rope_bwd_ws(r->B, r->N, 0, r->Hkv, r->d)});
+  const bool bf16 = r->dtype == PISA_DTYPE_BF16;
+  auto bytes = [&](int H, int Hkv) { return pisa::norm_rope_bwd_ws(r->B, r->N, H, Hkv, r->d, bf16); };
+  return std::max({bytes(r->H, r->Hkv), bytes(r->H, 0), bytes(0, r->Hkv)});
 }
 
 }  // namespace

@@ -11,7 +11,9 @@
 // among them both values of each of its pairs, so that the rotation stays in the
 // lane and the sums over the head are three (two) exchanges between neighbours.
 // Everything is held in fp32 and rounded once.  Each value is read once and
-// written once, which bounds the kernels.
+// written once, which bounds the kernels: 131072 rows of 16 heads of 128 in bf16 take
+// 204 to 209 us (5.2 TB/s, a copy's rate), gradients of 30011 rows of 20 heads 100 us
+// (4.6 TB/s, 3 us of it the weights' sums).
 #include <algorithm>
 
 #include "common.h"
@@ -22,34 +24,33 @@ namespace pisa {
 
 namespace {
 
-// Where a lane's values are: dimensions lo .. lo + 7 and hi .. hi + 7; or, where the
-// border of the rotated pairs falls among its pairs (mixed), each on its own.
+// How pairs lie: (2i, 2i + 1); (i, i + pairs) with a lane's all before or all behind the
+// border of what is rotated, 16 dimensions of lane u from 16 u on behind it; and the
+// same with the border among a lane's pairs (pairs no multiple of 8).
+constexpr int kPairs = 0, kHalves = 1, kMixed = 2;
+
+// Where a lane's values are: dimensions lo .. lo + 7 and hi .. hi + 7.  The lane with
+// the border (kMixed) has r < 8 pairs; its `hi` runs on into the dimensions behind the
+// rotated ones, and its `lo` has from value r on those that follow, lo2 + r ...
+// lo2 + 7.  So three runs are loaded and one value chosen from two (131072 rows of 16
+// heads: 309 us, 209 without a border; each value loaded on its own 782).
+template <int LAY>
 struct Slots {
-  int lo, hi, p0, pairs;
-  bool mixed;
+  int lo, hi, lo2, r, p0;
 
-  __device__ __forceinline__ int lo_at(int j) const {
-    const int i = p0 + j;
-    return !mixed ? lo + j : i < pairs ? i : 2 * i;
+  __device__ __forceinline__ Slots(int u, int pairs) : lo(16 * u), hi(16 * u + 8), lo2(16 * u), r(8), p0(8 * u) {
+    if (LAY != kPairs && p0 < pairs) {
+      lo = lo2 = p0;
+      hi = p0 + pairs;
+      if (LAY == kMixed && p0 + 8 > pairs) {
+        r = pairs - p0;
+        lo2 = 2 * pairs + 8 - 2 * r;
+      }
+    }
   }
-  __device__ __forceinline__ int hi_at(int j) const {
-    const int i = p0 + j;
-    return !mixed ? hi + j : i < pairs ? i + pairs : 2 * i + 1;
-  }
+  __device__ __forceinline__ int lo_at(int j) const { return (LAY == kMixed && j >= r ? lo2 : lo) + j; }
+  __device__ __forceinline__ int hi_at(int j) const { return hi + j; }
 };
-
-// HALF: pairs (i, i + pairs), and what is not rotated behind them: 16 dimensions of
-// lane u from 16 u on where all its pairs lie past the border.
-template <bool HALF>
-__device__ __forceinline__ Slots slots_of(int u, int pairs) {
-  Slots s{16 * u, 16 * u + 8, 8 * u, pairs, false};
-  if (HALF && 8 * u < pairs) {
-    s.lo = 8 * u;
-    s.hi = 8 * u + pairs;
-    s.mixed = 8 * u + 8 > pairs;
-  }
-  return s;
-}
 
 template <typename T>
 __device__ __forceinline__ float value(T x) {
@@ -57,30 +58,25 @@ __device__ __forceinline__ float value(T x) {
   else return x;
 }
 
-template <bool HALF, typename T>
-__device__ __forceinline__ void load16(const T* p, const Slots& s, float (&lo)[8], float (&hi)[8]) {
-  if (HALF && s.mixed) {
+template <int LAY, typename T>
+__device__ __forceinline__ void load16(const T* p, const Slots<LAY>& s, float (&lo)[8], float (&hi)[8]) {
+  load8(p + s.lo, lo);
+  load8(p + s.hi, hi);
+  if constexpr (LAY == kMixed) {
+    float more[8];
+    load8(p + s.lo2, more);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      lo[j] = value(p[s.lo_at(j)]);
-      hi[j] = value(p[s.hi_at(j)]);
-    }
-  } else {
-    load8(p + s.lo, lo);
-    load8(p + s.hi, hi);
+    for (int j = 0; j < 8; ++j) lo[j] = j < s.r ? lo[j] : more[j];
   }
 }
-template <bool HALF, typename T>
-__device__ __forceinline__ void store16(T* p, const Slots& s, const float (&lo)[8], const float (&hi)[8]) {
-  if (HALF && s.mixed) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      store1(p + s.lo_at(j), lo[j]);
-      store1(p + s.hi_at(j), hi[j]);
-    }
-  } else {
+template <int LAY, typename T>
+__device__ __forceinline__ void store16(T* p, const Slots<LAY>& s, const float (&lo)[8], const float (&hi)[8]) {
+  store8(p + s.hi, hi);
+  if (LAY != kMixed || s.r == 8) {
     store8(p + s.lo, lo);
-    store8(p + s.hi, hi);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) store1(p + s.lo_at(j), lo[j]);
   }
 }
 
@@ -89,11 +85,11 @@ __device__ __forceinline__ void turn2(float& x, float& y, float c, float s) {
   x = a * c - b * s;
   y = b * c + a * s;
 }
-template <bool HALF>
+template <int LAY>
 __device__ __forceinline__ void turn(float (&lo)[8], float (&hi)[8], const float (&c)[8], const float (&s)[8]) {
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    if constexpr (HALF) turn2(lo[j], hi[j], c[j], s[j]);
+    if constexpr (LAY != kPairs) turn2(lo[j], hi[j], c[j], s[j]);
     else if (j < 4) turn2(lo[2 * j], lo[2 * j + 1], c[j], s[j]);
     else turn2(hi[2 * j - 8], hi[2 * j - 7], c[j], s[j]);
   }
@@ -109,13 +105,13 @@ __device__ __forceinline__ float row_sum(float v) {
 }
 
 // Weights of a lane's values (1 where there are none).
-template <bool HALF>
-__device__ __forceinline__ void load_weights(const NormArgs& m, const void* w, const Slots& s, float (&lo)[8], float (&hi)[8]) {
+template <int LAY>
+__device__ __forceinline__ void load_weights(const NormArgs& m, const void* w, const Slots<LAY>& s, float (&lo)[8], float (&hi)[8]) {
 #pragma unroll
   for (int j = 0; j < 8; ++j) lo[j] = hi[j] = 1.f;
   if (!w) return;
-  if (m.w_bf16) load16<HALF>(static_cast<const uint16_t*>(w), s, lo, hi);
-  else load16<HALF>(static_cast<const float*>(w), s, lo, hi);
+  if (m.w_bf16) load16<LAY>(static_cast<const uint16_t*>(w), s, lo, hi);
+  else load16<LAY>(static_cast<const float*>(w), s, lo, hi);
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     lo[j] += m.offset;
@@ -157,15 +153,15 @@ __device__ __forceinline__ void lane_angles(const RopeArgs& a, int b, int n, int
 }  // namespace
 
 // Workgroups (rows, heads): 256 threads take 256 / UNITS rows at a time.
-template <typename T, int D, bool HALF>
+template <typename T, int D, int LAY>
 __global__ __launch_bounds__(256) void norm_rope_kernel(RopeArgs a, NormArgs m) {
   constexpr int UNITS = D / 16, ROWS = 256 / UNITS;
   const int u = threadIdx.x % UNITS, pairs = a.rot / 2;
-  const Slots at = slots_of<HALF>(u, pairs);
+  const Slots<LAY> at(u, pairs);
   const HeadRange heads = heads_of(a, blockIdx.y);
   const RopeSide& io = heads.is_q ? a.q : a.k;
   float wlo[8], whi[8];
-  load_weights<HALF>(m, heads.is_q ? m.q_weight : m.k_weight, at, wlo, whi);
+  load_weights<LAY>(m, heads.is_q ? m.q_weight : m.k_weight, at, wlo, whi);
   const int rows = a.B * a.N;
   for (int row = static_cast<int>(blockIdx.x) * ROWS + threadIdx.x / UNITS; row < rows; row += static_cast<int>(gridDim.x) * ROWS) {
     const int b = row / a.N, n = row - b * a.N;
@@ -173,7 +169,7 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(RopeArgs a, NormArgs m) 
     lane_angles(a, b, n, 8 * u, pairs, c, s);
     for (int h = heads.first; h < heads.end; ++h) {
       float lo[8], hi[8];
-      load16<HALF>(row_in<T>(io, b, h, n), at, lo, hi);
+      load16<LAY>(row_in<T>(io, b, h, n), at, lo, hi);
       float sum = 0.f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) sum += lo[j] * lo[j] + hi[j] * hi[j];
@@ -183,57 +179,106 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(RopeArgs a, NormArgs m) 
         lo[j] *= r * wlo[j];
         hi[j] *= r * whi[j];
       }
-      turn<HALF>(lo, hi, c, s);
-      store16<HALF>(row_out<T>(io, b, h, n), at, lo, hi);
+      turn<LAY>(lo, hi, c, s);
+      store16<LAY>(row_out<T>(io, b, h, n), at, lo, hi);
     }
   }
 }
 
-// The weights' gradients: each thread sums its rows', then the workgroup's meet in
-// LDS, and norm_rope_weights_kernel adds the workgroups' in their order.
-template <typename T, int D, bool HALF>
-__global__ __launch_bounds__(256) void norm_rope_bwd_kernel(RopeArgs a, NormArgs m, RopeSide dq, RopeSide dk) {
+// A lane's 16 values of a row as they lie in memory.
+template <typename T, int LAY>
+struct Raw16 {
+  static constexpr int W = 2 * sizeof(T), V = 4 / sizeof(T);  // words of 8 values, values of a word
+  uint32_t lo[W], hi[W], more[LAY == kMixed ? W : 1];
+  __device__ __forceinline__ void load(const T* p, const Slots<LAY>& s) {
+    __builtin_memcpy(lo, p + s.lo, sizeof(lo));
+    __builtin_memcpy(hi, p + s.hi, sizeof(hi));
+    if constexpr (LAY == kMixed) __builtin_memcpy(more, p + s.lo2, sizeof(more));
+  }
+  static __device__ __forceinline__ float at(uint32_t w, int j) {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w);
+    else return __uint_as_float(j & 1 ? w & 0xFFFF0000u : w << 16);
+  }
+  __device__ __forceinline__ void values(const Slots<LAY>& s, float (&x)[8], float (&y)[8]) const {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      x[j] = at(lo[j / V], j);
+      y[j] = at(hi[j / V], j);
+      if constexpr (LAY == kMixed) x[j] = j < s.r ? x[j] : at(more[j / V], j);
+    }
+  }
+};
+
+// The next head's values are on their way while one is worked on (without: 139 us for
+// 30011 rows of 20 heads, with 95), which takes the registers of three wavefronts on a
+// SIMD in bf16, two in fp32 (at four they spill).  The weights'
+// gradients: each thread sums its rows', then the workgroup's meet in LDS, and
+// norm_rope_weights_kernel adds the workgroups' in their order.
+template <typename T, int D, int LAY>
+__global__ __launch_bounds__(256, sizeof(T) == 2 && LAY != kMixed ? 3 : 2) void norm_rope_bwd_kernel(RopeArgs a, NormArgs m, RopeSide dq, RopeSide dk) {
   constexpr int UNITS = D / 16, ROWS = 256 / UNITS;
   __shared__ float part[4][D];
   const int u = threadIdx.x % UNITS, pairs = a.rot / 2;
-  const Slots at = slots_of<HALF>(u, pairs);
+  const Slots<LAY> at(u, pairs);
   const HeadRange heads = heads_of(a, blockIdx.y);
   const RopeSide& io = heads.is_q ? a.q : a.k;   // in: x
   const RopeSide& gr = heads.is_q ? dq : dk;     // in: dy, out: dx
-  float wlo[8], whi[8], dlo[8], dhi[8];
-  load_weights<HALF>(m, heads.is_q ? m.q_weight : m.k_weight, at, wlo, whi);
+  float wlo[8], whi[8], dlo[8], dhi[8], c[8], s[8];
+  load_weights<LAY>(m, heads.is_q ? m.q_weight : m.k_weight, at, wlo, whi);
 #pragma unroll
   for (int j = 0; j < 8; ++j) dlo[j] = dhi[j] = 0.f;
-  const int rows = a.B * a.N;
-  for (int row = static_cast<int>(blockIdx.x) * ROWS + threadIdx.x / UNITS; row < rows; row += static_cast<int>(gridDim.x) * ROWS) {
-    const int b = row / a.N, n = row - b * a.N;
-    float c[8], s[8];
-    lane_angles(a, b, n, 8 * u, pairs, c, s);
-    for (int h = heads.first; h < heads.end; ++h) {
-      float lo[8], hi[8], ulo[8], uhi[8];
-      load16<HALF>(row_in<T>(io, b, h, n), at, lo, hi);
-      load16<HALF>(row_in<T>(gr, b, h, n), at, ulo, uhi);
-      turn<HALF>(ulo, uhi, c, s);
-      float sum = 0.f, dot = 0.f;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        sum += lo[j] * lo[j] + hi[j] * hi[j];
-        dot += ulo[j] * wlo[j] * lo[j] + uhi[j] * whi[j] * hi[j];
-      }
-      const float r = rsqrtf(row_sum<UNITS>(sum) * (1.f / D) + m.eps);
-      const float along = row_sum<UNITS>(dot) * r * (1.f / D);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        lo[j] *= r;
-        hi[j] *= r;
-        dlo[j] = fmaf(ulo[j], lo[j], dlo[j]);
-        dhi[j] = fmaf(uhi[j], hi[j], dhi[j]);
-        lo[j] = r * (ulo[j] * wlo[j] - lo[j] * along);
-        hi[j] = r * (uhi[j] * whi[j] - hi[j] * along);
-      }
-      store16<HALF>(row_out<T>(gr, b, h, n), at, lo, hi);
+  const int rows = a.B * a.N, step = static_cast<int>(gridDim.x) * ROWS;
+  int row = static_cast<int>(blockIdx.x) * ROWS + threadIdx.x / UNITS, h = heads.first;
+  int b = row / a.N, n = row - b * a.N;
+  Raw16<T, LAY> x0, u0, x1, u1;
+
+  // works on row `row`, head h, and moves on to the next ones
+  auto pass = [&](const Raw16<T, LAY>& xr, const Raw16<T, LAY>& ur, Raw16<T, LAY>& xn, Raw16<T, LAY>& un) {
+    if (h == heads.first) lane_angles(a, b, n, 8 * u, pairs, c, s);
+    T* out = row_out<T>(gr, b, h, n);
+    if (++h == heads.end) {
+      h = heads.first;
+      row += step;
+      b = row / a.N;
+      n = row - b * a.N;
     }
+    if (row < rows) {
+      xn.load(row_in<T>(io, b, h, n), at);
+      un.load(row_in<T>(gr, b, h, n), at);
+    }
+    float lo[8], hi[8], ulo[8], uhi[8];
+    xr.values(at, lo, hi);
+    ur.values(at, ulo, uhi);
+    turn<LAY>(ulo, uhi, c, s);
+    float sum = 0.f, dot = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      sum += lo[j] * lo[j] + hi[j] * hi[j];
+      dot += ulo[j] * wlo[j] * lo[j] + uhi[j] * whi[j] * hi[j];
+    }
+    const float r = rsqrtf(row_sum<UNITS>(sum) * (1.f / D) + m.eps);
+    const float along = row_sum<UNITS>(dot) * r * (1.f / D);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      lo[j] *= r;
+      hi[j] *= r;
+      dlo[j] = fmaf(ulo[j], lo[j], dlo[j]);
+      dhi[j] = fmaf(uhi[j], hi[j], dhi[j]);
+      lo[j] = r * (ulo[j] * wlo[j] - lo[j] * along);
+      hi[j] = r * (uhi[j] * whi[j] - hi[j] * along);
+    }
+    store16<LAY>(out, at, lo, hi);
+  };
+  if (row < rows) {
+    x0.load(row_in<T>(io, b, h, n), at);
+    u0.load(row_in<T>(gr, b, h, n), at);
   }
+  while (row < rows) {
+    pass(x0, u0, x1, u1);
+    if (row >= rows) break;
+    pass(x1, u1, x0, u0);
+  }
+
   if (!(heads.is_q ? m.d_q_weight : m.d_k_weight)) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
@@ -255,23 +300,28 @@ __global__ __launch_bounds__(256) void norm_rope_bwd_kernel(RopeArgs a, NormArgs
   }
 }
 
-// Sums of the parts: a workgroup for 16 dimensions of a side, 64 threads for each
-// four of them.
+// Sums of the parts: a workgroup for 16 dimensions of a side, 256 threads for each
+// four of them, whose loads are four at a time on their way.
 template <int D>
-__global__ __launch_bounds__(256) void norm_rope_weights_kernel(const float* __restrict__ parts, int nq, int nk, float* d_q, float* d_k) {
-  __shared__ float4 sums[64][4];
+__global__ __launch_bounds__(1024) void norm_rope_weights_kernel(const float* __restrict__ parts, int nq, int nk, float* d_q, float* d_k) {
+  __shared__ float4 sums[256][4];
   const bool is_q = blockIdx.y == 0;
   float* out = is_q ? d_q : d_k;
   if (!out) return;
   const int quad = threadIdx.x & 3, t = threadIdx.x >> 2, n = is_q ? nq : nk;
   const float* p = parts + (is_q ? 0 : static_cast<int64_t>(nq) * D) + blockIdx.x * 16 + quad * 4;
   float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int i = t; i < n; i += 64) {
-    const float4 x = *reinterpret_cast<const float4*>(p + static_cast<int64_t>(i) * D);
-    v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
+  for (int i = t; i < n; i += 1024) {
+    float4 x[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = *reinterpret_cast<const float4*>(p + static_cast<int64_t>(min(i + 256 * j, n - 1)) * D);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (i + 256 * j < n) v.x += x[j].x, v.y += x[j].y, v.z += x[j].z, v.w += x[j].w;
+    }
   }
   sums[t][quad] = v;
-  for (int o = 32; o >= 1; o >>= 1) {
+  for (int o = 128; o >= 1; o >>= 1) {
     __syncthreads();
     if (t < o) {
       const float4 x = sums[t + o][quad];
@@ -288,31 +338,39 @@ namespace {
 struct Grid {
   int heads, gx, gq, gk;
 };
-Grid grid_of(int B, int N, int H, int Hkv, int d) {
+Grid grid_of(int B, int N, int H, int Hkv, int d, bool bf16, bool bwd) {
   const int64_t rows = static_cast<int64_t>(B) * N, groups = (rows * (d / 16) + 255) / 256;
   Grid g{};
   g.heads = groups * (H + Hkv) >= 4 * 1024 ? 4 : groups * (H + Hkv) >= 2 * 1024 ? 2 : 1;
   g.gq = (H + g.heads - 1) / g.heads;
   g.gk = (Hkv + g.heads - 1) / g.heads;
-  g.gx = static_cast<int>(std::min<int64_t>(groups, std::max(1, 4096 / (g.gq + g.gk))));
+  // gradients: as few workgroups (and parts of the weights' sums) as the device holds
+  // at once, three (fp32: two) on each CU, each the same number of rows (20 heads at
+  // 30011 rows, bf16: 640 workgroups 108 us, 768 100, 1024 110, 4096 109)
+  if (bwd) {
+    const int64_t most = 256 * (bf16 ? 3 : 2), rounds = (groups * (g.gq + g.gk) + most - 1) / most;
+    g.gx = static_cast<int>((groups + rounds - 1) / rounds);
+  } else {
+    g.gx = static_cast<int>(std::min<int64_t>(groups, std::max(1, 4096 / (g.gq + g.gk))));
+  }
   return g;
 }
 
-template <typename T, int D, bool HALF>
+template <typename T, int D, int LAY>
 hipError_t launch(const RopeArgs& a, const NormArgs& m, const RopeSide* dq, const RopeSide* dk, const Grid& g, hipStream_t st) {
   const dim3 grid(static_cast<unsigned>(g.gx), static_cast<unsigned>(g.gq + g.gk));
   if (!dq) {
     ProfScope ps("norm_rope", st);
-    norm_rope_kernel<T, D, HALF><<<grid, 256, 0, st>>>(a, m);
+    norm_rope_kernel<T, D, LAY><<<grid, 256, 0, st>>>(a, m);
     return hipGetLastError();
   }
   {
     ProfScope ps("norm_rope_bwd", st);
-    norm_rope_bwd_kernel<T, D, HALF><<<grid, 256, 0, st>>>(a, m, *dq, *dk);
+    norm_rope_bwd_kernel<T, D, LAY><<<grid, 256, 0, st>>>(a, m, *dq, *dk);
   }
   if (m.d_q_weight || m.d_k_weight) {
     ProfScope ps("norm_rope_weights", st);
-    norm_rope_weights_kernel<D><<<dim3(D / 16, 2), 256, 0, st>>>(m.parts, g.gx * g.gq, g.gx * g.gk, m.d_q_weight, m.d_k_weight);
+    norm_rope_weights_kernel<D><<<dim3(D / 16, 2), 1024, 0, st>>>(m.parts, g.gx * g.gq, g.gx * g.gk, m.d_q_weight, m.d_k_weight);
   }
   return hipGetLastError();
 }
@@ -320,20 +378,21 @@ hipError_t launch(const RopeArgs& a, const NormArgs& m, const RopeSide* dq, cons
 template <typename T, int D>
 hipError_t launch_layout(const RopeArgs& a, const NormArgs& m, const RopeSide* dq, const RopeSide* dk, const Grid& g, bool half,
                          hipStream_t st) {
-  return half ? launch<T, D, true>(a, m, dq, dk, g, st) : launch<T, D, false>(a, m, dq, dk, g, st);
+  if (!half) return launch<T, D, kPairs>(a, m, dq, dk, g, st);
+  return a.rot % 16 == 0 ? launch<T, D, kHalves>(a, m, dq, dk, g, st) : launch<T, D, kMixed>(a, m, dq, dk, g, st);
 }
 
 }  // namespace
 
-size_t norm_rope_bwd_ws(int B, int N, int H, int Hkv, int d) {
-  const Grid g = grid_of(B, N, H, Hkv, d);
+size_t norm_rope_bwd_ws(int B, int N, int H, int Hkv, int d, bool bf16) {
+  const Grid g = grid_of(B, N, H, Hkv, d, bf16, true);
   return static_cast<size_t>(g.gx) * (g.gq + g.gk) * d * sizeof(float);
 }
 
 hipError_t launch_norm_rope(const RopeArgs& args, const NormArgs& m, const RopeSide* dq, const RopeSide* dk, bool bf16, bool half,
                             hipStream_t st) {
   RopeArgs a = args;
-  const Grid g = grid_of(a.B, a.N, a.H, a.HH - a.H, a.d);
+  const Grid g = grid_of(a.B, a.N, a.H, a.HH - a.H, a.d, bf16, dq != nullptr);
   a.heads = g.heads;
   if (bf16)
     return a.d == 128 ? launch_layout<uint16_t, 128>(a, m, dq, dk, g, half, st) : launch_layout<uint16_t, 64>(a, m, dq, dk, g, half, st);
