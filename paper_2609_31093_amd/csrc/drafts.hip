@@ -151,13 +151,12 @@ __device__ __forceinline__ void append_block(const BlockRows<T, D, PICK>& src, i
 
 }  // namespace
 
-// A wavefront per changed block and side.  PATH (one block changes and no level is
-// new): a workgroup per (batch, KV head), wavefront 0 for the keys, 1 for the values,
-// the others for the ancestors' unchanged children, as qcache_append_kernel has it.
-template <typename T, int D, bool PATH, bool PICK>
-__global__ __launch_bounds__(256) void cache_append_kernel(CacheAppend a, Geo geo) {
+// A wavefront per changed block and side.  PATH (one or two blocks change): a workgroup per (batch, KV head), a wavefront for the keys and one for the
+// values of each block, and two for the levels, as qcache_append_kernel has it.
+template <typename T, int D, int PATH, bool PICK>
+__global__ __launch_bounds__(PATH == 2 ? 384 : 256) void cache_append_kernel(CacheAppend a, Geo geo, bool grown) {
   constexpr int DPL = D / 16;
-  __shared__ __align__(16) float mean[D];
+  __shared__ __align__(16) float mean[PATH ? PATH : 1][D];
   const int C = geo.C;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int sub = lane & 15, rg = lane >> 4;
@@ -167,7 +166,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheAppend a, Geo ge
   const int leaf = first + unit / 2;
   const bool keys = unit % 2 == 0;
   float* pb = a.pyr + static_cast<int64_t>(bh) * geo.R * D;
-  if (PATH ? wave < 2 : leaf <= last) {
+  if (PATH ? wave < 2 * PATH : leaf <= last) {
     BlockRows<T, D, PICK> src;
     src.cache = static_cast<T*>(keys ? a.k : a.v) + (static_cast<int64_t>(bh) * geo.Nkv + static_cast<int64_t>(leaf) * C) * D + sub * DPL;
     src.fresh = static_cast<const T*>(keys ? a.k_new : a.v_new) + b * (keys ? a.ksb : a.vsb) + h * (keys ? a.ksh : a.vsh) + sub * DPL;
@@ -186,28 +185,30 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheAppend a, Geo ge
         for (int e = 0; e < DPL; e += 4) {
           const float4 v4 = make_float4(m[e], m[e + 1], m[e + 2], m[e + 3]);
           *reinterpret_cast<float4*>(dst + e) = v4;
-          if constexpr (PATH) *reinterpret_cast<float4*>(mean + sub * DPL + e) = v4;
+          if constexpr (PATH > 0) *reinterpret_cast<float4*>(&mean[unit / 2][sub * DPL + e]) = v4;
         }
       }
     } else {
       append_block<T, D, false>(src, nrows, rg, m);
     }
     if (PATH && a.pyr) __syncthreads();
-  } else if (PATH && a.pyr) {
-    path_levels<D>(geo, pb, mean, threadIdx.x - 128);
+  } else if constexpr (PATH > 0) {
+    if (a.pyr) path_levels<D, PATH>(geo, pb, mean, threadIdx.x - 128 * PATH, grown);
   }
 }
 
 template <typename T, int D, bool PICK>
 static hipError_t launch_append(const Geo& geo, const Geo& geo_old, int BH, const CacheAppend& a, hipStream_t st) {
-  const int nleaf = geo.M[1] - a.n_old / geo.C;
-  const bool path = a.n_old > 0 && nleaf == 1 && geo_old.Lstore == geo.Lstore;
+  const int nleaf = geo.M[1] - a.n_old / geo.C, path = path_leaves(geo, a.n_old);
+  const bool grown = geo_old.Lstore != geo.Lstore;  // (n_old > 0)
   {
     ProfScope ps("cache_append", st);
-    if (path)
-      cache_append_kernel<T, D, true, PICK><<<dim3(1, BH), 256, 0, st>>>(a, geo);
+    if (path == 1)
+      cache_append_kernel<T, D, 1, PICK><<<dim3(1, BH), 256, 0, st>>>(a, geo, grown);
+    else if (path == 2)
+      cache_append_kernel<T, D, 2, PICK><<<dim3(1, BH), 384, 0, st>>>(a, geo, grown);
     else
-      cache_append_kernel<T, D, false, PICK><<<dim3((nleaf + 1) / 2, BH), 256, 0, st>>>(a, geo);
+      cache_append_kernel<T, D, 0, PICK><<<dim3((nleaf + 1) / 2, BH), 256, 0, st>>>(a, geo, grown);
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || path || !a.pyr) return e;

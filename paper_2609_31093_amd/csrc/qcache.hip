@@ -277,16 +277,14 @@ __device__ __forceinline__ void keep_raw(const Source<T, D, PICK>& src, T* open,
 
 }  // namespace
 
-// A wavefront per changed block and side.  PATH (only the last block changed and
-// no level is new): a workgroup per (batch, KV head), wavefront 0 for the keys, 1
-// for the values; the others sum the unchanged children of the block's ancestors
-// meanwhile, all levels' loads in flight at once, and take the mean up from
-// there (node_mean's order: children by index, the changed one last).  Otherwise
-// four wavefronts on their own: blocks x {keys, values}.
-template <typename T, int D, int CH, bool PATH, bool PICK>
-__global__ __launch_bounds__(256) void qcache_append_kernel(QAppend a, Geo geo) {
+// A wavefront per changed block and side.  PATH (only the last block or the last two
+// changed): a workgroup per (batch, KV head), a wavefront for the
+// keys and one for the values of each block, and two that update the levels meanwhile
+// (pyramid_path.h).  Otherwise four wavefronts on their own: blocks x {keys, values}.
+template <typename T, int D, int CH, int PATH, bool PICK>
+__global__ __launch_bounds__(PATH == 2 ? 384 : 256) void qcache_append_kernel(QAppend a, Geo geo, bool grown) {
   constexpr int DPL = D / 16;
-  __shared__ __align__(16) float mean[D];
+  __shared__ __align__(16) float mean[PATH ? PATH : 1][D];
   const int C = geo.C;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int sub = lane & 15, rg = lane >> 4;
@@ -297,7 +295,7 @@ __global__ __launch_bounds__(256) void qcache_append_kernel(QAppend a, Geo geo) 
   const bool keys = unit % 2 == 0;
   float* pb = a.pyr + static_cast<int64_t>(bh) * geo.R * D;
 
-  if (PATH ? wave < 2 : leaf <= last) {
+  if (PATH ? wave < 2 * PATH : leaf <= last) {
     Source<T, D, PICK> src;
     T* open = static_cast<T*>(keys ? a.k_open : a.v_open) + static_cast<int64_t>(bh) * C * D + sub * DPL;
     src.open = open;
@@ -319,32 +317,34 @@ __global__ __launch_bounds__(256) void qcache_append_kernel(QAppend a, Geo geo) 
           for (int e = 0; e < DPL; e += 4) {
             const float4 v4 = make_float4(m[e], m[e + 1], m[e + 2], m[e + 3]);
             *reinterpret_cast<float4*>(dst + e) = v4;
-            if constexpr (PATH) *reinterpret_cast<float4*>(mean + sub * DPL + e) = v4;
+            if constexpr (PATH > 0) *reinterpret_cast<float4*>(&mean[unit / 2][sub * DPL + e]) = v4;
           }
         }
-        if constexpr (PATH) __syncthreads();
+        if constexpr (PATH > 0) __syncthreads();
       });
     } else {
-      if constexpr (PATH)
+      if constexpr (PATH > 0)
         if (a.pyr) __syncthreads();
       quantise_block<T, D, false, CH, PICK>(src, C, a.c.v + blk * C * D, a.c.v_scale + blk, lane, [](const float (&)[DPL]) {});
     }
     if (leaf == first) keep_raw<T, D, PICK>(src, open, last * C, geo.N, lane);
-  } else if (PATH && a.pyr) {
-    path_levels<D>(geo, pb, mean, threadIdx.x - 128);
+  } else if constexpr (PATH > 0) {
+    if (a.pyr) path_levels<D, PATH>(geo, pb, mean, threadIdx.x - 128 * PATH, grown);
   }
 }
 
 template <typename T, int D, int CH, bool PICK>
 static hipError_t launch_append(const Geo& geo, const Geo& geo_old, int BH, const QAppend& a, hipStream_t st) {
-  const int first = a.n_old / geo.C, nleaf = geo.M[1] - first;
-  const bool path = a.n_old > 0 && nleaf == 1 && geo_old.Lstore == geo.Lstore;
+  const int nleaf = geo.M[1] - a.n_old / geo.C, path = path_leaves(geo, a.n_old);
+  const bool grown = geo_old.Lstore != geo.Lstore;  // (n_old > 0)
   {
     ProfScope ps("qcache_append", st);
-    if (path) {
-      qcache_append_kernel<T, D, CH, true, PICK><<<dim3(1, BH), 256, 0, st>>>(a, geo);
+    if (path == 1) {
+      qcache_append_kernel<T, D, CH, 1, PICK><<<dim3(1, BH), 256, 0, st>>>(a, geo, grown);
+    } else if (path == 2) {
+      if constexpr (CH == 64 || D == 64) qcache_append_kernel<T, D, CH, 2, PICK><<<dim3(1, BH), 384, 0, st>>>(a, geo, grown);
     } else {
-      qcache_append_kernel<T, D, CH, false, PICK><<<dim3((nleaf + 1) / 2, BH), 256, 0, st>>>(a, geo);
+      qcache_append_kernel<T, D, CH, 0, PICK><<<dim3((nleaf + 1) / 2, BH), 256, 0, st>>>(a, geo, grown);
     }
   }
   const hipError_t e = hipGetLastError();
@@ -353,20 +353,24 @@ static hipError_t launch_append(const Geo& geo, const Geo& geo_old, int BH, cons
 }
 
 // Rows in registers: 64 are 64 registers a lane in bf16 with d = 128 (128 in
-// fp32); bf16 blocks of more than 64 tokens get 128.
-template <typename T, int D>
+// fp32); bf16 blocks of more than 64 tokens get 128, but for two blocks of d = 128 in
+// one workgroup, whose six wavefronts have too few.
+template <typename T, int D, bool PICK>
 static hipError_t launch_append_ch(const Geo& geo, const Geo& geo_old, int BH, const QAppend& a, hipStream_t st) {
   if constexpr (sizeof(T) == 2)
-    if (geo.C > 64)
-      return a.rows ? launch_append<T, D, 128, true>(geo, geo_old, BH, a, st) : launch_append<T, D, 128, false>(geo, geo_old, BH, a, st);
-  return a.rows ? launch_append<T, D, 64, true>(geo, geo_old, BH, a, st) : launch_append<T, D, 64, false>(geo, geo_old, BH, a, st);
+    if (geo.C > 64 && (D == 64 || path_leaves(geo, a.n_old) != 2)) return launch_append<T, D, 128, PICK>(geo, geo_old, BH, a, st);
+  return launch_append<T, D, 64, PICK>(geo, geo_old, BH, a, st);
+}
+template <typename T, int D>
+static hipError_t launch_append_rows(const Geo& geo, const Geo& geo_old, int BH, const QAppend& a, hipStream_t st) {
+  return a.rows ? launch_append_ch<T, D, true>(geo, geo_old, BH, a, st) : launch_append_ch<T, D, false>(geo, geo_old, BH, a, st);
 }
 
 hipError_t launch_qcache_append(const Geo& geo, const Geo& geo_old, int BH, int D, bool bf16, const QAppend& a,
                                 hipStream_t st) {
   if (bf16)
-    return D == 128 ? launch_append_ch<uint16_t, 128>(geo, geo_old, BH, a, st) : launch_append_ch<uint16_t, 64>(geo, geo_old, BH, a, st);
-  return D == 128 ? launch_append_ch<float, 128>(geo, geo_old, BH, a, st) : launch_append_ch<float, 64>(geo, geo_old, BH, a, st);
+    return D == 128 ? launch_append_rows<uint16_t, 128>(geo, geo_old, BH, a, st) : launch_append_rows<uint16_t, 64>(geo, geo_old, BH, a, st);
+  return D == 128 ? launch_append_rows<float, 128>(geo, geo_old, BH, a, st) : launch_append_rows<float, 64>(geo, geo_old, BH, a, st);
 }
 
 }  // namespace pisa

@@ -172,6 +172,37 @@ def test_8bit_append(shape):
         assert torch.equal(torch.nan_to_num(trees[0], 7.0), torch.nan_to_num(trees[1], 7.0))
 
 
+@pytest.mark.parametrize("d,C,dtype", [(64, 32, "f32"), (128, 128, "bf16")])
+@pytest.mark.parametrize("g", [2, 3, 4, 16])
+def test_two_blocks_at_every_count(d, C, dtype, g):
+    """Appends that change the last two blocks, of as many blocks as have them under one node or two at each level."""
+    cap = 40 * C
+    k, v = base.normal((1, 1, cap, d), 1, dtype), base.normal((1, 1, cap, d), 2, dtype)
+    for M in range(2, 38):
+        for n_old, N in (((M - 1) * C - 3, (M - 1) * C + 2), ((M - 2) * C + 1, M * C), ((M - 2) * C, (M - 1) * C + 1)):
+            if n_old == 0:
+                continue
+            p = base.problem(1, 1, 1, 1, N, d, C, g, 3, 1, dtype, cap)
+            want = base.new_pyramid(p)
+            pisa.pisa_build_pyramid(p, k, want)
+            used = torch.isfinite(want)
+            trees = [base.new_pyramid(p) for _ in range(2)]
+            held = [x.clone() for x in (k, v)]
+            for x in held:
+                x[:, :, n_old:] = float("nan")
+            cache = pisa.make_qcache(p)
+            pisa.qcache_append(base.at(p, n_old), cache, k[:, :, :n_old], v[:, :, :n_old], 0, trees[0])
+            pisa.pisa_build_pyramid(base.at(p, n_old), held[0], trees[1])
+            new = [x[:, :, n_old:N] for x in (k, v)]
+            pisa.qcache_append(p, cache, *new, n_old, trees[0])
+            pisa.cache_append_rows(p, *held, *new, None, n_old, trees[1])
+            for tree in trees:
+                assert torch.equal(tree[used], want[used]) and not torch.isfinite(tree[~used]).any(), (M, n_old, N)
+            assert torch.equal(held[0][:, :, :N], k[:, :, :N]) and torch.equal(held[1][:, :, :N], v[:, :, :N])
+    p = base.problem(1, 1, 1, 1, N, d, C, g, 3, 1, dtype, cap)
+    base.check_cache(p, cache, k[:, :, :N], v[:, :, :N])
+
+
 @pytest.mark.parametrize("eight", [False, True])
 def test_append_nothing(eight):
     p = base.problem(2, 1, 1, 1, 100, 64, 32, 2, 4, 1, "bf16", 200)
