@@ -180,23 +180,26 @@ def library():
 def _ptr(x):
     if x is None:
         return None
-    if isinstance(x, int):
-        return x
-    return x.data_ptr()
+    try:
+        return x.data_ptr()
+    except AttributeError:
+        return x  # an address
 
 
 def _at(x):
     return None if x is None else ctypes.addressof(x)
 
 
-# the current stream's handle without the Stream object that torch.cuda.current_stream() builds (0.1 us against 2.7)
+# the current stream's handle without the Stream object that torch.cuda.current_stream() builds (0.1 us against 2.7), and
+# the current device without the question whether a GPU is in use yet
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream(stream):
     if stream is None:
         if _raw_stream is not None:
-            return _raw_stream(torch.cuda.current_device())
+            return _raw_stream(_device())
         return torch.cuda.current_stream().cuda_stream
     if isinstance(stream, int):
         return stream
@@ -620,7 +623,7 @@ def _side(x, y, name, dtype, shape, device, stream):
 
 
 def _rope(turn, r: Rope, q, k, positions, q_out, k_out, stream):
-    dt, dev, B, N, d = _TORCH[r.dtype], torch.cuda.current_device(), r.B, r.N, r.d
+    dt, dev, B, N, d = _TORCH[r.dtype], _device(), r.B, r.N, r.d
     if positions is not None:
         shared = positions.dim() == 1
         _take(positions, "positions", torch.int32, (N,) if shared else (B, N), dev)
@@ -659,18 +662,16 @@ def make_qk_norm(r: Rope, q_weight=None, k_weight=None, eps=1e-6, offset=0.0):
         raise ValueError(f"weights are bfloat16 or float32, got {dt}")
     for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
         if w is not None:
-            _take(w, name, dt, (r.d,), torch.cuda.current_device())
+            _take(w, name, dt, (r.d,), _device())
     m = _Norm(_ptr(q_weight), _ptr(k_weight), _DTYPES[dt], 0, eps, offset)
-    m.weights, m.device = (q_weight, k_weight), torch.cuda.current_device() if given else None
+    m.weights, m.place = (q_weight, k_weight), (_device(), r.d) if given else None
     return m
 
 
-def _norm_here(m, r: Rope, device):
-    if m.device not in (None, device):
-        raise ValueError(f"the norm's weights are on cuda:{m.device}, the current device is cuda:{device}")
-    for w in m.weights:
-        if w is not None and w.shape[0] != r.d:
-            raise ValueError(f"the norm's weights {tuple(w.shape)} do not fit heads of {r.d}")
+def _norm_here(m, r: Rope):
+    if m.place is not None and m.place != (_device(), r.d):
+        raise ValueError(f"the norm's weights are on cuda:{m.place[0]} for heads of {m.place[1]}, the call is on cuda:{_device()} "
+                         f"for heads of {r.d}")
 
 
 def norm_rope_fwd(r: Rope, m, q, k=None, positions=None, q_out=None, k_out=None, stream=None):
@@ -678,32 +679,33 @@ def norm_rope_fwd(r: Rope, m, q, k=None, positions=None, q_out=None, k_out=None,
     there."""
     def turn(r, q, qs, k, ks, positions, q_out, qos, k_out, kos, stream):
         pisa_norm_rope_fwd(r, m, q, qs, k, ks, positions, q_out, qos, k_out, kos, stream)
-    _norm_here(m, r, torch.cuda.current_device())
+    _norm_here(m, r)
     return _rope(turn, r, q, k, positions, q_out, k_out, stream)
 
 
 def norm_rope_bwd(r: Rope, m, q, k, d_q_out, d_k_out=None, positions=None, d_q=None, d_k=None, stream=None):
     """The gradients of norm_rope_fwd's inputs and weights from those of its outputs, the inputs q and k as they were:
     (d_q, d_k, d_q_weight, d_k_weight), the weights' in float32 (None where there is no weight or no side)."""
-    dev = torch.cuda.current_device()
-    _norm_here(m, r, dev)
+    _norm_here(m, r)
     if (q is None) != (d_q_out is None) or (k is None) != (d_k_out is None):
         raise ValueError("a side comes with its input and its output's gradient, or with neither")
-    dt, like = _TORCH[r.dtype], q if q is not None else k
+    dt, dev, like = _TORCH[r.dtype], _device(), q if q is not None else k
     if like is None:
         raise ValueError("neither q nor k given")
     qs = None if q is None else _strided(q, "q", dt, (r.B, r.H, r.N, r.d), dev)
     ks = None if k is None else _strided(k, "k", dt, (r.B, r.Hkv, r.N, r.d), dev)
     want = [x is not None and w is not None for x, w in zip((q, k), m.weights)]
-    nb = pisa_norm_rope_bwd_workspace_bytes(r) if any(want) else 0
-    with _on(stream, like.device):
-        dw = [torch.empty(r.d, dtype=torch.float32, device=like.device) if x else None for x in want]
-        ws = _workspace(nb, like.device)
+    dw, ws, nb = (None, None), None, 0
+    if any(want):  # both in one tensor
+        nb = pisa_norm_rope_bwd_workspace_bytes(r)
+        with _on(stream, like.device):
+            dw, ws = torch.empty((2, r.d), dtype=torch.float32, device=like.device), _workspace(nb, like.device)
+        _results(stream, dw)
+        dw = [x if w else None for x, w in zip(dw.unbind(), want)]
 
     def turn(r, gq, gqs, gk, gks, positions, d_q, dqs, d_k, dks, stream):
         pisa_norm_rope_bwd(r, m, q, qs, k, ks, gq, gqs, gk, gks, positions, d_q, dqs, d_k, dks, *dw, ws, nb, stream)
-    d_q, d_k = _rope(turn, r, d_q_out, d_k_out, positions, d_q, d_k, stream)
-    return d_q, d_k, *_results(stream, *dw)
+    return *_rope(turn, r, d_q_out, d_k_out, positions, d_q, d_k, stream), *dw
 
 
 class QCache:
@@ -734,8 +736,8 @@ class QCache:
         B, H, M, C, d = self._shape
         if (B, H, C, d) != (p.B, p.Hkv, p.C, p.d) or M != -(-(p.Ncap or p.N) // C):
             raise ValueError(f"the cache's codes {self._shape} do not fit {p}")
-        if self.device != torch.cuda.current_device():
-            raise ValueError(f"the cache is on cuda:{self.device}, the current device is cuda:{torch.cuda.current_device()}")
+        if self.device != _device():
+            raise ValueError(f"the cache is on cuda:{self.device}, the current device is cuda:{_device()}")
         if appending and (self.k_open is None or self.k_open.dtype != _TORCH[p.dtype]):
             raise ValueError("appending needs k_open and v_open in the problem's dtype")
 
@@ -807,7 +809,7 @@ def draft_layout(parents, n: int, stream=None):
     if parents.dim() != 2:
         raise ValueError(f"parents: expected [B, T], got {tuple(parents.shape)}")
     B, T = parents.shape
-    _take(parents, "parents", torch.int32, (B, T), torch.cuda.current_device())
+    _take(parents, "parents", torch.int32, (B, T), _device())
     with _on(stream, parents.device):
         mask = torch.empty((B, T, (T + 63) // 64), dtype=torch.int64, device=parents.device)
         positions = torch.empty((B, T), dtype=torch.int32, device=parents.device)
@@ -815,23 +817,24 @@ def draft_layout(parents, n: int, stream=None):
     return _results(stream, mask, positions)
 
 
-def _draft_attn(call, nb, p: Problem, q, block_idx, k_new, v_new, mask, o, lse, ws, stream, dev):
-    dt, T = _TORCH[p.dtype], p.Nq
-    _take(q, "q", dt, (p.B, p.H, T, p.d), dev)
-    _take(block_idx, "block_idx", torch.int32, (p.B, p.Hkv, T, p.K), dev)
-    shape = (p.B, p.Hkv, T, p.d)
-    ks, vs = _strided(k_new, "k_new", dt, shape, dev), _strided(v_new, "v_new", dt, shape, dev)
-    W = (T + 63) // 64
+def _draft_attn(entry, workspace_bytes, p: Problem, cache, q, block_idx, k_new, v_new, mask, o, lse, ws, stream, dev):
+    dt, B, H, Hkv, T, d = _TORCH[p.dtype], p.B, p.H, p.Hkv, p.Nq, p.d
+    W, rows, new = (T + 63) // 64, (B, H, T, d), (B, Hkv, T, d)
+    _take(q, "q", dt, rows, dev)
+    _take(block_idx, "block_idx", torch.int32, (B, Hkv, T, p.K), dev)
+    ks, vs = _strided(k_new, "k_new", dt, new, dev), _strided(v_new, "v_new", dt, new, dev)
     shared = mask.dim() == 2
-    _take(mask, "mask", torch.int64, (T, W) if shared else (p.B, T, W), dev)
-    with _on(stream, q.device):
-        mine = [torch.empty_like(q) if o is None else None,
-                torch.empty((p.B, p.H, T), dtype=torch.float32, device=q.device) if lse is None else None]
-        ws = _workspace(nb, q.device) if ws is None else ws
-    _results(stream, *mine)
-    o = mine[0] if o is None else _take(o, "o", dt, (p.B, p.H, T, p.d), dev)
-    lse = mine[1] if lse is None else _take(lse, "lse", torch.float32, (p.B, p.H, T), dev)
-    call(k_new, ks, v_new, vs, mask, 0 if shared else T * W, o, lse, ws, 0 if ws is None else ws.numel() * ws.element_size(), stream)
+    _take(mask, "mask", torch.int64, (T, W) if shared else (B, T, W), dev)
+    if o is None or lse is None or ws is None:
+        with _on(stream, q.device):
+            ws = _workspace(workspace_bytes(p), q.device) if ws is None else ws
+            mine = [torch.empty_like(q) if o is None else None,
+                    torch.empty((B, H, T), dtype=torch.float32, device=q.device) if lse is None else None]
+        _results(stream, *mine)
+    o = mine[0] if o is None else _take(o, "o", dt, rows, dev)
+    lse = mine[1] if lse is None else _take(lse, "lse", torch.float32, (B, H, T), dev)
+    entry(p, *cache, block_idx, k_new, ks, v_new, vs, mask, 0 if shared else T * W, o, lse, ws,
+          0 if ws is None else ws.nbytes, stream)
     return o, lse
 
 
@@ -840,19 +843,18 @@ def draft_attn_fwd(p: Problem, q, k, v, block_idx, k_new, v_new, mask, o=None, l
     [B, Hkv, Ncap, d] holds, and over the drafted rows k_new, v_new [B, Hkv, Nq, d] (views with a contiguous last dimension)
     of their mask (draft_layout's, or one [Nq, W] for the batch).  Returns (o, lse), allocated with the workspace where not
     given."""
-    dev, shape = torch.cuda.current_device(), (p.B, p.Hkv, p.Ncap or p.N, p.d)
-    _take(k, "k", _TORCH[p.dtype], shape, dev)
-    _take(v, "v", _TORCH[p.dtype], shape, dev)
-    return _draft_attn(lambda *a: pisa_draft_attn_fwd(p, q, k, v, block_idx, *a), pisa_draft_attn_workspace_bytes(p), p, q,
-                       block_idx, k_new, v_new, mask, o, lse, ws, stream, dev)
+    dev, dt, shape = _device(), _TORCH[p.dtype], (p.B, p.Hkv, p.Ncap or p.N, p.d)
+    _take(k, "k", dt, shape, dev)
+    _take(v, "v", dt, shape, dev)
+    return _draft_attn(pisa_draft_attn_fwd, pisa_draft_attn_workspace_bytes, p, (q, k, v), q, block_idx, k_new, v_new, mask, o,
+                       lse, ws, stream, dev)
 
 
 def qcache_draft_attn_fwd(p: Problem, cache: QCache, q, block_idx, k_new, v_new, mask, o=None, lse=None, ws=None, stream=None):
     """draft_attn_fwd over the 8-bit cache."""
     cache.check(p)
-    return _draft_attn(lambda *a: pisa_qcache_draft_attn_fwd(p, cache, q, block_idx, *a),
-                       pisa_qcache_draft_attn_workspace_bytes(p), p, q, block_idx, k_new, v_new, mask, o, lse, ws, stream,
-                       cache.device)
+    return _draft_attn(pisa_qcache_draft_attn_fwd, pisa_qcache_draft_attn_workspace_bytes, p, (cache, q), q, block_idx, k_new,
+                       v_new, mask, o, lse, ws, stream, cache.device)
 
 
 def _append_args(p: Problem, k_new, v_new, rows, n_old, pyramid, dev):
@@ -873,7 +875,7 @@ def cache_append_rows(p: Problem, k, v, k_new, v_new, rows, n_old: int, pyramid=
     """Rows n_old .. N-1 of the cache k, v [B, Hkv, Ncap, d] from chosen rows of k_new, v_new [B, Hkv, T, d] (views with a
     contiguous last dimension): rows int32 [B, N - n_old] names them, None takes the first; the pyramid with them where one
     is given."""
-    dev, shape = torch.cuda.current_device(), (p.B, p.Hkv, p.Ncap or p.N, p.d)
+    dev, shape = _device(), (p.B, p.Hkv, p.Ncap or p.N, p.d)
     _take(k, "k", _TORCH[p.dtype], shape, dev)
     _take(v, "v", _TORCH[p.dtype], shape, dev)
     ks, vs, n_rows = _append_args(p, k_new, v_new, rows, n_old, pyramid, dev)
