@@ -8,17 +8,26 @@
 // the columns whose row did not select it are masked.  (16 tokens of one head, 16
 // blocks each: 50 blocks together, not 256.)
 //
-// The products are those of qcache_attn.hip, with keys and values straight from the
-// cache into operands, no LDS:
+// The products are those of qcache_attn.hip:
 //   S^T = K q^T      row r of key tile mt is key (r/4) (KU/4) + 4 mt + r%4 of the unit,
 //                    so that lane group grp gets the logits of KU/4 consecutive keys
 //   O^T += V^T P^T   over those keys.  Row r of dimension tile dt is dimension
-//                    r D/16 + dt: a lane then reads D/16 consecutive values of each of
+//                    r D/16 + dt: a lane then needs D/16 consecutive values of each of
 //                    its keys, 16 lanes a whole row, and turns eight keys' values into
-//                    operands by itself (a byte permutation for two of them).
-// The drafted rows, and a bf16 cache, are units of 32 keys on v_mfma_f32_16x16x32_bf16
-// (weights as bf16); fp32 ones take v_mfma_f32_16x16x4_f32, whose operands are one
-// value a lane.  The 8-bit cache is multiplied as qcache_attn.hip does it.
+//                    operands by itself (a byte permutation for two of them); 8-bit
+//                    values lie by dimension already.
+// Keys, and the 8-bit values, go through the wavefront's own LDS (KeyRows), the next
+// unit's being loaded meanwhile.  The drafted rows, and a bf16 cache, are units of 32
+// keys on v_mfma_f32_16x16x32_bf16 (weights as bf16); fp32 ones take
+// v_mfma_f32_16x16x4_f32, whose operands are one value a lane.  The 8-bit cache is
+// multiplied as qcache_attn.hip does it.
+//
+// What bounds it: few tokens the chain of latencies (the list 1.2 us, a unit's loads
+// 1.5 and products 1.6, the wavefronts' sums 1.2; 11.5 us with the second launch for 16
+// tokens of 8 heads over 131072 in 8 bits); many the vector instructions of a unit, half
+// of them conversions and the sums' rescaling (256 tokens of 8 heads on 2 over 523776:
+// 36 us; with operands straight from the cache, whose scattered pieces a CU takes in at
+// 13 bytes a clock, 48).
 //
 // The running maximum is that of the products before the softmax's scale.  Sums of
 // weights times values are held in units of kUnit, so that values up to the type's
@@ -52,6 +61,7 @@ struct DraftAttnArgs {
   int H, Hkv, G, T, n, C, K, Nkv;
   int M;               // blocks of the n cached tokens
   int R;               // rows of a tile
+  int KS;              // wavefronts of a workgroup
   int W;               // words of a mask row
   int BH, splits;
   int tile0;           // first tile of this launch
@@ -67,43 +77,89 @@ constexpr float kHead = Q8 && sizeof(T) == 2 ? 14.f : 0.f;
 template <typename T, bool Q8>
 constexpr float kUnit = Q8 && sizeof(T) == 2 ? 0x1p-30f : 0x1p-16f;
 
-// 32 keys and values in bf16 as a wavefront's lanes hold them.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// Key rows of RB bytes on their way to matrix operands.  An operand's lane holds a part
+// of one key's row, 16 lanes 16 rows: loaded like that, each lane's 16 bytes are a
+// request of their own and a CU takes in 13 bytes a clock.  So a wavefront loads 1 KB in
+// a row, puts it into its own LDS and reads operands from there; a row's pieces are
+// placed so that 8 lanes' reads of 8 rows, as operand() makes them, meet 8 banks.
+template <int RB, int KU>
+struct KeyRows {
+  static constexpr int NP = RB / 16, NL = KU * NP / 64, BYTES = KU * RB;
+  u32x4 r[NL];
+
+  static __device__ __forceinline__ int at(int row, int p) {
+    const int run = (row / (KU / 4)) & 1;
+    return row * NP + (p ^ (NP >= 8 ? (row & 3) | run << 2 : ((row >> 1) & 1) | run << 1));
+  }
+  // ptr(i): row i of the unit
+  template <typename F>
+  __device__ __forceinline__ void load(F ptr, int lane) {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int n = i * 64 + lane, row = n / NP;
+      r[i] = reinterpret_cast<const u32x4*>(ptr(row))[n % NP];
+    }
+  }
+  __device__ __forceinline__ void stage(u32x4* lds, int lane) const {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int n = i * 64 + lane;
+      lds[at(n / NP, n % NP)] = r[i];
+    }
+  }
+  // piece i of lane (col, grp)'s part of key tile mt
+  static __device__ __forceinline__ u32x4 operand(const u32x4* lds, int mt, int i, int col, int grp) {
+    return lds[at((col >> 2) * (KU / 4) + mt * 4 + (col & 3), grp * (NP / 4) + i)];
+  }
+};
+
+// 32 keys and values in bf16.
 template <int D>
 struct Unit16 {
   static constexpr int KU = 32, MT = 2, DT = D / 16, KS = D / 32;
   static constexpr int VW = DT / 2;  // words of a lane's part of a value row
   using Query = bf16x8a[KS][1];
-  uint4 kw[MT][KS];
-  uint32_t vw[8][VW];
+  using Keys = KeyRows<2 * D, KU>;
+  static constexpr int BYTES = Keys::BYTES;  // of LDS
+  Keys keys;
+  uint32_t next[8][VW], vw[8][VW];
 
-  // key(i), value(i): addresses of row i of the unit
+  // key(i), value(i): addresses of row i of the unit.  Values: 16 lanes read a row.
   template <typename FK, typename FV>
-  __device__ __forceinline__ void load(FK key, FV value, int col, int grp) {
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-      const uint4* p = reinterpret_cast<const uint4*>(key((col >> 2) * 8 + mt * 4 + (col & 3)) + grp * (D / 4));
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) kw[mt][ks] = p[ks];
-    }
+  __device__ __forceinline__ void load(FK key, FV value, int lane) {
+    const int col = lane & 15, grp = lane >> 4;
+    keys.load(key, lane);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const uint16_t* p = value(grp * 8 + j) + col * DT;
       if constexpr (VW == 4) {
         const uint4 x = *reinterpret_cast<const uint4*>(p);
-        vw[j][0] = x.x, vw[j][1] = x.y, vw[j][2] = x.z, vw[j][3] = x.w;
+        next[j][0] = x.x, next[j][1] = x.y, next[j][2] = x.z, next[j][3] = x.w;
       } else {
         const uint2 x = *reinterpret_cast<const uint2*>(p);
-        vw[j][0] = x.x, vw[j][1] = x.y;
+        next[j][0] = x.x, next[j][1] = x.y;
       }
     }
   }
-  __device__ __forceinline__ void logits(const Query& q, f32x4a (&s)[MT]) const {
+  // What was loaded becomes the unit that is worked on: its first n keys.
+  __device__ __forceinline__ void stage(u32x4* lds, int lane, int n) {
+    keys.stage(lds, lane);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t live = (lane >> 4) * 8 + j < n ? ~0u : 0u;  // 0 times a NaN would not be 0
+#pragma unroll
+      for (int i = 0; i < VW; ++i) vw[j][i] = next[j][i] & live;
+    }
+  }
+  __device__ __forceinline__ void logits(const u32x4* lds, const Query& q, f32x4a (&s)[MT], int col, int grp) const {
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       s[mt] = f32x4a{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks)
-        s[mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(u4_as_bf16x8(kw[mt][ks]), q[ks][0], s[mt], 0, 0, 0);
+        s[mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8a, Keys::operand(lds, mt, ks, col, grp)), q[ks][0], s[mt], 0, 0, 0);
     }
   }
   // Keeps the compiler from making operands of all values ahead of the weights, which
@@ -113,15 +169,6 @@ struct Unit16 {
     for (int j = 0; j < 8; ++j) {
 #pragma unroll
       for (int i = 0; i < VW; ++i) asm volatile("" : "+v"(vw[j][i]));
-    }
-  }
-  // Clears the values of keys that `bits` does not have.
-  __device__ __forceinline__ void keep(uint32_t bits, int grp) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint32_t live = (bits >> (grp * 8 + j)) & 1u ? ~0u : 0u;
-#pragma unroll
-      for (int i = 0; i < VW; ++i) vw[j][i] &= live;
     }
   }
   __device__ __forceinline__ bool odd() const {  // an infinity or NaN among any lane's values
@@ -145,7 +192,7 @@ struct Unit16 {
     return {u4_as_bf16x8(make_uint4(w[0], w[1], w[2], w[3]))};
   }
   // bits: this lane group's keys whose values count
-  __device__ __forceinline__ f32x4a tile(int dt, const Operand& p, uint32_t bits = ~0u) const {
+  __device__ __forceinline__ f32x4a tile(const u32x4*, int dt, const Operand& p, int, int, uint32_t bits = ~0u) const {
     const uint32_t sel = dt & 1 ? 0x07060302u : 0x05040100u;  // high or low halves
     uint32_t a[4];
 #pragma unroll
@@ -164,46 +211,48 @@ struct Unit32 {
   static constexpr int KU = D == 128 ? 16 : 32, MT = KU / 16, DT = D / 16, KS = D / 4;
   static constexpr int VT = KU / 4;  // keys of a lane group
   using Query = float[KS];
-  float kw[MT][KS], vw[VT][DT];
+  using Keys = KeyRows<4 * D, KU>;
+  static constexpr int BYTES = Keys::BYTES;
+  Keys keys;
+  float next[VT][DT], vw[VT][DT];
 
   template <typename FK, typename FV>
-  __device__ __forceinline__ void load(FK key, FV value, int col, int grp) {
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-      const float4* p = reinterpret_cast<const float4*>(key((col >> 2) * VT + mt * 4 + (col & 3)) + grp * KS);
-#pragma unroll
-      for (int i = 0; i < KS; i += 4) {
-        const float4 x = p[i / 4];
-        kw[mt][i] = x.x, kw[mt][i + 1] = x.y, kw[mt][i + 2] = x.z, kw[mt][i + 3] = x.w;
-      }
-    }
+  __device__ __forceinline__ void load(FK key, FV value, int lane) {
+    const int col = lane & 15, grp = lane >> 4;
+    keys.load(key, lane);
 #pragma unroll
     for (int j = 0; j < VT; ++j) {
       const float4* p = reinterpret_cast<const float4*>(value(grp * VT + j) + col * DT);
 #pragma unroll
       for (int i = 0; i < DT; i += 4) {
         const float4 x = p[i / 4];
-        vw[j][i] = x.x, vw[j][i + 1] = x.y, vw[j][i + 2] = x.z, vw[j][i + 3] = x.w;
+        next[j][i] = x.x, next[j][i + 1] = x.y, next[j][i + 2] = x.z, next[j][i + 3] = x.w;
       }
     }
   }
-  __device__ __forceinline__ void logits(const Query& q, f32x4a (&s)[MT]) const {
+  __device__ __forceinline__ void stage(u32x4* lds, int lane, int n) {
+    keys.stage(lds, lane);
+#pragma unroll
+    for (int j = 0; j < VT; ++j) {
+      const bool live = (lane >> 4) * VT + j < n;
+#pragma unroll
+      for (int i = 0; i < DT; ++i) vw[j][i] = live ? next[j][i] : 0.f;
+    }
+  }
+  __device__ __forceinline__ void logits(const u32x4* lds, const Query& q, f32x4a (&s)[MT], int col, int grp) const {
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       s[mt] = f32x4a{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < KS; ++i) s[mt] = __builtin_amdgcn_mfma_f32_16x16x4f32(kw[mt][i], q[i], s[mt], 0, 0, 0);
+      for (int i = 0; i < KS / 4; ++i) {
+        const u32x4 x = Keys::operand(lds, mt, i, col, grp);
+        const float k[4] = {__uint_as_float(x.x), __uint_as_float(x.y), __uint_as_float(x.z), __uint_as_float(x.w)};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[mt] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[e], q[4 * i + e], s[mt], 0, 0, 0);
+      }
     }
   }
   __device__ __forceinline__ void pin() {}
-  __device__ __forceinline__ void keep(uint32_t bits, int grp) {
-#pragma unroll
-    for (int j = 0; j < VT; ++j) {
-      const bool live = (bits >> (grp * VT + j)) & 1u;
-#pragma unroll
-      for (int i = 0; i < DT; ++i) vw[j][i] = live ? vw[j][i] : 0.f;
-    }
-  }
   __device__ __forceinline__ bool odd() const {
     bool any = false;
 #pragma unroll
@@ -222,7 +271,7 @@ struct Unit32 {
     for (int j = 0; j < VT; ++j) w.t[j] = p[j] * unit;
     return w;
   }
-  __device__ __forceinline__ f32x4a tile(int dt, const Operand& p, uint32_t bits = ~0u) const {
+  __device__ __forceinline__ f32x4a tile(const u32x4*, int dt, const Operand& p, int, int, uint32_t bits = ~0u) const {
     f32x4a x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < VT; ++j)
@@ -231,23 +280,63 @@ struct Unit32 {
   }
 };
 
-// KU8 keys of the 8-bit cache (qcache_unit.h); NT bf16 terms of a query and a weight.
+// KU keys of the 8-bit cache, keys and values by way of LDS; NT bf16 terms of a query
+// and a weight (qcache_unit.h).  Row r of the values' dimension tile dt is dimension
+// r D/16 + dt, as above.
 template <int D, int KU8, int NT>
 struct Unit8 {
   static constexpr int KU = KU8, MT = KU / 16, DT = D / 16, KS = D / 32;
+  static constexpr int NP = KU / 16, NL = D * NP / 64;  // pieces of a dimension's codes
   using Query = bf16x8a[KS][NT];
-  Unit<D, KU, true> u;
+  using Keys = KeyRows<D, KU>;
+  static constexpr int BYTES = Keys::BYTES + D * KU;
+  Keys keys;
+  u32x4 codes[NL];
+  float ksc, vsc, ksc_next, vsc_next;
 
-  __device__ __forceinline__ void pin() { u.pin(); }
-  __device__ __forceinline__ void logits(const Query& q, f32x4a (&s)[MT]) const {
+  // piece p of a dimension: those of 16 lanes' dimensions lie on different banks
+  static __device__ __forceinline__ int at(int dim, int p) { return Keys::BYTES / 16 + ((dim * NP + p) ^ ((dim / DT) & 7)); }
+
+  __device__ __forceinline__ void load(const QCache& c, int64_t cell, int C, int u, int lane) {
+    const uint8_t* kp = c.k + (cell * C + u * KU) * D;
+    const uint8_t* vp = c.v + cell * C * D + u * KU;
+    keys.load([&](int row) { return kp + row * D; }, lane);
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int n = i * 64 + lane;
+      codes[i] = reinterpret_cast<const u32x4*>(vp + n / NP * C)[n % NP];
+    }
+    ksc_next = c.k_scale[cell];
+    vsc_next = c.v_scale[cell];
+  }
+  __device__ __forceinline__ void stage(u32x4* lds, int lane, int n) {
+    keys.stage(lds, lane);
+    ksc = ksc_next;
+    vsc = vsc_next;
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int m = i * 64 + lane, p = m % NP;
+      u32x4 x = codes[i];
+      if (n < KU) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = keep_below(x[e], p * 16 + 4 * e, n);
+      }
+      lds[at(m / NP, p)] = x;
+    }
+  }
+  __device__ __forceinline__ void pin() {}
+  __device__ __forceinline__ void logits(const u32x4* lds, const Query& q, f32x4a (&s)[MT], int col, int grp) const {
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       s[mt] = f32x4a{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const bf16x8a kv = u.key(mt, ks);
+      for (int i = 0; i < KS / 2; ++i) {
+        const u32x4 x = Keys::operand(lds, mt, i, col, grp);
+        const bf16x8a k0 = codes8_bf16(x.x, x.y, ksc), k1 = codes8_bf16(x.z, x.w, ksc);
 #pragma unroll
-        for (int j = 0; j < NT; ++j) s[mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kv, q[ks][j], s[mt], 0, 0, 0);
+        for (int j = 0; j < NT; ++j) s[mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, q[2 * i][j], s[mt], 0, 0, 0);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) s[mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, q[2 * i + 1][j], s[mt], 0, 0, 0);
       }
     }
   }
@@ -264,13 +353,19 @@ struct Unit8 {
       for (int i = 0; i < 8; ++i) x[i] = p[8 * st + i];
       w.t[st].set(x);
     }
-    w.scale = u.vsc * unit;
+    w.scale = vsc * unit;
     return w;
   }
-  __device__ __forceinline__ f32x4a tile(int dt, const Operand& p, uint32_t = ~0u) const {
+  __device__ __forceinline__ f32x4a tile(const u32x4* lds, int dt, const Operand& p, int col, int grp, uint32_t = ~0u) const {
     f32x4a x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int st = 0; st < KU / 32; ++st) x = p.t[st].times(u.template value<NT>(st, dt), x);
+    if constexpr (KU == 64) {
+      const u32x4 v = lds[at(col * DT + dt, grp)];
+      x = p.t[0].times(Weights<NT>::codes(v.x, v.y), x);
+      x = p.t[1].times(Weights<NT>::codes(v.z, v.w), x);
+    } else {
+      const uint2 v = reinterpret_cast<const uint2*>(lds + at(col * DT + dt, grp >> 1))[grp & 1];
+      x = p.t[0].times(Weights<NT>::codes(v.x, v.y), x);
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] *= p.scale;
     return x;
@@ -311,10 +406,11 @@ struct Columns {
   // A unit's values with their weights p.  Columns that see none of the unit keep
   // their sums (their weights of 0 do not hide an infinity or NaN).
   template <typename U>
-  __device__ __forceinline__ void add(const U& u, const typename U::Operand& p, float corr, bool sees, uint32_t bits = ~0u) {
+  __device__ __forceinline__ void add(const U& u, const u32x4* lds, const typename U::Operand& p, float corr, bool sees, int col,
+                                      int grp, uint32_t bits = ~0u) {
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
-      const f32x4a x = u.tile(dt, p, bits);
+      const f32x4a x = u.tile(lds, dt, p, col, grp, bits);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float y = fmaf(o[dt][i], corr, x[i]);
@@ -326,43 +422,45 @@ struct Columns {
 
 __device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; }
 
-// Drafted keys j0 .. j0 + KU - 1; bits: those that this column sees.
-template <typename U, typename T, int D, bool Q8>
-__device__ __forceinline__ void add_drafted(Columns<T, D, Q8>& cs, const DraftAttnArgs& a, const T* kn, const T* vn, int j0,
-                                            uint32_t bits, const typename U::Query& q, int col, int grp) {
-  U u;
+// Drafted keys j0 .. j0 + KU - 1.
+template <typename U, typename T>
+__device__ __forceinline__ void load_drafted(U& u, const DraftAttnArgs& a, const T* kn, const T* vn, int j0, int lane) {
   const int last = a.T - 1;
-  u.load([&](int i) { return kn + min(j0 + i, last) * a.ksn; }, [&](int i) { return vn + min(j0 + i, last) * a.vsn; }, col, grp);
-  const uint32_t real = low_bits(a.T - j0);
-  u.keep(real, grp);
+  u.load([&](int i) { return kn + min(j0 + i, last) * a.ksn; }, [&](int i) { return vn + min(j0 + i, last) * a.vsn; }, lane);
+}
+// bits: those that this column sees.
+template <typename U, typename T, int D, bool Q8>
+__device__ __forceinline__ void add_drafted(Columns<T, D, Q8>& cs, U& u, const u32x4* lds, float qscale2, uint32_t bits,
+                                            const typename U::Query& q, int col, int grp) {
   f32x4a s[U::MT];
-  u.logits(q, s);
+  u.logits(lds, q, s, col, grp);
 #pragma unroll
   for (int mt = 0; mt < U::MT; ++mt) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) s[mt][i] = (bits >> (grp * (U::KU / 4) + 4 * mt + i)) & 1u ? s[mt][i] : -INFINITY;
   }
   float p[4 * U::MT];
-  const float corr = cs.template weigh<U::MT>(s, a.qscale2, p);
+  const float corr = cs.template weigh<U::MT>(s, qscale2, p);
   const typename U::Operand w = u.operand(p, kUnit<T, Q8>);
   u.pin();
   if (u.odd()) {  // a column at a time, without the values that it does not see
 #pragma unroll 1
     for (int c = 0; c < 16; ++c) {
       u.pin();
-      cs.add(u, w, corr, bits != 0 && col == c, static_cast<uint32_t>(__builtin_amdgcn_readlane(bits, c)) >> (grp * (U::KU / 4)));
+      cs.add(u, lds, w, corr, bits != 0 && col == c, col, grp,
+             static_cast<uint32_t>(__builtin_amdgcn_readlane(bits, c)) >> (grp * (U::KU / 4)));
     }
   } else {
-    cs.add(u, w, corr, bits != 0);
+    cs.add(u, lds, w, corr, bits != 0, col, grp);
   }
 }
 
 // A cached unit of which the first `visible` keys exist.
 template <typename U, typename T, int D, bool Q8>
-__device__ __forceinline__ void add_cached(Columns<T, D, Q8>& cs, U& u, float qscale2, int visible, bool sees,
-                                           const typename U::Query& q, int grp) {
+__device__ __forceinline__ void add_cached(Columns<T, D, Q8>& cs, U& u, const u32x4* lds, float qscale2, int visible, bool sees,
+                                           const typename U::Query& q, int col, int grp) {
   f32x4a s[U::MT];
-  u.logits(q, s);
+  u.logits(lds, q, s, col, grp);
   if (__any(!sees) || visible < U::KU) {
 #pragma unroll
     for (int mt = 0; mt < U::MT; ++mt) {
@@ -374,8 +472,21 @@ __device__ __forceinline__ void add_cached(Columns<T, D, Q8>& cs, U& u, float qs
   const float corr = cs.template weigh<U::MT>(s, qscale2, p);
   const typename U::Operand w = u.operand(p, kUnit<T, Q8>);
   u.pin();
-  cs.add(u, w, corr, sees);
+  cs.add(u, lds, w, corr, sees, col, grp);
 }
+
+// Most wavefronts of a workgroup.
+constexpr int kMaxWaves = 8;
+
+// 16-byte pieces of LDS that the list takes.
+__host__ __device__ __forceinline__ int list_pieces(int M, int list) { return ((M + 31) / 32 + list + 1) / 2; }
+
+// LDS of a wavefront's unit.
+template <typename T, int D, bool Q8, int KU>
+constexpr int kStage = Q8 ? (Unit8<D, KU, 1>::BYTES > (sizeof(T) == 4 ? Unit32<D>::BYTES : Unit16<D>::BYTES)
+                                 ? Unit8<D, KU, 1>::BYTES
+                                 : (sizeof(T) == 4 ? Unit32<D>::BYTES : Unit16<D>::BYTES))
+                          : (sizeof(T) == 4 ? Unit32<D>::BYTES : Unit16<D>::BYTES);
 
 // The blocks that any of a tile's rows selected, ascending, and for each the rows
 // that did, in LDS: a bitmap of the cache's blocks, its words' running counts, and
@@ -387,13 +498,23 @@ __device__ __forceinline__ int union_list(const DraftAttnArgs& a, int bh, int ro
   blocks = before + words;
   who = blocks + a.list;
   const int32_t* sel = a.idx + (static_cast<int64_t>(bh) * a.T + row0) * a.K;
+  const int entries = rows * a.K;
+  constexpr int KEEP = 4;  // entries that a thread reads once
+  int kept[KEEP];
+#pragma unroll
+  for (int i = 0; i < KEEP; ++i) {
+    const int e = threadIdx.x + i * nt;
+    kept[i] = e < entries ? sel[e] : -1;
+  }
   for (int i = threadIdx.x; i < words; i += nt) bitmap[i] = 0;
   for (int i = threadIdx.x; i < a.list; i += nt) who[i] = 0;
   __syncthreads();
-  for (int e = threadIdx.x; e < rows * a.K; e += nt) {
-    const int blk = sel[e];
+  auto mark = [&](int blk) {
     if (static_cast<uint32_t>(blk) < static_cast<uint32_t>(a.M)) atomicOr(&bitmap[blk >> 5], 1u << (blk & 31));
-  }
+  };
+#pragma unroll
+  for (int i = 0; i < KEEP; ++i) mark(kept[i]);
+  for (int e = threadIdx.x + KEEP * nt; e < entries; e += nt) mark(sel[e]);
   __syncthreads();
   int total = 0;
   for (int base = 0; base < words; base += 64) {  // every wavefront counts; the first one writes
@@ -408,14 +529,16 @@ __device__ __forceinline__ int union_list(const DraftAttnArgs& a, int bh, int ro
     total += __shfl(incl, 63);
   }
   __syncthreads();
-  for (int e = threadIdx.x; e < rows * a.K; e += nt) {
-    const int blk = sel[e];
+  auto place = [&](int blk, int e) {
     if (static_cast<uint32_t>(blk) < static_cast<uint32_t>(a.M)) {
       const uint32_t at = before[blk >> 5] + __popc(bitmap[blk >> 5] & ((1u << (blk & 31)) - 1u));
       blocks[at] = static_cast<uint32_t>(blk);
       atomicOr(&who[at], 1u << (e / a.K));
     }
-  }
+  };
+#pragma unroll
+  for (int i = 0; i < KEEP; ++i) place(kept[i], threadIdx.x + i * nt);
+  for (int e = threadIdx.x + KEEP * nt; e < entries; e += nt) place(sel[e], e);
   __syncthreads();
   return total;
 }
@@ -460,20 +583,62 @@ __device__ __forceinline__ void store_out(void* o, int64_t at, float x) {
   if constexpr (sizeof(T) == 2) static_cast<uint16_t*>(o)[at] = f32_to_bf16_rne(x);
   else static_cast<float*>(o)[at] = x;
 }
+template <typename T>
+__device__ __forceinline__ void store_out4(void* o, int64_t at, const float (&x)[4]) {
+  if constexpr (sizeof(T) == 2) {
+    uint2 w;
+    w.x = f32_to_bf16_rne(x[0]) | static_cast<uint32_t>(f32_to_bf16_rne(x[1])) << 16;
+    w.y = f32_to_bf16_rne(x[2]) | static_cast<uint32_t>(f32_to_bf16_rne(x[3])) << 16;
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(o) + at) = w;
+  } else {
+    *reinterpret_cast<float4*>(static_cast<float*>(o) + at) = make_float4(x[0], x[1], x[2], x[3]);
+  }
+}
+
+// Where column c (of R G) of a tile is kept: its row of the outputs, or its place among
+// the partials.
+struct Place {
+  int64_t row, part;
+};
+__device__ __forceinline__ Place place_of(const DraftAttnArgs& a, int tile, int bh, int c) {
+  const int b = bh / a.Hkv, h = bh - b * a.Hkv, r = c / a.G;
+  const int64_t at = static_cast<int64_t>(tile) * a.BH + bh;
+  return {(static_cast<int64_t>(b) * a.H + h * a.G + (c - r * a.G)) * a.T + tile * a.R + r,
+          at * (a.R * a.G) + c};
+}
+
+// Four dimensions from dd on of a column's sums, and with the first ones its state.
+template <typename T, int D, bool Q8>
+__device__ __forceinline__ void finish(const DraftAttnArgs& a, const Place& pl, int dd, const float (&x)[4], float top, float l, int split) {
+  if (a.splits == 1) {
+    const float inv = l == 0.f ? 0.f : 1.f / (l * kUnit<T, Q8>);
+    const float y[4] = {l == 0.f ? 0.f : x[0] * inv, l == 0.f ? 0.f : x[1] * inv, l == 0.f ? 0.f : x[2] * inv, l == 0.f ? 0.f : x[3] * inv};
+    store_out4<T>(a.o, pl.row * D + dd, y);
+    if (a.lse && dd == 0) a.lse[pl.row] = row_lse<T, Q8>(top == -INFINITY ? 0.f : top, l, a.qscale2);
+  } else {
+    const int64_t at = pl.part * a.splits + split;
+    *reinterpret_cast<float4*>(a.part_o + at * D + dd) = make_float4(x[0], x[1], x[2], x[3]);
+    if (dd == 0) a.part_ml[at] = make_float2(top, l);
+  }
+}
 
 }  // namespace
 
-// A workgroup of NW wavefronts per (tile of R rows, KV head, split of its units).
-template <typename T, int D, bool Q8, int KU, int NW>
-__global__ __launch_bounds__(NW * 64, 2) void draft_attn_kernel(DraftAttnArgs a) {
+// A workgroup of KS wavefronts per (tile, KV head, split of its units).  The splits of
+// a tile are ranges of its ascending list and neighbours in the grid, which the device
+// deals to its 8 XCDs in turn: where tiles look for the same blocks, an XCD's L2 holds
+// those of its range (256 rows of 8 heads on 2, 32 blocks of 128 each, 13 MB together:
+// 47 us; splits that take every fourth unit 48).
+template <typename T, int D, bool Q8, int KU>
+__global__ __launch_bounds__(kMaxWaves * 64, 2) void draft_attn_kernel(DraftAttnArgs a) {
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int NT = F32 ? 3 : 1, DT = D / 16;
   using Drafted = std::conditional_t<F32, Unit32<D>, Unit16<D>>;
   using Cached = std::conditional_t<Q8, Unit8<D, KU, NT>, Drafted>;
   extern __shared__ __align__(16) uint32_t lds[];
 
-  const int64_t w = blockIdx.x;
-  const int bh = static_cast<int>(w % a.BH), tile = a.tile0 + static_cast<int>(w / a.BH);
+  const int split = static_cast<int>(blockIdx.x % a.splits), w = static_cast<int>(blockIdx.x / a.splits);
+  const int bh = w % a.BH, tile = a.tile0 + w / a.BH;
   const int b = bh / a.Hkv, h = bh - b * a.Hkv;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const int col = lane & 15, grp = lane >> 4;
@@ -490,81 +655,92 @@ __global__ __launch_bounds__(NW * 64, 2) void draft_attn_kernel(DraftAttnArgs a)
     for (int i = 0; i < QW; ++i) qw[i] = on ? reinterpret_cast<const uint4*>(q)[i] : make_uint4(0, 0, 0, 0);
   }
 
-  uint32_t *blocks, *who;
-  const int nblk = union_list(a, bh, row0, rows, lds, blocks, who);
-
   const int chunks = (a.T + Drafted::KU - 1) / Drafted::KU;
-  const int per = a.C / KU, ntask = chunks + nblk * per, step = a.splits * NW;
-  int task = static_cast<int>(blockIdx.y) * NW + wave;
-  Columns<T, D, Q8> cs;
+  const uint64_t* mask = a.mask + b * a.mask_bstride + static_cast<int64_t>(row) * a.W;
+  const T* kn = static_cast<const T*>(a.k_new) + b * a.ksb + h * a.ksh;
+  const T* vn = static_cast<const T*>(a.v_new) + b * a.vsb + h * a.vsh;
+  auto seen = [&](int j0) {  // drafted keys from j0 on that this column sees
+    return on ? static_cast<uint32_t>(mask[j0 >> 6] >> (j0 & 63)) & low_bits(min(Drafted::KU, a.T - j0)) : 0u;
+  };
+  // units are the drafted keys', then the list's; the first ones are on their way while
+  // the list is made
+  Drafted ud;
+  uint32_t bits = 0;
+  const bool early = split == 0 && wave < chunks;
+  if (early) {
+    bits = seen(wave * Drafted::KU);
+    load_drafted(ud, a, kn, vn, wave * Drafted::KU, lane);
+  }
 
-  {  // drafted keys
+  uint32_t *blocks, *who;
+  const int nblk = uniform(union_list(a, bh, row0, rows, lds, blocks, who));
+  u32x4* stage = reinterpret_cast<u32x4*>(lds) + list_pieces(a.M, a.list) + wave * (kStage<T, D, Q8, KU> / 16);
+  const int per = a.C / KU, all = chunks + nblk * per, step = a.KS;
+  const int begin = static_cast<int>(static_cast<int64_t>(all) * split / a.splits);
+  const int end = static_cast<int>(static_cast<int64_t>(all) * (split + 1) / a.splits);
+
+  Columns<T, D, Q8> cs;
+  int t = begin + wave;
+  if (t < min(chunks, end)) {
     typename Drafted::Query q;
     make_query<T>(qw, q);
-    const uint64_t* mask = a.mask + b * a.mask_bstride + static_cast<int64_t>(row) * a.W;
-    const T* kn = static_cast<const T*>(a.k_new) + b * a.ksb + h * a.ksh;
-    const T* vn = static_cast<const T*>(a.v_new) + b * a.vsb + h * a.vsh;
-    for (; task < chunks; task += step) {
-      const int j0 = task * Drafted::KU;
-      const uint32_t word = static_cast<uint32_t>(mask[j0 >> 6] >> (j0 & 63));
-      const uint32_t bits = on ? word & low_bits(min(Drafted::KU, a.T - j0)) : 0u;
-      if (__any(bits != 0)) add_drafted<Drafted, T, D, Q8>(cs, a, kn, vn, j0, bits, q, col, grp);
+    if (!early) {
+      bits = seen(t * Drafted::KU);
+      load_drafted(ud, a, kn, vn, t * Drafted::KU, lane);
+    }
+    for (;;) {
+      if (__any(bits != 0)) {
+        wave_sync();
+        ud.stage(stage, lane, a.T - t * Drafted::KU);
+        wave_sync();
+        add_drafted<Drafted, T, D, Q8>(cs, ud, stage, a.qscale2, bits, q, col, grp);
+      }
+      t += step;
+      if (t >= min(chunks, end)) break;
+      bits = seen(t * Drafted::KU);
+      load_drafted(ud, a, kn, vn, t * Drafted::KU, lane);
     }
   }
 
-  {  // cached keys
+  {
     typename Cached::Query q;
     make_query<T>(qw, q);
-    // the unit of task t: its codes or rows, its visible keys, and whether this column sees it
-    auto fetch = [&](int t, Cached& u, int& visible, bool& sees) {
-      if (t >= ntask) return;
-      const int e = t - chunks, slot = e / per, part = e - slot * per;
+    Cached u;
+    int next_visible = 0;
+    bool next_sees = false;
+    // loads the cached unit of task t: its visible keys, and whether this column sees it
+    auto fetch = [&](int t) {
+      next_visible = 0;
+      if (t >= end) return;
+      const int slot = (t - chunks) / per, part = t - chunks - slot * per;
       const int blk = uniform(blocks[slot]);
       const uint32_t rows_in = static_cast<uint32_t>(uniform(who[slot]));
       const int key0 = blk * a.C + part * KU;
-      visible = min(KU, a.n - key0);
-      sees = on && ((rows_in >> r) & 1u);
-      if (visible <= 0) return;  // the last block's end
+      next_sees = ((rows_in >> r) & 1u) || !on;
+      next_visible = min(KU, a.n - key0);
+      if (next_visible <= 0) return;  // the last block's end
       if constexpr (Q8) {
-        u.u.load(a.c, static_cast<int64_t>(bh) * a.c.M + blk, a.C, part, col, grp);
+        u.load(a.c, static_cast<int64_t>(bh) * a.c.M + blk, a.C, part, lane);
       } else {
         const int64_t first = (static_cast<int64_t>(bh) * a.Nkv + key0) * D;
         const T *kb = static_cast<const T*>(a.k) + first, *vb = static_cast<const T*>(a.v) + first;
-        const int last = visible - 1;
+        const int last = next_visible - 1;
         u.load([&](int i) { return kb + static_cast<uint32_t>(min(i, last) * D); },
-               [&](int i) { return vb + static_cast<uint32_t>(min(i, last) * D); }, col, grp);
+               [&](int i) { return vb + static_cast<uint32_t>(min(i, last) * D); }, lane);
       }
     };
-    auto add = [&](Cached& u, int visible, bool sees) {
-      if (visible <= 0) return;
-      if (visible < KU) {
-        if constexpr (Q8) u.u.clear_from(visible, grp);
-        else u.keep(low_bits(visible), grp);
+    fetch(t);
+    while (t < end) {  // the next unit's loads are in flight while one is added
+      const int visible = next_visible;
+      const bool sees = next_sees;
+      if (visible > 0) {
+        wave_sync();
+        u.stage(stage, lane, visible);
+        wave_sync();
       }
-      add_cached<Cached, T, D, Q8>(cs, u, a.qscale2, visible, sees || !on, q, grp);
-    };
-    Cached ua;
-    int na = 0;
-    bool sa = false;
-    fetch(task, ua, na, sa);
-    if constexpr (F32 && !Q8 && D == 128) {  // two units and their sums are more than the registers hold
-      for (; task < ntask; task += step) {
-        add(ua, na, sa);
-        fetch(task + step, ua, na, sa);
-      }
-    } else {
-      Cached ub;
-      int nb = 0;
-      bool sb = false;
-      while (task < ntask) {  // the next unit's loads are in flight while one is added
-        fetch(task + step, ub, nb, sb);
-        add(ua, na, sa);
-        task += step;
-        if (task >= ntask) break;
-        fetch(task + step, ua, na, sa);
-        add(ub, nb, sb);
-        task += step;
-      }
+      t += step;
+      fetch(t);
+      if (visible > 0) add_cached<Cached, T, D, Q8>(cs, u, stage, a.qscale2, visible, sees, q, col, grp);
     }
   }
 
@@ -572,8 +748,22 @@ __global__ __launch_bounds__(NW * 64, 2) void draft_attn_kernel(DraftAttnArgs a)
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
 
+  if (a.KS == 1) {
+    if (!on) return;
+    const Place pl = place_of(a, tile, bh, col);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+#pragma unroll
+      for (int dt = 0; dt < DT; dt += 4) {
+        const float x[4] = {cs.o[dt][i], cs.o[dt + 1][i], cs.o[dt + 2][i], cs.o[dt + 3][i]};
+        finish<T, D, Q8>(a, pl, (grp * 4 + i) * DT + dt, x, cs.m, l, split);
+      }
+    }
+    return;
+  }
+
   // the wavefronts' states of every column meet in LDS, where the list was
-  constexpr int LW = D + 2;
+  constexpr int LW = D + 4;
   const int cols = a.R * a.G;
   float* red = reinterpret_cast<float*>(lds);
   __syncthreads();
@@ -582,7 +772,8 @@ __global__ __launch_bounds__(NW * 64, 2) void draft_attn_kernel(DraftAttnArgs a)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) mine[(grp * 4 + i) * DT + dt] = cs.o[dt][i];
+      for (int dt = 0; dt < DT; dt += 4)
+        *reinterpret_cast<float4*>(mine + (grp * 4 + i) * DT + dt) = make_float4(cs.o[dt][i], cs.o[dt + 1][i], cs.o[dt + 2][i], cs.o[dt + 3][i]);
     }
     if (grp == 0) {
       mine[D] = cs.m;
@@ -590,58 +781,59 @@ __global__ __launch_bounds__(NW * 64, 2) void draft_attn_kernel(DraftAttnArgs a)
     }
   }
   __syncthreads();
-  const int64_t at = static_cast<int64_t>(tile) * a.BH + bh;
-  for (int e = threadIdx.x; e < live * D; e += NW * 64) {
-    const int c = e / D, dd = e - c * D;
-    float top = -INFINITY;
+  for (int e = threadIdx.x; e < live * (D / 4); e += static_cast<int>(blockDim.x)) {
+    const int c = e / (D / 4), dd = (e - c * (D / 4)) * 4, next = cols * LW;  // to the next wavefront's
+    const float* x = red + c * LW;
+    float2 ml[kMaxWaves];  // all of them asked for at once; the last one's again for those that are not there
+    f32x4a y[kMaxWaves];
 #pragma unroll
-    for (int i = 0; i < NW; ++i) top = fmaxf(top, red[(i * cols + c) * LW + D]);
+    for (int i = 0; i < kMaxWaves; ++i) {
+      const float* xi = x + min(i, a.KS - 1) * next;
+      ml[i] = *reinterpret_cast<const float2*>(xi + D);
+      y[i] = *reinterpret_cast<const f32x4a*>(xi + dd);
+    }
+    float top = ml[0].x;
+#pragma unroll
+    for (int i = 1; i < kMaxWaves; ++i) top = fmaxf(top, ml[i].x);
     const float ref = top == -INFINITY ? 0.f : top;
-    float ll = 0.f, oo = 0.f;
+    float ll = 0.f, oo[4] = {};
 #pragma unroll
-    for (int i = 0; i < NW; ++i) {
-      const float* x = red + (i * cols + c) * LW;
-      const float f = fast_exp2((x[D] - ref) * a.qscale2);
-      ll += x[D + 1] * f;
-      oo += x[dd] * f;
+    for (int i = 0; i < kMaxWaves; ++i) {
+      if (i < a.KS) {
+        const float f = fast_exp2((ml[i].x - ref) * a.qscale2);
+        ll += ml[i].y * f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) oo[e] += y[i][e] * f;
+      }
     }
-    if (a.splits == 1) {
-      const int cr = c / a.G;
-      const int64_t orow = (static_cast<int64_t>(b) * a.H + h * a.G + (c - cr * a.G)) * a.T + row0 + cr;
-      store_out<T>(a.o, orow * D + dd, ll == 0.f ? 0.f : oo / (ll * kUnit<T, Q8>));
-      if (a.lse && dd == 0) a.lse[orow] = row_lse<T, Q8>(ref, ll, a.qscale2);
-    } else {
-      a.part_o[((at * a.splits + blockIdx.y) * cols + c) * D + dd] = oo;
-      if (dd == 0) a.part_ml[(at * cols + c) * a.splits + blockIdx.y] = make_float2(top, ll);
-    }
+    finish<T, D, Q8>(a, place_of(a, tile, bh, c), dd, oo, top, ll, split);
   }
 }
 
 // The splits' states of one column: a wavefront, lane i < splits holding split i's
 // weight.
-constexpr int kMaxSplits = 16;
+constexpr int kMaxSplits = 32;
 template <typename T, int D, bool Q8>
 __global__ __launch_bounds__(64) void draft_merge_kernel(DraftAttnArgs a) {
-  constexpr int E = D / 64;
-  const int64_t w = blockIdx.x;
-  const int c = blockIdx.y, lane = threadIdx.x, cols = a.R * a.G;
-  const int bh = static_cast<int>(w % a.BH), tile = a.tile0 + static_cast<int>(w / a.BH);
-  const int64_t at = static_cast<int64_t>(tile) * a.BH + bh;
-  const int cr = c / a.G, row = tile * a.R + cr;
-  if (row >= a.T) return;
-  const float2 ml = lane < a.splits ? a.part_ml[(at * cols + c) * a.splits + lane] : make_float2(-INFINITY, 0.f);
-  float x[kMaxSplits][E];
+  constexpr int E = D / 64, CHUNK = 16;
+  const int w = static_cast<int>(blockIdx.x), c = static_cast<int>(blockIdx.y), lane = threadIdx.x;
+  const int bh = w % a.BH, tile = a.tile0 + w / a.BH;
+  if (tile * a.R + c / a.G >= a.T) return;
+  const Place pl = place_of(a, tile, bh, c);
+  const float2 ml = lane < a.splits ? a.part_ml[pl.part * a.splits + lane] : make_float2(-INFINITY, 0.f);
+  const float* p = a.part_o + pl.part * a.splits * D + lane * E;
+  float x[CHUNK][E];
 #pragma unroll
-  for (int i = 0; i < kMaxSplits; ++i) {
+  for (int i = 0; i < CHUNK; ++i) {
     if (i < a.splits) {
-      const float* p = a.part_o + ((at * a.splits + i) * cols + c) * D + lane * E;
 #pragma unroll
-      for (int e = 0; e < E; ++e) x[i][e] = p[e];
+      for (int e = 0; e < E; ++e) x[i][e] = p[i * D + e];
     }
   }
   float top = ml.x;
 #pragma unroll
   for (int o = 1; o < kMaxSplits; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+  top = __shfl(top, 0);
   const float ref = top == -INFINITY ? 0.f : top;
   const float f = fast_exp2((ml.x - ref) * a.qscale2);
   float ll = ml.y * f;
@@ -650,20 +842,28 @@ __global__ __launch_bounds__(64) void draft_merge_kernel(DraftAttnArgs a) {
   ll = __shfl(ll, 0);
   const float inv = ll == 0.f ? 0.f : 1.f / (ll * kUnit<T, Q8>);
   float oo[E] = {};
+  for (int base = 0;;) {
 #pragma unroll
-  for (int i = 0; i < kMaxSplits; ++i) {
-    if (i < a.splits) {
-      const float fi = __shfl(f, i);
+    for (int i = 0; i < CHUNK; ++i) {
+      if (base + i < a.splits) {
+        const float fi = __shfl(f, base + i);
 #pragma unroll
-      for (int e = 0; e < E; ++e) oo[e] += x[i][e] * fi;
+        for (int e = 0; e < E; ++e) oo[e] += x[i][e] * fi;
+      }
+    }
+    base += CHUNK;
+    if (base >= a.splits) break;
+#pragma unroll
+    for (int i = 0; i < CHUNK; ++i) {
+      if (base + i < a.splits) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[i][e] = p[(base + i) * D + e];
+      }
     }
   }
-  const int b = bh / a.Hkv, h = bh - b * a.Hkv;
-  const int64_t orow = (static_cast<int64_t>(b) * a.H + h * a.G + (c - cr * a.G)) * a.T + row;
 #pragma unroll
-  for (int e = 0; e < E; ++e) store_out<T>(a.o, orow * D + lane * E + e, oo[e] * inv);
-  const float top0 = __shfl(ref, 0);
-  if (a.lse && lane == 0) a.lse[orow] = row_lse<T, Q8>(top0, ll, a.qscale2);
+  for (int e = 0; e < E; ++e) store_out<T>(a.o, pl.row * D + lane * E + e, oo[e] * inv);
+  if (a.lse && lane == 0) a.lse[pl.row] = row_lse<T, Q8>(ref, ll, a.qscale2);
 }
 
 namespace {
@@ -676,48 +876,60 @@ int unit_keys(const Shape& s, bool q8) {
   return s.C % 64 == 0 && (s.bf16 || s.D == 64) ? 64 : 32;
 }
 
-// Wavefronts that share a tile's units: nw of a workgroup, splits of them.  As in
-// qcache_attn.hip the device holds 2048 of these wavefronts.
+// How a tile's units are spread: over the wavefronts of a workgroup, and workgroups.
+// The device holds 2048 of these wavefronts (3072 in bf16 of 64 dimensions); beyond
+// that they only share units more finely.  Otherwise a unit to a wavefront is best, with
+// as many to spare as rows may want other blocks, up to 64 and where that is much more
+// than one workgroup can do: the second launch that joins workgroups costs what 32 units
+// of bf16 and 64 dimensions do in eight wavefronts (12 units of 64 dimensions, 118
+// tiles: 8.0 us in one workgroup, 10.6 in two; 50 of 128, 8 tiles: 34 in one, 12.2 in
+// eight of eight wavefronts, 11.4 in sixteen of four).  Workgroups of four where that
+// leaves at most one to a CU (above), of eight elsewhere (64 tiles of 32: 13.8 and 15.4).
 struct Spread {
-  int nw, splits;
+  int ks, splits;
 };
 Spread spread(const Shape& s, bool q8) {
-  const int R = tile_rows(s);
+  const int R = tile_rows(s), M = (s.N - s.Nq + s.C - 1) / s.C, ku = unit_keys(s, q8);
   const int64_t tiles = static_cast<int64_t>(s.BH()) * ((s.Nq + R - 1) / R);
-  const int64_t units = static_cast<int64_t>(s.K) * (s.C / unit_keys(s, q8)) * (R > 1 ? 2 : 1);
-  int w = 1;
-  while (w < units && w < 64 && 2 * w * tiles <= 2048) w *= 2;
-  if (w <= 8) return {w, 1};
-  const int nw = w == 16 ? 2 : 4;
-  return {nw, w / nw};
+  // blocks that the rows of a tile select together, about (a tree's rows: 1.6 times one
+  // row's for four, 2.5 times for sixteen), and units
+  int lg = 0;
+  while ((2 << lg) <= R) ++lg;
+  const int64_t blocks = std::min<int64_t>(M, static_cast<int64_t>(s.K) * (8 + 3 * lg) / 8);
+  const int64_t units = blocks * (s.C / ku) + (s.Nq + 31) / 32;
+  const int64_t held = ((s.bf16 && s.D == 64 ? 3072 : 2048) + tiles / 2) / tiles;  // of a tile's wavefronts
+  const int64_t w = std::max<int64_t>(1, std::min<int64_t>({held, 64, units * 7 / 5}));
+  if (w <= kMaxWaves || units * (s.D / 64) * (s.bf16 ? 1 : 3) <= 32) return {static_cast<int>(std::min<int64_t>(w, kMaxWaves)), 1};
+  const int ks = tiles * ((w + 3) / 4) <= kDeviceCUs ? 4 : kMaxWaves;
+  return {ks, static_cast<int>(w == held ? w / ks : (w + ks - 1) / ks)};
 }
 
 size_t al256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
-size_t part_ml_at(const Shape& s, int splits) {
-  const int R = tile_rows(s);
-  return al256(static_cast<size_t>(s.BH()) * ((s.Nq + R - 1) / R) * splits * R * s.G * s.D * sizeof(float));
+int tiles_of(const Shape& s) { return (s.Nq + tile_rows(s) - 1) / tile_rows(s); }
+
+// Columns of the partials.
+size_t part_cols(const Shape& s, int splits) {
+  return static_cast<size_t>(s.BH()) * tiles_of(s) * tile_rows(s) * s.G * splits;
 }
 
-template <typename T, int D, bool Q8, int KU, int NW>
+template <typename T, int D, bool Q8, int KU>
 hipError_t launch(const Shape& s, const DraftAttnArgs& a, hipStream_t st) {
-  const int tiles = (s.Nq + a.R - 1) / a.R;
-  const size_t words = (a.M + 31) / 32;
-  const size_t lds = std::max((2 * words + 2 * static_cast<size_t>(a.list)) * 4, static_cast<size_t>(NW) * a.R * s.G * (D + 2) * 4);
+  const int tiles = tiles_of(s);
+  size_t lds = static_cast<size_t>(list_pieces(a.M, a.list)) * 16 + static_cast<size_t>(a.KS) * kStage<T, D, Q8, KU>;
+  if (a.KS > 1) lds = std::max(lds, static_cast<size_t>(a.KS) * a.R * s.G * (D + 4) * 4);
   if (lds > 65536) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(draft_attn_kernel<T, D, Q8, KU, NW>),
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(draft_attn_kernel<T, D, Q8, KU>),
                                              hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
     if (e != hipSuccess) return e;
   }
-  // a launch's threads fit 32 bits; workgroup w takes KV head w % BH, so that an
-  // XCD's workgroups share KV heads
-  const int most = std::max(1, (1 << 22) / s.BH());
+  const int most = std::max(1, (1 << 22) / (s.BH() * a.splits));  // a launch's threads fit 32 bits
   DraftAttnArgs c = a;
   for (c.tile0 = 0; c.tile0 < tiles; c.tile0 += most) {
     const unsigned n = static_cast<unsigned>(std::min(most, tiles - c.tile0)) * static_cast<unsigned>(s.BH());
     {
       ProfScope ps("draft_attn", st);
-      draft_attn_kernel<T, D, Q8, KU, NW><<<dim3(n, a.splits), NW * 64, lds, st>>>(c);
+      draft_attn_kernel<T, D, Q8, KU><<<n * a.splits, a.KS * 64, lds, st>>>(c);
     }
     if (a.splits > 1) {
       ProfScope ps("draft_merge", st);
@@ -729,22 +941,13 @@ hipError_t launch(const Shape& s, const DraftAttnArgs& a, hipStream_t st) {
   return hipSuccess;
 }
 
-template <typename T, int D, bool Q8, int KU>
-hipError_t launch_nw(const Shape& s, const DraftAttnArgs& a, int nw, hipStream_t st) {
-  switch (nw) {
-    case 1: return launch<T, D, Q8, KU, 1>(s, a, st);
-    case 2: return launch<T, D, Q8, KU, 2>(s, a, st);
-    case 4: return launch<T, D, Q8, KU, 4>(s, a, st);
-    default: return launch<T, D, Q8, KU, 8>(s, a, st);
-  }
-}
-
 }  // namespace
 
 size_t draft_attn_ws(const Shape& s, bool q8) {
-  const int splits = spread(s, q8).splits, R = tile_rows(s);
-  if (splits == 1) return 0;
-  return part_ml_at(s, splits) + static_cast<size_t>(s.BH()) * ((s.Nq + R - 1) / R) * splits * R * s.G * sizeof(float2);
+  const Spread sp = spread(s, q8);
+  if (sp.splits == 1) return 0;
+  const size_t n = part_cols(s, sp.splits);
+  return al256(n * s.D * sizeof(float)) + n * sizeof(float2);
 }
 
 hipError_t launch_draft_attn(const Shape& s, const DraftAttn& d, const void* q, const int32_t* idx, void* o, float* lse, void* ws,
@@ -770,6 +973,7 @@ hipError_t launch_draft_attn(const Shape& s, const DraftAttn& d, const void* q, 
   a.H = s.H, a.Hkv = s.Hkv, a.G = s.G, a.T = s.Nq, a.n = n, a.C = s.C, a.K = s.K, a.Nkv = s.Nkv;
   a.M = (n + s.C - 1) / s.C;
   a.R = tile_rows(s);
+  a.KS = sp.ks;
   a.W = (s.Nq + 63) / 64;
   a.BH = s.BH();
   a.splits = sp.splits;
@@ -777,19 +981,19 @@ hipError_t launch_draft_attn(const Shape& s, const DraftAttn& d, const void* q, 
   a.qscale2 = kLog2e / sqrtf(static_cast<float>(s.D));
   if (sp.splits > 1) {
     a.part_o = reinterpret_cast<float*>(base);
-    a.part_ml = reinterpret_cast<float2*>(base + part_ml_at(s, sp.splits));
+    a.part_ml = reinterpret_cast<float2*>(base + al256(part_cols(s, sp.splits) * s.D * sizeof(float)));
   }
   if (q8) {
     if (s.bf16) {
       if (s.D == 128)
-        return ku == 64 ? launch_nw<uint16_t, 128, true, 64>(s, a, sp.nw, st) : launch_nw<uint16_t, 128, true, 32>(s, a, sp.nw, st);
-      return ku == 64 ? launch_nw<uint16_t, 64, true, 64>(s, a, sp.nw, st) : launch_nw<uint16_t, 64, true, 32>(s, a, sp.nw, st);
+        return ku == 64 ? launch<uint16_t, 128, true, 64>(s, a, st) : launch<uint16_t, 128, true, 32>(s, a, st);
+      return ku == 64 ? launch<uint16_t, 64, true, 64>(s, a, st) : launch<uint16_t, 64, true, 32>(s, a, st);
     }
-    if (s.D == 128) return launch_nw<float, 128, true, 32>(s, a, sp.nw, st);
-    return ku == 64 ? launch_nw<float, 64, true, 64>(s, a, sp.nw, st) : launch_nw<float, 64, true, 32>(s, a, sp.nw, st);
+    if (s.D == 128) return launch<float, 128, true, 32>(s, a, st);
+    return ku == 64 ? launch<float, 64, true, 64>(s, a, st) : launch<float, 64, true, 32>(s, a, st);
   }
-  if (s.bf16) return s.D == 128 ? launch_nw<uint16_t, 128, false, 32>(s, a, sp.nw, st) : launch_nw<uint16_t, 64, false, 32>(s, a, sp.nw, st);
-  return s.D == 128 ? launch_nw<float, 128, false, 16>(s, a, sp.nw, st) : launch_nw<float, 64, false, 32>(s, a, sp.nw, st);
+  if (s.bf16) return s.D == 128 ? launch<uint16_t, 128, false, 32>(s, a, st) : launch<uint16_t, 64, false, 32>(s, a, st);
+  return s.D == 128 ? launch<float, 128, false, 16>(s, a, st) : launch<float, 64, false, 32>(s, a, st);
 }
 
 }  // namespace pisa

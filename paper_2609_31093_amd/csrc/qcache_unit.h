@@ -86,10 +86,8 @@ __device__ __forceinline__ uint32_t keep_below(uint32_t w, int at, int limit) {
   return n >= 4 ? w : n <= 0 ? 0u : w & ((1u << (8 * n)) - 1u);
 }
 
-// A key unit's codes and scales, as a wavefront's lanes hold them.  Row r of the
-// values' dimension tile dt is dimension 16 dt + r, or with RUNS r D/16 + dt, so that
-// a row's tiles are consecutive dimensions.
-template <int D, int KU, bool RUNS = false>
+// A key unit's codes and scales, as a wavefront's lanes hold them.
+template <int D, int KU>
 struct Unit {
   static constexpr int MT = KU / 16;  // key tiles
   static constexpr int DT = D / 16;   // dimension tiles of O
@@ -112,7 +110,7 @@ struct Unit {
     }
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
-      const uint8_t* p = vp + (RUNS ? col * DT + dt : dt * 16 + col) * C;
+      const uint8_t* p = vp + (dt * 16 + col) * C;
       if constexpr (VW == 4) {
         const uint4 x = *reinterpret_cast<const uint4*>(p);
         vw[dt][0] = x.x, vw[dt][1] = x.y, vw[dt][2] = x.z, vw[dt][3] = x.w;
