@@ -33,6 +33,7 @@
 // weights times values are held in units of kUnit, so that values up to the type's
 // largest do not overflow before they are divided (values below 2^-109 lose bits).
 #include <algorithm>
+#include <atomic>
 
 #include "attn_shared.h"
 #include "common.h"
@@ -475,8 +476,11 @@ __device__ __forceinline__ void add_cached(Columns<T, D, Q8>& cs, U& u, const u3
   cs.add(u, lds, w, corr, sees, col, grp);
 }
 
-// Most wavefronts of a workgroup.
+// Most wavefronts of a workgroup; LDS of a CU, the most a wavefront's unit takes of it,
+// and the list (65535 blocks, 16 rows of 128 at most, since fanout * K <= 256).
 constexpr int kMaxWaves = 8;
+constexpr size_t kMaxLds = 160 * 1024, kStageMost = 16 * 1024, kListMost = (2048 + 16 * (kMaxCand / 2)) * 8;
+static_assert(kMaxWaves * kStageMost + kListMost <= kMaxLds);
 
 // 16-byte pieces of LDS that the list takes.
 __host__ __device__ __forceinline__ int list_pieces(int M, int list) { return ((M + 31) / 32 + list + 1) / 2; }
@@ -487,6 +491,7 @@ constexpr int kStage = Q8 ? (Unit8<D, KU, 1>::BYTES > (sizeof(T) == 4 ? Unit32<D
                                  ? Unit8<D, KU, 1>::BYTES
                                  : (sizeof(T) == 4 ? Unit32<D>::BYTES : Unit16<D>::BYTES))
                           : (sizeof(T) == 4 ? Unit32<D>::BYTES : Unit16<D>::BYTES);
+static_assert(kStage<uint16_t, 128, true, 64> <= kStageMost && kStage<float, 128, false, 16> <= kStageMost);
 
 // The blocks that any of a tile's rows selected, ascending, and for each the rows
 // that did, in LDS: a bitmap of the cache's blocks, its words' running counts, and
@@ -812,19 +817,19 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void draft_attn_kernel(DraftAttn
 
 // The splits' states of one column: a wavefront, lane i < splits holding split i's
 // weight.
-constexpr int kMaxSplits = 32;
+constexpr int kMaxSplits = 16;  // 64 wavefronts, four to a workgroup
 template <typename T, int D, bool Q8>
 __global__ __launch_bounds__(64) void draft_merge_kernel(DraftAttnArgs a) {
-  constexpr int E = D / 64, CHUNK = 16;
+  constexpr int E = D / 64;
   const int w = static_cast<int>(blockIdx.x), c = static_cast<int>(blockIdx.y), lane = threadIdx.x;
   const int bh = w % a.BH, tile = a.tile0 + w / a.BH;
   if (tile * a.R + c / a.G >= a.T) return;
   const Place pl = place_of(a, tile, bh, c);
   const float2 ml = lane < a.splits ? a.part_ml[pl.part * a.splits + lane] : make_float2(-INFINITY, 0.f);
   const float* p = a.part_o + pl.part * a.splits * D + lane * E;
-  float x[CHUNK][E];
+  float x[kMaxSplits][E];
 #pragma unroll
-  for (int i = 0; i < CHUNK; ++i) {
+  for (int i = 0; i < kMaxSplits; ++i) {
     if (i < a.splits) {
 #pragma unroll
       for (int e = 0; e < E; ++e) x[i][e] = p[i * D + e];
@@ -842,23 +847,12 @@ __global__ __launch_bounds__(64) void draft_merge_kernel(DraftAttnArgs a) {
   ll = __shfl(ll, 0);
   const float inv = ll == 0.f ? 0.f : 1.f / (ll * kUnit<T, Q8>);
   float oo[E] = {};
-  for (int base = 0;;) {
 #pragma unroll
-    for (int i = 0; i < CHUNK; ++i) {
-      if (base + i < a.splits) {
-        const float fi = __shfl(f, base + i);
+  for (int i = 0; i < kMaxSplits; ++i) {
+    if (i < a.splits) {
+      const float fi = __shfl(f, i);
 #pragma unroll
-        for (int e = 0; e < E; ++e) oo[e] += x[i][e] * fi;
-      }
-    }
-    base += CHUNK;
-    if (base >= a.splits) break;
-#pragma unroll
-    for (int i = 0; i < CHUNK; ++i) {
-      if (base + i < a.splits) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) x[i][e] = p[(base + i) * D + e];
-      }
+      for (int e = 0; e < E; ++e) oo[e] += x[i][e] * fi;
     }
   }
 #pragma unroll
@@ -919,9 +913,17 @@ hipError_t launch(const Shape& s, const DraftAttnArgs& a, hipStream_t st) {
   size_t lds = static_cast<size_t>(list_pieces(a.M, a.list)) * 16 + static_cast<size_t>(a.KS) * kStage<T, D, Q8, KU>;
   if (a.KS > 1) lds = std::max(lds, static_cast<size_t>(a.KS) * a.R * s.G * (D + 4) * 4);
   if (lds > 65536) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(draft_attn_kernel<T, D, Q8, KU>),
-                                             hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
+    static std::atomic<uint64_t> allowed{0};  // devices that were told
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
     if (e != hipSuccess) return e;
+    const uint64_t bit = uint64_t(1) << (dev & 63);
+    if (dev > 63 || !(allowed.load(std::memory_order_acquire) & bit)) {
+      e = hipFuncSetAttribute(reinterpret_cast<const void*>(draft_attn_kernel<T, D, Q8, KU>),
+                              hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kMaxLds));
+      if (e != hipSuccess) return e;
+      if (dev <= 63) allowed.fetch_or(bit, std::memory_order_release);
+    }
   }
   const int most = std::max(1, (1 << 22) / (s.BH() * a.splits));  // a launch's threads fit 32 bits
   DraftAttnArgs c = a;

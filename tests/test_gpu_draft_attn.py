@@ -363,6 +363,44 @@ def test_long_cache():
 
 
 @pytest.mark.parametrize("eight", [False, True], ids=["raw", "8bit"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_longest_list(eight, dtype):
+    """As many blocks as a tile can select together, out of as many as there are: the list that leaves a unit least room."""
+    T, d, C, K = 20, 64, 32, 128
+    n = 65535 * C - T
+    p = base.problem(1, 1, 1, T, n + T, d, C, 2, K, 1, dtype, 0)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(1)
+    k, v = (torch.randn((1, 1, n + T, d), generator=gen, device="cuda").to(base.TYPES[dtype]) for _ in range(2))
+    if eight:
+        cache = pisa.make_qcache(p)
+        pisa.qcache_append(base.at(p, n), cache, k[:, :, :n], v[:, :, :n], 0)
+    q, new, mask = normal((1, 1, T, d), 3, dtype), drafted(p, 5, dtype), trees(1, T, 6)
+    M, rng = -(-n // C), np.random.default_rng(2)
+    order = rng.permutation(M - 1)[:T * K].reshape(T, K)
+    order[:, 0] = M - 1
+    idx = torch.from_numpy(order.astype(np.int32))[None, None].contiguous().cuda()
+    o, lse = attend(p, cache if eight else (k, v), q, idx, *new, mask)
+    # each row's blocks out of a short cache of their own
+    for r in (0, 7, 15, 16, 19):
+        at = idx[0, 0, r].sort().values.long()
+        ns = (K - 1) * C + n - (M - 1) * C
+        ps = base.problem(1, 1, 1, T, ns + T, d, C, 2, K, 1, dtype, K * C + T)
+        if eight:
+            short = pisa.make_qcache(ps)
+            for f in ("k", "v", "k_scale", "v_scale"):
+                getattr(short, f)[:, :, :K] = getattr(cache, f)[:, :, at]
+        else:
+            short = tuple(torch.nn.functional.pad(x[:, :, :M * C].unflatten(2, (M, C))[:, :, at].flatten(2, 3)[:, :, :ns], (0, 0, 0, C + T + K * C - ns - C))
+                          for x in (k, v))
+        only = torch.full_like(idx, -1)
+        only[0, 0, r] = torch.arange(K, device="cuda")
+        want_o, want_l, tol_o, tol_l = (x[:, :, r] for x in reference(ps, short, q, only, *new, mask))
+        assert (abs(o[:, :, r].double().cpu().numpy() - want_o) <= tol_o).all()
+        assert (abs(lse[:, :, r].double().cpu().numpy() - want_l) <= tol_l).all()
+
+
+@pytest.mark.parametrize("eight", [False, True], ids=["raw", "8bit"])
 def test_wrapper_refuses(eight):
     p = problem((1, 4, 2, 12, 300, 64, 32, 2, 5, "bf16", 10))
     cache, q, new = make(p, eight, 1, "bf16"), normal((1, 4, 12, 64), 3, "bf16"), drafted(p, 5, "bf16")
