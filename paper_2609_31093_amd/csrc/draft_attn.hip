@@ -90,29 +90,32 @@ struct KeyRows {
   static constexpr int NP = RB / 16, NL = KU * NP / 64, BYTES = KU * RB;
   u32x4 r[NL];
 
-  static __device__ __forceinline__ int at(int row, int p) {
+  // Piece p of a row is at place p ^ turn(row) of it.
+  static __device__ __forceinline__ int turn(int row) {
     const int run = (row / (KU / 4)) & 1;
-    return row * NP + (p ^ (NP >= 8 ? (row & 3) | run << 2 : ((row >> 1) & 1) | run << 1));
+    return NP >= 8 ? (row & 3) | run << 2 : ((row >> 1) & 1) | run << 1;
   }
   // ptr(i): row i of the unit
   template <typename F>
   __device__ __forceinline__ void load(F ptr, int lane) {
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      const int n = i * 64 + lane, row = n / NP;
-      r[i] = reinterpret_cast<const u32x4*>(ptr(row))[n % NP];
-    }
-  }
-  __device__ __forceinline__ void stage(u32x4* lds, int lane) const {
-#pragma unroll
-    for (int i = 0; i < NL; ++i) {
       const int n = i * 64 + lane;
-      lds[at(n / NP, n % NP)] = r[i];
+      r[i] = reinterpret_cast<const u32x4*>(ptr(n / NP))[n % NP];
     }
   }
-  // piece i of lane (col, grp)'s part of key tile mt
+  // (Load i has rows i 64/NP + lane/NP, whose turns differ from lane/NP's in bits that
+  // depend on i alone.)
+  __device__ __forceinline__ void stage(u32x4* lds, int lane) const {
+    const int first = lane ^ turn(lane / NP);
+#pragma unroll
+    for (int i = 0; i < NL; ++i) lds[i * 64 + (first ^ turn(i * (64 / NP)))] = r[i];
+  }
+  // piece i of lane (col, grp)'s part of key tile mt (a turn depends on the column alone,
+  // and a lane's pieces differ in their lowest bits)
   static __device__ __forceinline__ u32x4 operand(const u32x4* lds, int mt, int i, int col, int grp) {
-    return lds[at((col >> 2) * (KU / 4) + mt * 4 + (col & 3), grp * (NP / 4) + i)];
+    const int row = (col >> 2) * (KU / 4) + (col & 3);
+    return lds[row * NP + mt * 4 * NP + ((grp * (NP / 4)) ^ turn(row) ^ i)];
   }
 };
 
@@ -295,8 +298,10 @@ struct Unit8 {
   u32x4 codes[NL];
   float ksc, vsc, ksc_next, vsc_next;
 
-  // piece p of a dimension: those of 16 lanes' dimensions lie on different banks
-  static __device__ __forceinline__ int at(int dim, int p) { return Keys::BYTES / 16 + ((dim * NP + p) ^ ((dim / DT) & 7)); }
+  // Piece p of a dimension is at place (NP dim + p) ^ (dim / DT % 8), so that 16 lanes'
+  // dimensions lie on different banks.  (Load i's places, and dimension tile dt's, differ
+  // from the first ones in bits that depend on i or dt alone.)
+  static constexpr int kFirst = Keys::BYTES / 16, kRun = NP * DT;
 
   __device__ __forceinline__ void load(const QCache& c, int64_t cell, int C, int u, int lane) {
     const uint8_t* kp = c.k + (cell * C + u * KU) * D;
@@ -322,7 +327,7 @@ struct Unit8 {
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[e] = keep_below(x[e], p * 16 + 4 * e, n);
       }
-      lds[at(m / NP, p)] = x;
+      lds[kFirst + i * 64 + ((lane ^ ((lane / kRun) & 7)) ^ ((i * 64 / kRun) & 7))] = x;
     }
   }
   __device__ __forceinline__ void pin() {}
@@ -359,12 +364,13 @@ struct Unit8 {
   }
   __device__ __forceinline__ f32x4a tile(const u32x4* lds, int dt, const Operand& p, int col, int grp, uint32_t = ~0u) const {
     f32x4a x = {0.f, 0.f, 0.f, 0.f};
+    const int far = kFirst + col * kRun + dt * NP / 8 * 8, near = (col & 7) ^ (dt * NP % 8);
     if constexpr (KU == 64) {
-      const u32x4 v = lds[at(col * DT + dt, grp)];
+      const u32x4 v = lds[far + (near ^ grp)];
       x = p.t[0].times(Weights<NT>::codes(v.x, v.y), x);
       x = p.t[1].times(Weights<NT>::codes(v.z, v.w), x);
     } else {
-      const uint2 v = reinterpret_cast<const uint2*>(lds + at(col * DT + dt, grp >> 1))[grp & 1];
+      const uint2 v = reinterpret_cast<const uint2*>(lds + far + (near ^ (grp >> 1)))[grp & 1];
       x = p.t[0].times(Weights<NT>::codes(v.x, v.y), x);
     }
 #pragma unroll
@@ -372,6 +378,14 @@ struct Unit8 {
     return x;
   }
 };
+
+// The largest of the four lane groups' values of a column.
+__device__ __forceinline__ float max_of_groups(float v) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
 
 // Running softmax of a wavefront's 16 columns.
 template <typename T, int D, bool Q8>
@@ -391,8 +405,7 @@ struct Columns {
     float mx = m;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) mx = fmaxf(mx, fmaxf(fmaxf(s[mt][0], s[mt][1]), fmaxf(s[mt][2], s[mt][3])));
-    mx = fmaxf(mx, __shfl_xor(mx, 16));
-    mx = fmaxf(mx, __shfl_xor(mx, 32));
+    mx = max_of_groups(mx);
     const float ref = mx == -INFINITY ? 0.f : mx;
     const float corr = fast_exp2((m - ref) * qscale2);
     m = mx;
