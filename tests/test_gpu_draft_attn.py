@@ -3,9 +3,9 @@
 Tolerance.  A logit z is a sum of d products, each exact in 32 bits (raw fp32: off by 2^-24), so off by at most delta =
 (d + 5) 2^-24 sum|q_i k_i| / sqrt(d) in any order and after its scaling; the exponent of base 2 adds the rounding of its
 argument (2^-23 |z - m| with the scale's) and 2 ulp.  A weight is then off by rel = exp(2 delta) - 1 + 2^-21 + 2^-23
-max|z - m|, its sum likewise, and sums of n terms by n 2^-23 (products and additions); weights that meet bf16 values by
-another 2^-8, 8-bit ones in bf16 problems by 2^-11.  With W the sum of weight times |value|:
-|o - o_ref| <= (2 rel + 2^-8 or 2^-11 [bf16] + 2 n 2^-23) W + 2^-8 |o| [bf16] + 2^-22 |o|,
+max|z - m|, its sum likewise, and sums of n terms by n 2^-23 (products and additions); weights that meet bf16 values are
+two bf16 terms, off by another 2^-8 2^-8 at most, for 8-bit ones in bf16 problems fp16, 2^-11.  With W the sum of weight
+times |value|: |o - o_ref| <= (2 rel + 2^-16 or 2^-11 [bf16] + 2 n 2^-23) W + 2^-8 |o| [bf16] + 2^-22 |o|,
 lse moves by no more than its logits do, and a weight's 2^-23 |z - m| is small where |z - m| is large (|z - m| exp(z - m) <
 1): |lse - lse_ref| <= delta + 2^-20 + n 2^-23 + 2^-22 max(1, |lse|).
 """
@@ -42,9 +42,9 @@ def bits_of(mask, T):
     return ((m[..., j // 64] >> (j % 64).astype(np.uint64)) & np.uint64(1)).astype(bool)
 
 
-def reference(p, cache, q, idx, k_new, v_new, mask, alone=None):
+def reference(p, cache, q, idx, k_new, v_new, mask, alone=None, terms=2.0 ** -16):
     """(o, lse, bound of o's error, of lse's) in 64 bits; `alone` lists the rows whose largest logit is 50 above the next
-    however both are off, for which o is that key's value."""
+    however both are off, for which o is that key's value; `terms`: how far weights for bf16 values are off."""
     C, d, G, T, n = p.C, p.d, p.H // p.Hkv, p.Nq, p.N - p.Nq
     M = -(-n // C)
     kk, vv = stored(p, cache)
@@ -53,7 +53,8 @@ def reference(p, cache, q, idx, k_new, v_new, mask, alone=None):
     see = bits_of(mask, T)
     o, lse = np.zeros((p.B, p.H, T, d)), np.full((p.B, p.H, T), -np.inf)
     tol_o, tol_l = np.zeros_like(o), np.zeros_like(lse)
-    half, weight = (2.0 ** -8, 2.0 ** -8 if isinstance(cache, tuple) else 2.0 ** -11) if p.dtype == pisa.PISA_DTYPE_BF16 else (0, 0)
+    half, own_w, weight = (2.0 ** -8, terms, terms if isinstance(cache, tuple) else 2.0 ** -11) \
+        if p.dtype == pisa.PISA_DTYPE_BF16 else (0, 0, 0)
     for b in range(p.B):
         for hk in range(p.Hkv):
             for r in range(T):
@@ -64,8 +65,8 @@ def reference(p, cache, q, idx, k_new, v_new, mask, alone=None):
                 vt = np.concatenate((vv[b, hk, tok], vn[b, hk, own]))
                 if not len(kt):
                     continue
-                # drafted rows' weights are bf16 over an 8-bit cache too
-                wt = np.concatenate((np.full(len(tok), weight), np.full(len(own), half)))
+                # drafted rows are bf16 over an 8-bit cache too
+                wt = np.concatenate((np.full(len(tok), weight), np.full(len(own), own_w)))
                 for h in range(hk * G, (hk + 1) * G):
                     z = kt @ q64[b, h, r] / math.sqrt(d)
                     m = z.max()
