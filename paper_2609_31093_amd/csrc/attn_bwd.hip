@@ -178,6 +178,7 @@ __global__ __launch_bounds__(256, bwd_compact(CT * 32) ? 2 : 1) void attn_bwd_bl
     *reinterpret_cast<uint4*>(at_kv(kl, r, c8)) = kv;
     *reinterpret_cast<uint4*>(at_kv(vl, r, c8)) = vv;
   }
+  __syncthreads();  // every wavefront reads the rows that all of them staged
 
   // dV, dK of this wavefront's dims: [key tile][dim tile j: dt = wave*DTW + j]
   f32x4b2 accv[MT][DTW], acck[MT][DTW];
