@@ -510,7 +510,8 @@ int pisa_qcache_attn_fwd(const pisa_problem* p, const pisa_qcache* c, const void
  * more): the last cached one; below -1: none, a token that pads the tree.  Parents
  * may come behind their children.
  * mask: uint64 [B, T, W], W = ceil(T / 64): bit j % 64 of word j / 64 of row i is set
- * where j is i or an ancestor of i (no bit for a token that pads).
+ * where j is i or an ancestor of i (none in the row of a token that pads; nothing
+ * should follow one).
  * positions: nullable int32 [B, T], n + the number of i's ancestors (n for one that
  * pads).  A token whose ancestors run in a circle has those of the circle, and a
  * position of n + T - 1.  B <= 65535, 1 <= T <= PISA_DRAFT_MAX, n + T < 2^31. */

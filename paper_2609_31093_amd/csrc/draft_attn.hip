@@ -23,11 +23,11 @@
 // multiplied as qcache_attn.hip does it.
 //
 // What bounds it: few tokens the chain of latencies (the list 1.2 us, a unit's loads
-// 1.5 and products 1.6, the wavefronts' sums 1.2; 11.5 us with the second launch for 16
-// tokens of 8 heads over 131072 in 8 bits); many the vector instructions of a unit, half
+// 1.5 and products 1.6, the wavefronts' sums 1.2; 10.9 us with the second launch for 16
+// tokens of 8 heads over 131071 in 8 bits); many the vector instructions of a unit, half
 // of them conversions and the sums' rescaling (256 tokens of 8 heads on 2 over 523776:
-// 36 us; with operands straight from the cache, whose scattered pieces a CU takes in at
-// 13 bytes a clock, 48).
+// 34.8 us; with operands straight from the cache, whose scattered pieces a CU takes in
+// at 13 bytes a clock, 48).
 //
 // The running maximum is that of the products before the softmax's scale.  Sums of
 // weights times values are held in units of kUnit, so that values up to the type's
@@ -73,12 +73,22 @@ struct DraftAttnArgs {
 // log2 of the largest weight: fp16 weights (bf16 queries on 8-bit values) are taken up
 // to 2^14, so that ones of 2^-28 of the largest are still normal numbers.
 template <typename T, bool Q8>
-constexpr float kHead = Q8 && sizeof(T) == 2 ? 14.f : 0.f;
-// Units of the sums: 1 / (the largest weight times the tokens of a row, below 2^16).
+constexpr float kHead = !Q8 ? -16.f : sizeof(T) == 2 ? 14.f : 0.f;
+// What weights are multiplied by besides, so that they add up to less than 1 (a row has
+// less than 2^16 tokens).
 template <typename T, bool Q8>
-constexpr float kUnit = Q8 && sizeof(T) == 2 ? 0x1p-30f : 0x1p-16f;
+constexpr float kUnit = !Q8 ? 1.f : sizeof(T) == 2 ? 0x1p-30f : 0x1p-16f;
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// A value at a wavefront's address plus a lane's offset, which the load adds by itself.
+template <typename V>
+__device__ __forceinline__ V value_at(const void* base, uint32_t off) {
+  return *reinterpret_cast<const V*>(static_cast<const char*>(base) + off);
+}
+// Row strides up to which a unit's rows are within a 32-bit offset.
+constexpr int64_t kNear = 1 << 24;
 
 // Key rows of RB bytes on their way to matrix operands.  An operand's lane holds a part
 // of one key's row, 16 lanes 16 rows: loaded like that, each lane's 16 bytes are a
@@ -103,6 +113,12 @@ struct KeyRows {
       const int n = i * 64 + lane;
       r[i] = reinterpret_cast<const u32x4*>(ptr(n / NP))[n % NP];
     }
+  }
+  // rows 0 .. KU - 1, `stride` bytes from one to the next
+  __device__ __forceinline__ void load_all(const void* base, uint32_t stride, int lane) {
+    const uint32_t off = lane / NP * stride + lane % NP * 16;
+#pragma unroll
+    for (int i = 0; i < NL; ++i) r[i] = value_at<u32x4>(static_cast<const char*>(base) + i * (64 / NP) * stride, off);
   }
   // (Load i has rows i 64/NP + lane/NP, whose turns differ from lane/NP's in bits that
   // depend on i alone.)
@@ -147,14 +163,37 @@ struct Unit16 {
       }
     }
   }
+  // The same where all rows are there, with their strides in elements (at most kNear).
+  __device__ __forceinline__ void load_all(const uint16_t* k, uint32_t ks, const uint16_t* v, uint32_t vs, int lane) {
+    keys.load_all(k, 2 * ks, lane);
+    const uint32_t off = (lane >> 4) * 8 * 2 * vs + (lane & 15) * DT * 2;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if constexpr (VW == 4) {
+        const u32x4 x = value_at<u32x4>(v + j * vs, off);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) next[j][i] = x[i];
+      } else {
+        const u32x2 x = value_at<u32x2>(v + j * vs, off);
+        next[j][0] = x[0], next[j][1] = x[1];
+      }
+    }
+  }
   // What was loaded becomes the unit that is worked on: its first n keys.
   __device__ __forceinline__ void stage(u32x4* lds, int lane, int n) {
     keys.stage(lds, lane);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const uint32_t live = (lane >> 4) * 8 + j < n ? ~0u : 0u;  // 0 times a NaN would not be 0
 #pragma unroll
-      for (int i = 0; i < VW; ++i) vw[j][i] = next[j][i] & live;
+      for (int i = 0; i < VW; ++i) vw[j][i] = next[j][i];
+    }
+    if (n < KU) {  // 0 times a NaN would not be 0
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t live = (lane >> 4) * 8 + j < n ? ~0u : 0u;
+#pragma unroll
+        for (int i = 0; i < VW; ++i) vw[j][i] &= live;
+      }
     }
   }
   __device__ __forceinline__ void logits(const u32x4* lds, const Query& q, f32x4a (&s)[MT], int col, int grp) const {
@@ -176,28 +215,31 @@ struct Unit16 {
     }
   }
   __device__ __forceinline__ bool odd() const {  // an infinity or NaN among any lane's values
-    uint32_t any = 0;
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    u16x2 top = {0, 0};
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
 #pragma unroll
-      for (int i = 0; i < VW; ++i) any |= ((vw[j][i] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
+      for (int i = 0; i < VW; ++i) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, vw[j][i] & 0x7FFF7FFFu));
     }
-    return __any(any != 0);
+    return __any(top.x >= 0x7F80 || top.y >= 0x7F80);
   }
   // The weights p of this lane's keys, times `unit`, as operands, and the values' sums
   // of dimension tile dt for them.  Two bf16 terms for a weight: with one the result was
   // 1.25 times as far from the exact one as its rounding (2.1e-3 and 1.7e-3 relative, 64
-  // tokens of 16 heads on 4), for 13.6 us instead of 14.0.
+  // tokens of 16 heads on 4), for 3% less time.
   struct Operand {
     bf16x8a t[2];
   };
   __device__ __forceinline__ Operand operand(const float (&p)[8], float unit) const {
-    float x[8];
+    uint32_t w0[4], w1[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = p[i] * unit;
-    Operand w;
-    split_terms<2>(x, w.t);
-    return w;
+    for (int i = 0; i < 4; ++i) {
+      const float x = unit == 1.f ? p[2 * i] : p[2 * i] * unit, y = unit == 1.f ? p[2 * i + 1] : p[2 * i + 1] * unit;
+      w0[i] = pack2_bf16(x, y);
+      w1[i] = pack2_bf16(x - __uint_as_float(w0[i] << 16), y - __uint_as_float(w0[i] & 0xFFFF0000u));
+    }
+    return {{u4_as_bf16x8(make_uint4(w0[0], w0[1], w0[2], w0[3])), u4_as_bf16x8(make_uint4(w1[0], w1[1], w1[2], w1[3]))}};
   }
   // bits: this lane group's keys whose values count
   __device__ __forceinline__ f32x4a tile(const u32x4*, int dt, const Operand& p, int, int, uint32_t bits = ~0u) const {
@@ -239,13 +281,33 @@ struct Unit32 {
       }
     }
   }
+  __device__ __forceinline__ void load_all(const float* k, uint32_t ks, const float* v, uint32_t vs, int lane) {
+    keys.load_all(k, 4 * ks, lane);
+    const uint32_t off = (lane >> 4) * VT * 4 * vs + (lane & 15) * DT * 4;
+#pragma unroll
+    for (int j = 0; j < VT; ++j) {
+#pragma unroll
+      for (int i = 0; i < DT; i += 4) {
+        const f32x4a x = value_at<f32x4a>(v + j * vs + i, off);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) next[j][i + e] = x[e];
+      }
+    }
+  }
   __device__ __forceinline__ void stage(u32x4* lds, int lane, int n) {
     keys.stage(lds, lane);
 #pragma unroll
     for (int j = 0; j < VT; ++j) {
-      const bool live = (lane >> 4) * VT + j < n;
 #pragma unroll
-      for (int i = 0; i < DT; ++i) vw[j][i] = live ? next[j][i] : 0.f;
+      for (int i = 0; i < DT; ++i) vw[j][i] = next[j][i];
+    }
+    if (n < KU) {
+#pragma unroll
+      for (int j = 0; j < VT; ++j) {
+        const bool live = (lane >> 4) * VT + j < n;
+#pragma unroll
+        for (int i = 0; i < DT; ++i) vw[j][i] = live ? vw[j][i] : 0.f;
+      }
     }
   }
   __device__ __forceinline__ void logits(const u32x4* lds, const Query& q, f32x4a (&s)[MT], int col, int grp) const {
@@ -277,7 +339,7 @@ struct Unit32 {
   __device__ __forceinline__ Operand operand(const float (&p)[VT], float unit) const {
     Operand w;
 #pragma unroll
-    for (int j = 0; j < VT; ++j) w.t[j] = p[j] * unit;
+    for (int j = 0; j < VT; ++j) w.t[j] = unit == 1.f ? p[j] : p[j] * unit;
     return w;
   }
   __device__ __forceinline__ f32x4a tile(const u32x4*, int dt, const Operand& p, int, int, uint32_t bits = ~0u) const {
@@ -311,12 +373,10 @@ struct Unit8 {
   __device__ __forceinline__ void load(const QCache& c, int64_t cell, int C, int u, int lane) {
     const uint8_t* kp = c.k + (cell * C + u * KU) * D;
     const uint8_t* vp = c.v + cell * C * D + u * KU;
-    keys.load([&](int row) { return kp + row * D; }, lane);
+    keys.load_all(kp, D, lane);
+    const uint32_t off = lane / NP * C + lane % NP * 16;
 #pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int n = i * 64 + lane;
-      codes[i] = reinterpret_cast<const u32x4*>(vp + n / NP * C)[n % NP];
-    }
+    for (int i = 0; i < NL; ++i) codes[i] = value_at<u32x4>(vp + i * (64 / NP) * C, off);
     ksc_next = c.k_scale[cell];
     vsc_next = c.v_scale[cell];
   }
@@ -444,6 +504,10 @@ __device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? ~0u : n <
 // Drafted keys j0 .. j0 + KU - 1.
 template <typename U, typename T>
 __device__ __forceinline__ void load_drafted(U& u, const DraftAttnArgs& a, const T* kn, const T* vn, int j0, int lane) {
+  if (j0 + U::KU <= a.T && a.ksn <= kNear && a.vsn <= kNear) {
+    u.load_all(kn + j0 * a.ksn, static_cast<uint32_t>(a.ksn), vn + j0 * a.vsn, static_cast<uint32_t>(a.vsn), lane);
+    return;
+  }
   const int last = a.T - 1;
   u.load([&](int i) { return kn + min(j0 + i, last) * a.ksn; }, [&](int i) { return vn + min(j0 + i, last) * a.vsn; }, lane);
 }
@@ -597,7 +661,7 @@ __device__ __forceinline__ int uniform(uint32_t x) { return __builtin_amdgcn_rea
 
 template <typename T, bool Q8>
 __device__ __forceinline__ float row_lse(float ref, float sum, float qscale2) {
-  constexpr float unit = kHead<T, Q8> == 14.f ? 0x1p-14f : 1.f;  // the headroom leaves the sum before its logarithm
+  constexpr float unit = kHead<T, Q8> == 14.f ? 0x1p-14f : kHead<T, Q8> == 0.f ? 1.f : 0x1p16f;  // 2^-kHead
   return sum == 0.f ? -INFINITY : fmaf(ref, qscale2, fast_log2(sum * unit)) * kLn2;
 }
 
@@ -704,7 +768,8 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void draft_attn_kernel(DraftAttn
 
   Columns<T, D, Q8> cs;
   int t = begin + wave;
-  if (t < min(chunks, end)) {
+  const int drafts = min(chunks, end);
+  if (t < drafts) {
     typename Drafted::Query q;
     make_query<T>(qw, q);
     if (!early) {
@@ -718,9 +783,11 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void draft_attn_kernel(DraftAttn
         wave_sync();
         add_drafted<Drafted, T, D, Q8>(cs, ud, stage, a.qscale2, bits, q, col, grp);
       }
-      t += step;
-      if (t >= min(chunks, end)) break;
-      bits = seen(t * Drafted::KU);
+      do {  // on to the next ones that any column sees
+        t += step;
+        bits = t < drafts ? seen(t * Drafted::KU) : 0u;
+      } while (t < drafts && !__any(bits != 0));
+      if (t >= drafts) break;
       load_drafted(ud, a, kn, vn, t * Drafted::KU, lane);
     }
   }
@@ -747,6 +814,10 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void draft_attn_kernel(DraftAttn
       } else {
         const int64_t first = (static_cast<int64_t>(bh) * a.Nkv + key0) * D;
         const T *kb = static_cast<const T*>(a.k) + first, *vb = static_cast<const T*>(a.v) + first;
+        if (next_visible == KU) {
+          u.load_all(kb, D, vb, D, lane);
+          return;
+        }
         const int last = next_visible - 1;
         u.load([&](int i) { return kb + static_cast<uint32_t>(min(i, last) * D); },
                [&](int i) { return vb + static_cast<uint32_t>(min(i, last) * D); }, lane);

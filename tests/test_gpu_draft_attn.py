@@ -321,6 +321,25 @@ def test_captured_and_on_another_stream(eight):
                 assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_drafted_rows_far_apart(dtype):
+    """Strides of drafted rows around the one up to which 32-bit offsets serve."""
+    p = problem((1, 2, 1, 70, 100, 64, 32, 2, 3, dtype, 0))
+    cache, q, idx, mask = make(p, False, 1, dtype), normal((1, 2, 70, 64), 3, dtype), selection(p, 4), trees(1, 70, 6)
+    new = drafted(p, 5, dtype)
+    want = attend(p, cache, q, idx, *new, mask)
+    for stride in ((1 << 24) - 8, 1 << 24, (1 << 24) + 8):
+        wide = torch.empty((70, stride), dtype=base.TYPES[dtype], device="cuda")
+        views = [wide[:, 64 * i:64 * (i + 1)][None, None] for i in range(2)]
+        for x, y in zip(views, new):
+            x.copy_(y)
+        got = attend(p, cache, q, idx, *views, mask)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        got = attend(p, cache, q, idx, new[0], views[1], mask)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        del wide, views
+
+
 def test_many_tiles_past_one_launch():
     """More tiles than the 2^22 that one launch takes: 5000 sequences of 1024 rows, a row to a tile, 9 heads on 1."""
     B, H, T, d = 5000, 9, 1024, 64
