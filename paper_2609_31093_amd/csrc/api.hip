@@ -153,6 +153,13 @@ int check_ptr(const void* ptr, const char* name, bool nullable = false) {
   return PISA_OK;
 }
 
+// The same for what kernels read or write a value at a time.
+int check_values(const void* ptr, const char* name, unsigned size, bool nullable = false) {
+  if (!ptr) return nullable ? PISA_OK : fail(PISA_ERR_INVALID_ARG, "%s is NULL", name);
+  if (reinterpret_cast<uintptr_t>(ptr) % size) return fail(PISA_ERR_INVALID_ARG, "%s is not %u-byte aligned", name, size);
+  return PISA_OK;
+}
+
 bool aligned256(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 255u) == 0; }
 
 int check_ws(void* ws, size_t ws_bytes, size_t need) {
@@ -653,26 +660,41 @@ int check_inputs_apart(const pisa_rope* r, const pisa::RopeSide (&x)[2], const p
   return PISA_OK;
 }
 
-// Weights, their gradients and the workspace against each other and against what is
-// written (by what lies between a tensor's first value and its last).
-int check_norm_overlaps(const pisa_rope* r, const pisa_qk_norm* m, const pisa::RopeSide (&side)[2], const float* d_q_weight,
-                        const float* d_k_weight, const void* ws, size_t ws_bytes) {
+// What a norm writes against what it reads, but for the tensors that check_rope_overlaps
+// and check_inputs_apart compare row by row (by what lies between a tensor's first value
+// and its last).  out: the sides' outputs; in, dy: the sides' inputs (of a gradient).
+int check_norm_overlaps(const pisa_rope* r, const pisa_qk_norm* m, const int32_t* positions, const pisa::RopeSide (&out)[2],
+                        const pisa::RopeSide (&in)[2], const float* d_q_weight, const float* d_k_weight, const void* ws,
+                        size_t ws_bytes) {
   const size_t w = static_cast<size_t>(r->d) * (m->weight_dtype == PISA_DTYPE_BF16 ? 2 : 4), dw = static_cast<size_t>(r->d) * 4;
   const size_t esz = r->dtype == PISA_DTYPE_BF16 ? 2 : 4;
-  auto bytes = [](const void* p, size_t n) { return p ? n : 0; };
-  const Region weights[] = {{m->q_weight, bytes(m->q_weight, w), "q_weight"}, {m->k_weight, bytes(m->k_weight, w), "k_weight"}};
-  Region out[5] = {{d_q_weight, bytes(d_q_weight, dw), "d_q_weight"}, {d_k_weight, bytes(d_k_weight, dw), "d_k_weight"},
-                   {ws, bytes(ws, ws_bytes), "workspace"}, {nullptr, 0, "q (output)"}, {nullptr, 0, "k (output)"}};
   const int heads[2] = {r->H, r->Hkv};
-  for (int i = 0; i < 2; ++i) {
-    out[3 + i].ptr = side[i].out;
-    if (side[i].out) out[3 + i].bytes = span_of({side[i].ob, side[i].oh, side[i].on}, r->B, heads[i], r->N, r->d, esz);
+  auto bytes = [](const void* p, size_t n) { return p ? n : 0; };
+  auto reads = [&](const pisa::RopeSide& x, int i, const char* name) {
+    return Region{x.in, bytes(x.in, span_of({x.ib, x.ih, x.in_n}, r->B, heads[i], r->N, r->d, esz)), name};
+  };
+  auto writes = [&](const pisa::RopeSide& x, int i, const char* name) {
+    return Region{x.out, bytes(x.out, span_of({x.ob, x.oh, x.on}, r->B, heads[i], r->N, r->d, esz)), name};
+  };
+  const Region small_in[] = {{m->q_weight, bytes(m->q_weight, w), "q_weight"},
+                             {m->k_weight, bytes(m->k_weight, w), "k_weight"},
+                             {positions, bytes(positions, span_of({r->pos_bstride, 0, 1}, r->B, 1, r->N, 1, 4)), "positions"}};
+  const Region small_out[] = {{d_q_weight, bytes(d_q_weight, dw), "d_q_weight"},
+                              {d_k_weight, bytes(d_k_weight, dw), "d_k_weight"},
+                              {ws, bytes(ws, ws_bytes), "workspace"}};
+  const Region large_in[] = {reads(in[0], 0, "q"), reads(in[1], 1, "k"), reads(out[0], 0, "d_q_out"), reads(out[1], 1, "d_k_out")};
+  const Region large_out[] = {writes(out[0], 0, "q (output)"), writes(out[1], 1, "k (output)")};
+  auto apart = [](const Region& x, const Region& y) {
+    return meet(x, y) ? fail(PISA_ERR_INVALID_ARG, "%s overlaps %s", x.name, y.name) : PISA_OK;
+  };
+  for (const Region& y : small_in) {
+    for (const Region& x : small_out) PISA_TRY(apart(x, y));
+    for (const Region& x : large_out) PISA_TRY(apart(x, y));
   }
-  for (int j = 0; j < 5; ++j) {
-    for (const Region& x : weights)
-      if (meet(x, out[j])) return fail(PISA_ERR_INVALID_ARG, "%s overlaps %s", out[j].name, x.name);
-    for (int i = 0; i < std::min(j, 3); ++i)
-      if (meet(out[i], out[j])) return fail(PISA_ERR_INVALID_ARG, "%s overlaps %s", out[j].name, out[i].name);
+  for (int i = 0; i < 3; ++i) {
+    for (const Region& y : large_in) PISA_TRY(apart(small_out[i], y));
+    for (const Region& y : large_out) PISA_TRY(apart(small_out[i], y));
+    for (int j = 0; j < i; ++j) PISA_TRY(apart(small_out[i], small_out[j]));
   }
   return PISA_OK;
 }
@@ -700,7 +722,7 @@ int run_draft_attn(const pisa_problem* p, const pisa::Shape& s, pisa::DraftAttn 
   PISA_TRY(check_ptr(block_idx, "block_idx"));
   PISA_TRY(check_ptr(k_new, "k_new"));
   PISA_TRY(check_ptr(v_new, "v_new"));
-  PISA_TRY(check_ptr(mask, "mask"));
+  PISA_TRY(check_values(mask, "mask", 8));
   PISA_TRY(check_ptr(o, "o"));
   PISA_TRY(check_ptr(lse, "lse", true));
   const int64_t W = (p->Nq + 63) / 64;
@@ -1118,9 +1140,9 @@ int pisa_draft_layout(int32_t B, int32_t T, const int32_t* parents, int32_t n, u
   if (B < 1 || B > 65535) return fail(PISA_ERR_INVALID_ARG, "B must be in [1, 65535] (got %d)", B);
   if (T < 1 || T > PISA_DRAFT_MAX) return fail(PISA_ERR_INVALID_ARG, "T must be in [1, %d] (got %d)", PISA_DRAFT_MAX, T);
   if (n < 0 || n > INT32_MAX - T) return fail(PISA_ERR_INVALID_ARG, "need 0 <= n <= 2^31 - 1 - T (got %d)", n);
-  PISA_TRY(check_ptr(parents, "parents"));
-  PISA_TRY(check_ptr(mask, "mask"));
-  PISA_TRY(check_ptr(positions, "positions", true));
+  PISA_TRY(check_values(parents, "parents", 4));
+  PISA_TRY(check_values(mask, "mask", 8));
+  PISA_TRY(check_values(positions, "positions", 4, true));
   const size_t row = static_cast<size_t>(B) * T;
   const Region r[] = {{parents, row * 4, "parents"}, {mask, row * 8 * ((T + 63) / 64), "mask"},
                       {positions, positions ? row * 4 : 0, "positions"}};
@@ -1181,7 +1203,7 @@ int pisa_norm_rope_fwd(const pisa_rope* r, const pisa_qk_norm* m, const void* q,
   if (!q && !k) return fail(PISA_ERR_INVALID_ARG, "neither q nor k given");
   PISA_TRY(check_positions(positions));
   PISA_TRY(check_rope_overlaps(r, {a.q, a.k}, {"q", "k"}));
-  PISA_TRY(check_norm_overlaps(r, m, {a.q, a.k}, nullptr, nullptr, nullptr, 0));
+  PISA_TRY(check_norm_overlaps(r, m, positions, {a.q, a.k}, {}, nullptr, nullptr, nullptr, 0));
   fill_rope(r, positions, 1.f, &a);
   return device_status(pisa::launch_norm_rope(a, na, nullptr, nullptr, r->dtype == PISA_DTYPE_BF16, r->layout == PISA_ROPE_HALF,
                                               static_cast<hipStream_t>(stream)),
@@ -1219,7 +1241,7 @@ int pisa_norm_rope_bwd(const pisa_rope* r, const pisa_qk_norm* m, const void* q,
   PISA_TRY(check_inputs_apart(r, {a.q, a.k}, {dq, dk}));
   const size_t need = d_q_weight || d_k_weight ? norm_rope_ws(r) : 0;
   PISA_TRY(check_ws(ws, ws_bytes, need));
-  PISA_TRY(check_norm_overlaps(r, m, {dq, dk}, d_q_weight, d_k_weight, need ? ws : nullptr, need));
+  PISA_TRY(check_norm_overlaps(r, m, positions, {dq, dk}, {a.q, a.k}, d_q_weight, d_k_weight, need ? ws : nullptr, need));
   na.d_q_weight = d_q_weight;
   na.d_k_weight = d_k_weight;
   na.parts = static_cast<float*>(ws);

@@ -70,6 +70,7 @@ def test_norm_fwd_refuses_bad_tensors():
     assert fwd(q=None) == INVALID and "q" in error()
     assert fwd(q=None, k=None, qo=None, ko=None) == INVALID
     assert fwd(pos=AT["positions"] + 2) == INVALID and "positions" in error()
+    assert fwd(pos=AT["d_q"] + 64) == INVALID and "positions" in error()
     assert fwd(qo=AT["w"]) == INVALID and "q_weight" in error()          # weights that are overwritten
     assert fwd(qo=AT["k"]) == INVALID and "overlaps" in error()
     assert fwd(qo=AT["d_q"], ko=AT["d_q"] + 256) == INVALID and "overlaps" in error()
@@ -93,6 +94,11 @@ def test_norm_bwd_refuses_bad_tensors():
     assert bwd(d_q_weight=AT["w"]) == INVALID and "q_weight" in error()
     assert bwd(d_k_weight=AT["d_q_weight"] + 256) == INVALID
     assert bwd(ws=AT["d_q"]) == INVALID and "workspace" in error()
+    for x in ("q", "k", "d_q_out", "d_k_out"):
+        for n in ("d_q_weight", "d_k_weight", "ws"):
+            assert bwd(**{n: AT[x] + 256}) == INVALID and x in error(), (n, x)
+    for n in ("d_q_weight", "d_k_weight", "ws", "d_q", "d_k"):
+        assert bwd(pos=AT["positions"], **{n: AT["positions"]}) == INVALID and "positions" in error(), n
     assert bwd(d_q_weight=AT["d_q"] + 1024) == INVALID
     assert bwd(d_q=AT["d_q_out"], d_q_s=S(4 * 128 * 100, 128, 4 * 128)) == INVALID and "in place" in error()
 
@@ -133,7 +139,7 @@ def attend(eight, p=None, c=None, **kw):
 def test_draft_attention_refuses(eight):
     for n in ("q", "idx", "k_new", "v_new", "mask", "o") + (() if eight else ("k", "v")):
         assert attend(eight, **{n: None}) == INVALID and error(), n
-        assert attend(eight, **{n: AT[n] + 8}) == INVALID and "aligned" in error(), n
+        assert attend(eight, **{n: AT[n] + (4 if n == "mask" else 8)}) == INVALID and "aligned" in error(), n
     assert attend(eight, lse=AT["lse"] + 4) == INVALID
     assert attend(eight, p=problem(Nq=1025, N=3000, Ncap=0)) == UNSUPPORTED
     assert attend(eight, p=problem(d=96)) == UNSUPPORTED
@@ -198,7 +204,7 @@ def test_layout_refuses():
     def call(B=2, T=20, parents=AT["parents"], n=100, mask=AT["mask"], positions=AT["positions"]):
         return LIB.pisa_draft_layout(B, T, parents, n, mask, positions, None)
     for kw in (dict(B=0), dict(B=65536), dict(T=0), dict(T=1025), dict(n=-1), dict(n=2**31 - 1), dict(parents=None), dict(mask=None),
-               dict(parents=AT["parents"] + 4), dict(mask=AT["mask"] + 8), dict(positions=AT["positions"] + 4),
+               dict(parents=AT["parents"] + 2), dict(mask=AT["mask"] + 4), dict(positions=AT["positions"] + 2),
                dict(mask=AT["parents"]), dict(positions=AT["mask"] + 16), dict(positions=AT["parents"])):
         assert call(**kw) == INVALID and error(), kw
 

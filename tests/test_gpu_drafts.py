@@ -72,6 +72,21 @@ def test_layout_of_odd_parents(T):
     check_layout(wild, 2 ** 31 - 1 - T)
 
 
+def test_layout_of_part_of_a_batch():
+    """Sequences of a batch on their own, which begin at any multiple of a value's size; their masks into attention."""
+    parents = torch.randint(-1, 7, (4, 7), dtype=torch.int32, device="cuda")
+    mask, pos = pisa.draft_layout(parents, 50)
+    p = base.problem(1, 2, 1, 7, 57, 64, 32, 2, 3, 1, "bf16")
+    x = [base.normal((1, h, n, 64), i, "bf16") for i, (h, n) in enumerate(((2, 7), (1, 57), (1, 57), (1, 7), (1, 7)))]
+    idx = torch.tensor([0, 1, -1], dtype=torch.int32, device="cuda").expand(1, 1, 7, 3).contiguous()
+    for b in range(1, 4):
+        got = pisa.draft_layout(parents[b:b + 1], 50)
+        assert torch.equal(got[0][0], mask[b]) and torch.equal(got[1][0], pos[b])
+        a = pisa.draft_attn_fwd(p, x[0], x[1], x[2], idx, x[3], x[4], mask[b])
+        c = pisa.draft_attn_fwd(p, x[0], x[1], x[2], idx, x[3], x[4], mask[b].clone())
+        assert torch.equal(a[0], c[0]) and torch.equal(a[1], c[1])
+
+
 def test_layout_without_positions_captured():
     parents = torch.tensor([[-1, 0, 1, 1, 0], [-1, -1, -2, 2, 3]], dtype=torch.int32, device="cuda")
     mask = torch.full((2, 5, 1), -1, dtype=torch.int64, device="cuda")
