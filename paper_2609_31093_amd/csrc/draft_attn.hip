@@ -202,7 +202,8 @@ struct Unit16 {
       s[mt] = f32x4a{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks)
-        s[mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8a, Keys::operand(lds, mt, ks, col, grp)), q[ks][0], s[mt], 0, 0, 0);
+        s[mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8a, Keys::operand(lds, mt, ks, col, grp)), q[ks][0],
+                                                        s[mt], 0, 0, 0);
     }
   }
   // Keeps the compiler from making operands of all values ahead of the weights, which
@@ -696,10 +697,13 @@ __device__ __forceinline__ Place place_of(const DraftAttnArgs& a, int tile, int 
 
 // Four dimensions from dd on of a column's sums, and with the first ones its state.
 template <typename T, int D, bool Q8>
-__device__ __forceinline__ void finish(const DraftAttnArgs& a, const Place& pl, int dd, const float (&x)[4], float top, float l, int split) {
+__device__ __forceinline__ void finish(const DraftAttnArgs& a, const Place& pl, int dd, const float (&x)[4], float top, float l,
+                                       int split) {
   if (a.splits == 1) {
     const float inv = l == 0.f ? 0.f : 1.f / (l * kUnit<T, Q8>);
-    const float y[4] = {l == 0.f ? 0.f : x[0] * inv, l == 0.f ? 0.f : x[1] * inv, l == 0.f ? 0.f : x[2] * inv, l == 0.f ? 0.f : x[3] * inv};
+    float y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = l == 0.f ? 0.f : x[i] * inv;
     store_out4<T>(a.o, pl.row * D + dd, y);
     if (a.lse && dd == 0) a.lse[pl.row] = row_lse<T, Q8>(top == -INFINITY ? 0.f : top, l, a.qscale2);
   } else {
@@ -867,7 +871,8 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void draft_attn_kernel(DraftAttn
     for (int i = 0; i < 4; ++i) {
 #pragma unroll
       for (int dt = 0; dt < DT; dt += 4)
-        *reinterpret_cast<float4*>(mine + (grp * 4 + i) * DT + dt) = make_float4(cs.o[dt][i], cs.o[dt + 1][i], cs.o[dt + 2][i], cs.o[dt + 3][i]);
+        *reinterpret_cast<float4*>(mine + (grp * 4 + i) * DT + dt) =
+            make_float4(cs.o[dt][i], cs.o[dt + 1][i], cs.o[dt + 2][i], cs.o[dt + 3][i]);
     }
     if (grp == 0) {
       mine[D] = cs.m;
@@ -982,7 +987,8 @@ Spread spread(const Shape& s, bool q8) {
   const int64_t units = blocks * (s.C / ku) + (s.Nq + 31) / 32;
   const int64_t held = ((s.bf16 && s.D == 64 ? 3072 : 2048) + tiles / 2) / tiles;  // of a tile's wavefronts
   const int64_t w = std::max<int64_t>(1, std::min<int64_t>({held, 64, units * 7 / 5}));
-  if (w <= kMaxWaves || units * (s.D / 64) * (s.bf16 ? 1 : 3) <= 32) return {static_cast<int>(std::min<int64_t>(w, kMaxWaves)), 1};
+  if (w <= kMaxWaves || units * (s.D / 64) * (s.bf16 ? 1 : 3) <= 32)
+    return {static_cast<int>(std::min<int64_t>(w, kMaxWaves)), 1};
   const int ks = tiles * ((w + 3) / 4) <= kDeviceCUs ? 4 : kMaxWaves;
   return {ks, static_cast<int>(w == held ? w / ks : (w + ks - 1) / ks)};
 }

@@ -151,8 +151,9 @@ __device__ __forceinline__ void append_block(const BlockRows<T, D, PICK>& src, i
 
 }  // namespace
 
-// A wavefront per changed block and side.  PATH (one or two blocks change): a workgroup per (batch, KV head), a wavefront for the keys and one for the
-// values of each block, and two for the levels, as qcache_append_kernel has it.
+// A wavefront per changed block and side.  PATH (one or two blocks change): a workgroup
+// per (batch, KV head), a wavefront for the keys and one for the values of each block,
+// and two for the levels, as qcache_append_kernel has it.
 template <typename T, int D, int PATH, bool PICK>
 __global__ __launch_bounds__(PATH == 2 ? 384 : 256) void cache_append_kernel(CacheAppend a, Geo geo, bool grown) {
   constexpr int DPL = D / 16;
@@ -168,7 +169,8 @@ __global__ __launch_bounds__(PATH == 2 ? 384 : 256) void cache_append_kernel(Cac
   float* pb = a.pyr + static_cast<int64_t>(bh) * geo.R * D;
   if (PATH ? wave < 2 * PATH : leaf <= last) {
     BlockRows<T, D, PICK> src;
-    src.cache = static_cast<T*>(keys ? a.k : a.v) + (static_cast<int64_t>(bh) * geo.Nkv + static_cast<int64_t>(leaf) * C) * D + sub * DPL;
+    src.cache = static_cast<T*>(keys ? a.k : a.v) + (static_cast<int64_t>(bh) * geo.Nkv + static_cast<int64_t>(leaf) * C) * D +
+                sub * DPL;
     src.fresh = static_cast<const T*>(keys ? a.k_new : a.v_new) + b * (keys ? a.ksb : a.vsb) + h * (keys ? a.ksh : a.vsh) + sub * DPL;
     src.rows = PICK ? a.rows + static_cast<int64_t>(b) * (geo.N - a.n_old) : nullptr;
     src.stride = keys ? a.ksn : a.vsn;
@@ -222,7 +224,8 @@ static hipError_t launch_append_rows(const Geo& geo, const Geo& geo_old, int BH,
 
 hipError_t launch_cache_append(const Geo& geo, const Geo& geo_old, int BH, int D, bool bf16, const CacheAppend& a, hipStream_t st) {
   if (bf16)
-    return D == 128 ? launch_append_rows<uint16_t, 128>(geo, geo_old, BH, a, st) : launch_append_rows<uint16_t, 64>(geo, geo_old, BH, a, st);
+    return D == 128 ? launch_append_rows<uint16_t, 128>(geo, geo_old, BH, a, st)
+                    : launch_append_rows<uint16_t, 64>(geo, geo_old, BH, a, st);
   return D == 128 ? launch_append_rows<float, 128>(geo, geo_old, BH, a, st) : launch_append_rows<float, 64>(geo, geo_old, BH, a, st);
 }
 

@@ -215,7 +215,8 @@ struct Raw16 {
 // gradients: each thread sums its rows', then the workgroup's meet in LDS, and
 // norm_rope_weights_kernel adds the workgroups' in their order.
 template <typename T, int D, int LAY>
-__global__ __launch_bounds__(256, sizeof(T) == 2 && LAY != kMixed ? 3 : 2) void norm_rope_bwd_kernel(RopeArgs a, NormArgs m, RopeSide dq, RopeSide dk) {
+__global__ __launch_bounds__(256, sizeof(T) == 2 && LAY != kMixed ? 3 : 2) void norm_rope_bwd_kernel(RopeArgs a, NormArgs m,
+                                                                                                  RopeSide dq, RopeSide dk) {
   constexpr int UNITS = D / 16, ROWS = 256 / UNITS;
   __shared__ float part[4][D];
   const int u = threadIdx.x % UNITS, pairs = a.rot / 2;
@@ -296,14 +297,16 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && LAY != kMixed ? 3 : 2) void 
   __syncthreads();
   if (threadIdx.x < D) {
     const int e = threadIdx.x;
-    m.parts[(static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x) * D + e] = (part[0][e] + part[1][e]) + (part[2][e] + part[3][e]);
+    m.parts[(static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x) * D + e] =
+        (part[0][e] + part[1][e]) + (part[2][e] + part[3][e]);
   }
 }
 
 // Sums of the parts: a workgroup for 16 dimensions of a side, 256 threads for each
 // four of them, whose loads are four at a time on their way.
 template <int D>
-__global__ __launch_bounds__(1024) void norm_rope_weights_kernel(const float* __restrict__ parts, int nq, int nk, float* d_q, float* d_k) {
+__global__ __launch_bounds__(1024) void norm_rope_weights_kernel(const float* __restrict__ parts, int nq, int nk, float* d_q,
+                                                                 float* d_k) {
   __shared__ float4 sums[256][4];
   const bool is_q = blockIdx.y == 0;
   float* out = is_q ? d_q : d_k;

@@ -278,9 +278,8 @@ __device__ __forceinline__ void keep_raw(const Source<T, D, PICK>& src, T* open,
 }  // namespace
 
 // A wavefront per changed block and side.  PATH (only the last block or the last two
-// changed): a workgroup per (batch, KV head), a wavefront for the
-// keys and one for the values of each block, and two that update the levels meanwhile
-// (pyramid_path.h).  Otherwise four wavefronts on their own: blocks x {keys, values}.
+// changed): a workgroup per (batch, KV head), a wavefront for the keys and one for the
+// values of each block, and two that update the levels meanwhile (pyramid_path.h).  Otherwise four wavefronts on their own: blocks x {keys, values}.
 template <typename T, int D, int CH, int PATH, bool PICK>
 __global__ __launch_bounds__(PATH == 2 ? 384 : 256) void qcache_append_kernel(QAppend a, Geo geo, bool grown) {
   constexpr int DPL = D / 16;
@@ -369,7 +368,8 @@ static hipError_t launch_append_rows(const Geo& geo, const Geo& geo_old, int BH,
 hipError_t launch_qcache_append(const Geo& geo, const Geo& geo_old, int BH, int D, bool bf16, const QAppend& a,
                                 hipStream_t st) {
   if (bf16)
-    return D == 128 ? launch_append_rows<uint16_t, 128>(geo, geo_old, BH, a, st) : launch_append_rows<uint16_t, 64>(geo, geo_old, BH, a, st);
+    return D == 128 ? launch_append_rows<uint16_t, 128>(geo, geo_old, BH, a, st)
+                    : launch_append_rows<uint16_t, 64>(geo, geo_old, BH, a, st);
   return D == 128 ? launch_append_rows<float, 128>(geo, geo_old, BH, a, st) : launch_append_rows<float, 64>(geo, geo_old, BH, a, st);
 }
 
