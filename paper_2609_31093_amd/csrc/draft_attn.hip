@@ -910,7 +910,8 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void draft_attn_kernel(DraftAttn
 }
 
 // The splits' states of one column: a wavefront, lane i < splits holding split i's
-// weight.
+// weight.  All of its loads are asked for at once: one latency and the launch, 2.4 to
+// 4.8 us.
 constexpr int kMaxSplits = 16;  // 64 wavefronts, four to a workgroup
 template <typename T, int D, bool Q8>
 __global__ __launch_bounds__(64) void draft_merge_kernel(DraftAttnArgs a) {
