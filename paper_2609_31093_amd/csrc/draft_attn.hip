@@ -966,8 +966,8 @@ int unit_keys(const Shape& s, bool q8) {
 }
 
 // How a tile's units are spread: over the wavefronts of a workgroup, and workgroups.
-// The device holds 2048 of these wavefronts (3072 in bf16 of 64 dimensions); beyond
-// that they only share units more finely.  Otherwise a unit to a wavefront is best, with
+// A CU holds eight of these wavefronts (twelve in bf16 of 64 dimensions); beyond that
+// they only share units more finely.  Otherwise a unit to a wavefront is best, with
 // as many to spare as rows may want other blocks, up to 64 and where that is much more
 // than one workgroup can do: the second launch that joins workgroups costs what 32 units
 // of bf16 and 64 dimensions do in eight wavefronts (12 units of 64 dimensions, 118
@@ -986,7 +986,7 @@ Spread spread(const Shape& s, bool q8) {
   while ((2 << lg) <= R) ++lg;
   const int64_t blocks = std::min<int64_t>(M, static_cast<int64_t>(s.K) * (8 + 3 * lg) / 8);
   const int64_t units = blocks * (s.C / ku) + (s.Nq + 31) / 32;
-  const int64_t held = ((s.bf16 && s.D == 64 ? 3072 : 2048) + tiles / 2) / tiles;  // of a tile's wavefronts
+  const int64_t held = (kDeviceCUs * (s.bf16 && s.D == 64 ? 12 : 8) + tiles / 2) / tiles;  // of a tile's wavefronts
   const int64_t w = std::max<int64_t>(1, std::min<int64_t>({held, 64, units * 7 / 5}));
   if (w <= kMaxWaves || units * (s.D / 64) * (s.bf16 ? 1 : 3) <= 32)
     return {static_cast<int>(std::min<int64_t>(w, kMaxWaves)), 1};
