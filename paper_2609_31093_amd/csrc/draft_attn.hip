@@ -977,21 +977,38 @@ int unit_keys(const Shape& s, bool q8) {
 struct Spread {
   int ks, splits;
 };
-Spread spread(const Shape& s, bool q8) {
-  const int R = tile_rows(s), M = (s.N - s.Nq + s.C - 1) / s.C, ku = unit_keys(s, q8);
-  const int64_t tiles = static_cast<int64_t>(s.BH()) * ((s.Nq + R - 1) / R);
+struct Units {
+  int64_t tiles, held, w;  // a tile's wavefronts: those that the device holds, those wanted
+  bool split;              // more than one workgroup to a tile
+};
+// M: blocks that there are.
+Units units_of(const Shape& s, bool q8, int64_t M) {
+  Units u{};
+  const int R = tile_rows(s);
+  u.tiles = static_cast<int64_t>(s.BH()) * ((s.Nq + R - 1) / R);
   // blocks that the rows of a tile select together, about (a tree's rows: 1.6 times one
   // row's for four, 2.5 times for sixteen), and units
   int lg = 0;
   while ((2 << lg) <= R) ++lg;
   const int64_t blocks = std::min<int64_t>(M, static_cast<int64_t>(s.K) * (8 + 3 * lg) / 8);
-  const int64_t units = blocks * (s.C / ku) + (s.Nq + 31) / 32;
-  const int64_t held = (kDeviceCUs * (s.bf16 && s.D == 64 ? 12 : 8) + tiles / 2) / tiles;  // of a tile's wavefronts
-  const int64_t w = std::max<int64_t>(1, std::min<int64_t>({held, 64, units * 7 / 5}));
-  if (w <= kMaxWaves || units * (s.D / 64) * (s.bf16 ? 1 : 3) <= 32)
-    return {static_cast<int>(std::min<int64_t>(w, kMaxWaves)), 1};
-  const int ks = tiles * ((w + 3) / 4) <= kDeviceCUs ? 4 : kMaxWaves;
-  return {ks, static_cast<int>(w == held ? w / ks : (w + ks - 1) / ks)};
+  const int64_t units = blocks * (s.C / unit_keys(s, q8)) + (s.Nq + 31) / 32;
+  u.held = (kDeviceCUs * (s.bf16 && s.D == 64 ? 12 : 8) + u.tiles / 2) / u.tiles;
+  u.w = std::max<int64_t>(1, std::min<int64_t>({u.held, 64, units * 7 / 5}));
+  u.split = u.w > kMaxWaves && units * (s.D / 64) * (s.bf16 ? 1 : 3) > 32;
+  return u;
+}
+Spread spread(const Shape& s, bool q8) {
+  const Units u = units_of(s, q8, (s.N - s.Nq + s.C - 1) / s.C);
+  if (!u.split) return {static_cast<int>(std::min<int64_t>(u.w, kMaxWaves)), 1};
+  const int ks = u.tiles * ((u.w + 3) / 4) <= kDeviceCUs ? 4 : kMaxWaves;
+  return {ks, static_cast<int>(u.w == u.held ? u.w / ks : (u.w + ks - 1) / ks)};
+}
+// Most splits that spread() takes whatever the cache holds, so that one workspace serves
+// a cache that grows.
+int most_splits(const Shape& s, bool q8) {
+  const Units u = units_of(s, q8, INT32_MAX);
+  if (!u.split) return 1;
+  return static_cast<int>(std::max(std::min((u.w + 3) / 4, kDeviceCUs / u.tiles), (u.w + kMaxWaves - 1) / kMaxWaves));
 }
 
 size_t al256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
@@ -1042,9 +1059,9 @@ hipError_t launch(const Shape& s, const DraftAttnArgs& a, hipStream_t st) {
 }  // namespace
 
 size_t draft_attn_ws(const Shape& s, bool q8) {
-  const Spread sp = spread(s, q8);
-  if (sp.splits == 1) return 0;
-  const size_t n = part_cols(s, sp.splits);
+  const int splits = most_splits(s, q8);
+  if (splits == 1) return 0;
+  const size_t n = part_cols(s, splits);
   return al256(n * s.D * sizeof(float)) + n * sizeof(float2);
 }
 

@@ -209,6 +209,21 @@ def test_layout_refuses():
         assert call(**kw) == INVALID and error(), kw
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,C,K", [(64, 32, 3), (64, 64, 16), (128, 64, 16), (128, 128, 32), (64, 256, 100)])
+def test_draft_workspaces_serve_a_growing_cache(dtype, d, C, K):
+    """One size for every length of the cache; and a call of any length is content with it (and refuses less)."""
+    for f, eight in ((pisa.pisa_draft_attn_workspace_bytes, False), (pisa.pisa_qcache_draft_attn_workspace_bytes, True)):
+        for H, Hkv, T in ((1, 1, 1), (4, 4, 20), (8, 2, 20), (16, 1, 3), (8, 8, 300), (32, 2, 1024)):
+            sizes = set()
+            for n in (0, 1, C, 5 * C + 3, 50 * C, 1000 * C + 1):
+                p = problem(H=H, Hkv=Hkv, Nq=T, N=n + T, d=d, C=C, K=K, dtype=dtype, Ncap=0, fanout=2)
+                sizes.add(f(p))
+                if f(p):
+                    assert attend(eight, p=p, mb=T * -(-T // 64), nb=f(p) - 1) == WORKSPACE
+            assert len(sizes) == 1
+
+
 def test_draft_workspaces_are_zero_for_bad_problems():
     for f in (pisa.pisa_draft_attn_workspace_bytes, pisa.pisa_qcache_draft_attn_workspace_bytes):
         assert f(problem(d=96)) == 0 and f(problem(Nq=1025, N=2000, Ncap=0)) == 0

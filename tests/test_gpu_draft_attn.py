@@ -321,6 +321,20 @@ def test_captured_and_on_another_stream(eight):
                 assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("eight", [False, True], ids=["raw", "8bit"])
+def test_one_workspace_for_a_growing_cache(eight):
+    """Lengths whose tiles are spread over one workgroup and over several, with what an earlier call left."""
+    need = pisa.pisa_qcache_draft_attn_workspace_bytes if eight else pisa.pisa_draft_attn_workspace_bytes
+    ws = None
+    for n in (0, 40, 700, 5000, 1500, 64):
+        p = problem((1, 8, 2, 12, n, 128, 64, 2, 16, "bf16", 64))
+        ws = torch.full((need(p),), 0xFF, dtype=torch.uint8, device="cuda") if ws is None else ws
+        assert need(p) == ws.numel() > 0
+        cache, q, new = make(p, eight, 1, "bf16"), normal((1, 8, 12, 128), 3, "bf16"), drafted(p, 5, "bf16")
+        idx, mask = selection(p, n), trees(1, 12, 6)
+        check(p, cache, q, idx, *new, mask, *attend(p, cache, q, idx, *new, mask, ws=ws))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_drafted_rows_far_apart(dtype):
     """Strides of drafted rows around the one up to which 32-bit offsets serve."""
