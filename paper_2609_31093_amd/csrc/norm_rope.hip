@@ -12,8 +12,9 @@
 // lane and the sums over the head are three (two) exchanges between neighbours.
 // Everything is held in fp32 and rounded once.  Each value is read once and
 // written once, which bounds the kernels: 131072 rows of 16 heads of 128 in bf16 take
-// 204 to 209 us (5.2 TB/s, a copy's rate), gradients of 30011 rows of 20 heads 100 us
-// (4.6 TB/s, 3 us of it the weights' sums).
+// 189 to 192 us (5.6 TB/s; a copy has 5.2; workgroups that go on to other rows 208 with 4096
+// of them), gradients of 30011 rows of 20 heads 100 us (4.6 TB/s, 3 us of it the
+// weights' sums).
 #include <algorithm>
 
 #include "common.h"
@@ -33,7 +34,7 @@ constexpr int kPairs = 0, kHalves = 1, kMixed = 2;
 // the border (kMixed) has r < 8 pairs; its `hi` runs on into the dimensions behind the
 // rotated ones, and its `lo` has from value r on those that follow, lo2 + r ...
 // lo2 + 7.  So three runs are loaded and one value chosen from two (131072 rows of 16
-// heads: 309 us, 209 without a border; each value loaded on its own 782).
+// heads: 333 us, 192 without a border; each value loaded on its own 782).
 template <int LAY>
 struct Slots {
   int lo, hi, lo2, r, p0;
@@ -152,7 +153,7 @@ __device__ __forceinline__ void lane_angles(const RopeArgs& a, int b, int n, int
 
 }  // namespace
 
-// Workgroups (rows, heads): 256 threads take 256 / UNITS rows at a time.
+// Workgroups (rows, heads): 256 threads take 256 / UNITS rows.
 template <typename T, int D, int LAY>
 __global__ __launch_bounds__(256) void norm_rope_kernel(RopeArgs a, NormArgs m) {
   constexpr int UNITS = D / 16, ROWS = 256 / UNITS;
@@ -162,26 +163,25 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(RopeArgs a, NormArgs m) 
   const RopeSide& io = heads.is_q ? a.q : a.k;
   float wlo[8], whi[8];
   load_weights<LAY>(m, heads.is_q ? m.q_weight : m.k_weight, at, wlo, whi);
-  const int rows = a.B * a.N;
-  for (int row = static_cast<int>(blockIdx.x) * ROWS + threadIdx.x / UNITS; row < rows; row += static_cast<int>(gridDim.x) * ROWS) {
-    const int b = row / a.N, n = row - b * a.N;
-    float c[8], s[8];
-    lane_angles(a, b, n, 8 * u, pairs, c, s);
-    for (int h = heads.first; h < heads.end; ++h) {
-      float lo[8], hi[8];
-      load16<LAY>(row_in<T>(io, b, h, n), at, lo, hi);
-      float sum = 0.f;
+  const int row = static_cast<int>(blockIdx.x) * ROWS + threadIdx.x / UNITS;
+  if (row >= a.B * a.N) return;
+  const int b = row / a.N, n = row - b * a.N;
+  float c[8], s[8];
+  lane_angles(a, b, n, 8 * u, pairs, c, s);
+  for (int h = heads.first; h < heads.end; ++h) {
+    float lo[8], hi[8];
+    load16<LAY>(row_in<T>(io, b, h, n), at, lo, hi);
+    float sum = 0.f;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) sum += lo[j] * lo[j] + hi[j] * hi[j];
-      const float r = rsqrtf(row_sum<UNITS>(sum) * (1.f / D) + m.eps);
+    for (int j = 0; j < 8; ++j) sum += lo[j] * lo[j] + hi[j] * hi[j];
+    const float r = rsqrtf(row_sum<UNITS>(sum) * (1.f / D) + m.eps);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        lo[j] *= r * wlo[j];
-        hi[j] *= r * whi[j];
-      }
-      turn<LAY>(lo, hi, c, s);
-      store16<LAY>(row_out<T>(io, b, h, n), at, lo, hi);
+    for (int j = 0; j < 8; ++j) {
+      lo[j] *= r * wlo[j];
+      hi[j] *= r * whi[j];
     }
+    turn<LAY>(lo, hi, c, s);
+    store16<LAY>(row_out<T>(io, b, h, n), at, lo, hi);
   }
 }
 
@@ -347,14 +347,13 @@ Grid grid_of(int B, int N, int H, int Hkv, int d, bool bf16, bool bwd) {
   g.heads = groups * (H + Hkv) >= 4 * 1024 ? 4 : groups * (H + Hkv) >= 2 * 1024 ? 2 : 1;
   g.gq = (H + g.heads - 1) / g.heads;
   g.gk = (Hkv + g.heads - 1) / g.heads;
+  g.gx = static_cast<int>(groups);
   // gradients: as few workgroups (and parts of the weights' sums) as the device holds
   // at once, three (fp32: two) on each CU, each the same number of rows (20 heads at
   // 30011 rows, bf16: 640 workgroups 108 us, 768 100, 1024 110, 4096 109)
   if (bwd) {
     const int64_t most = 256 * (bf16 ? 3 : 2), rounds = (groups * (g.gq + g.gk) + most - 1) / most;
     g.gx = static_cast<int>((groups + rounds - 1) / rounds);
-  } else {
-    g.gx = static_cast<int>(std::min<int64_t>(groups, std::max(1, 4096 / (g.gq + g.gk))));
   }
   return g;
 }
