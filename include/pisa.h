@@ -497,7 +497,8 @@ int pisa_qcache_attn_fwd(const pisa_problem* p, const pisa_qcache* c, const void
  * there is nothing to take back: rows k_new, v_new [B, Hkv, T, d] in the problem
  * dtype (strides as in pisa_strides).  Masks are 8-byte aligned, parents, positions and
  * rows 4-byte.  With a problem of Nq = T, N = n + T (and room for them, Ncap >= N):
- *   pisa_draft_layout       masks, and positions for pisa_rope_fwd, from the parents
+ *   pisa_draft_layout       masks, and positions for pisa_rope_fwd or pisa_norm_rope_fwd,
+ *                           from the parents
  *   pisa_select, pisa_select_flat_bsa
  *                           as for T rows after n: those blocks that hold drafted
  *                           rows are forced, so that neither call reads them (T <= C)
