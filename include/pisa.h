@@ -529,10 +529,10 @@ int pisa_draft_layout(int32_t B, int32_t T, const int32_t* parents, int32_t n, u
  * mask_bstride words lie between two sequences, 0 shares one mask among the batch.
  * Rows that nothing selects or masks in are hidden whatever their values.  Writes o
  * [B, H, Nq, d] and lse (nullable); a row that sees nothing gets o = 0 and lse = -inf.
- * Sums in fp32; weights are two bf16 terms (off by 2^-16; fp16 for 8-bit values, as
- * they are in fp32 problems) where they meet the values.  Nq <= PISA_DRAFT_MAX; N = Nq is an empty
- * cache.  o, lse and the workspace must not overlap anything else (PISA_ERR_INVALID_ARG).
- * The workspace's size does not depend on N: one serves a cache that grows. */
+ * Sums in fp32.  Weights meet bf16 values as two bf16 terms (off by 2^-16), 8-bit ones
+ * as fp16, in fp32 problems as they are.  Nq <= PISA_DRAFT_MAX; N = Nq is an empty cache.
+ * o, lse and the workspace must not overlap anything else (PISA_ERR_INVALID_ARG).  The
+ * workspace's size does not depend on N: one serves a cache that grows. */
 size_t pisa_draft_attn_workspace_bytes(const pisa_problem* p);
 int pisa_draft_attn_fwd(const pisa_problem* p, const void* q, const void* k, const void* v, const int32_t* block_idx,
                         const void* k_new, const pisa_strides* k_strides, const void* v_new, const pisa_strides* v_strides,
