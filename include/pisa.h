@@ -530,7 +530,7 @@ int pisa_draft_layout(int32_t B, int32_t T, const int32_t* parents, int32_t n, u
  * Rows that nothing selects or masks in are hidden whatever their values.  Writes o
  * [B, H, Nq, d] and lse (nullable); a row that sees nothing gets o = 0 and lse = -inf.
  * Sums in fp32.  Weights meet bf16 values as two bf16 terms (off by 2^-16), 8-bit ones
- * as fp16, in fp32 problems as they are.  Nq <= PISA_DRAFT_MAX; N = Nq is an empty cache.
+ * as two fp16 terms (2^-22), in fp32 problems as they are.  Nq <= PISA_DRAFT_MAX; N = Nq is an empty cache.
  * o, lse and the workspace must not overlap anything else (PISA_ERR_INVALID_ARG).  The
  * workspace's size does not depend on N: one serves a cache that grows. */
 size_t pisa_draft_attn_workspace_bytes(const pisa_problem* p);

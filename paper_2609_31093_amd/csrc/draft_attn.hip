@@ -20,13 +20,13 @@
 // unit's being loaded meanwhile.  The drafted rows, and a bf16 cache, are units of 32
 // keys on v_mfma_f32_16x16x32_bf16 (weights as two bf16 terms); fp32 ones take
 // v_mfma_f32_16x16x4_f32, whose operands are one value a lane.  The 8-bit cache is
-// multiplied as qcache_attn.hip does it.
+// multiplied as qcache_attn.hip does it, with two fp16 terms of a weight.
 //
 // What bounds it: few tokens the chain of latencies (the list 1.2 us, a unit's loads
 // 1.5 and products 1.6, the wavefronts' sums 1.2; 10.9 us with the second launch for 16
 // tokens of 8 heads over 131071 in 8 bits); many the vector instructions of a unit, half
 // of them conversions and the sums' rescaling (256 tokens of 8 heads on 2 over 523776:
-// 34.8 us; with operands straight from the cache, whose scattered pieces a CU takes in
+// 37.1 us; with operands straight from the cache, whose scattered pieces a CU takes in
 // at 13 bytes a clock, 48).
 //
 // The running maximum is that of the products before the softmax's scale.  Sums of
@@ -352,11 +352,36 @@ struct Unit32 {
   }
 };
 
+// Weights of a bf16 problem over 8-bit values: two fp16 terms, off by 2^-22 (codes are
+// exact in fp16).  One term, off by 2^-11, left the result 1.71e-3 from the exact one where
+// rounding to bf16 leaves 1.70e-3, and further where values cancel (256 tokens of 8 heads
+// on 2 over 523776: 34.9 us with one, 37.1 with two; 16 tokens 11.0 either way).
+struct WeightPair {
+  f16x8a t[2];
+  __device__ __forceinline__ void set(const float (&p)[8]) {
+    uint32_t w0[4], w1[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      w0[i] = pack2_f16(p[2 * i], p[2 * i + 1]);
+      const f16x2a first = __builtin_bit_cast(f16x2a, w0[i]);
+      w1[i] = pack2_f16(p[2 * i] - static_cast<float>(first[0]), p[2 * i + 1] - static_cast<float>(first[1]));
+    }
+    t[0] = __builtin_bit_cast(f16x8a, make_uint4(w0[0], w0[1], w0[2], w0[3]));
+    t[1] = __builtin_bit_cast(f16x8a, make_uint4(w1[0], w1[1], w1[2], w1[3]));
+  }
+  static __device__ __forceinline__ f16x8a codes(uint32_t w0, uint32_t w1) { return Weights<1>::codes(w0, w1); }
+  __device__ __forceinline__ f32x4a times(f16x8a v, f32x4a acc) const {
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, t[1], acc, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(v, t[0], acc, 0, 0, 0);
+  }
+};
+
 // KU keys of the 8-bit cache, keys and values by way of LDS; NT bf16 terms of a query
-// and a weight (qcache_unit.h).  Row r of the values' dimension tile dt is dimension
-// r D/16 + dt, as above.
+// (qcache_unit.h), and of a weight where that is more than one.  Row r of the values'
+// dimension tile dt is dimension r D/16 + dt, as above.
 template <int D, int KU8, int NT>
 struct Unit8 {
+  using Weight = std::conditional_t<NT == 1, WeightPair, Weights<NT>>;
   static constexpr int KU = KU8, MT = KU / 16, DT = D / 16, KS = D / 32;
   static constexpr int NP = KU / 16, NL = D * NP / 64;  // pieces of a dimension's codes
   using Query = bf16x8a[KS][NT];
@@ -413,7 +438,7 @@ struct Unit8 {
     }
   }
   struct Operand {
-    Weights<NT> t[KU / 32];
+    Weight t[KU / 32];
     float scale;
   };
   __device__ __forceinline__ Operand operand(const float (&p)[KU / 4], float unit) const {
@@ -433,11 +458,11 @@ struct Unit8 {
     const int far = kFirst + col * kRun + dt * NP / 8 * 8, near = (col & 7) ^ (dt * NP % 8);
     if constexpr (KU == 64) {
       const u32x4 v = lds[far + (near ^ grp)];
-      x = p.t[0].times(Weights<NT>::codes(v.x, v.y), x);
-      x = p.t[1].times(Weights<NT>::codes(v.z, v.w), x);
+      x = p.t[0].times(Weight::codes(v.x, v.y), x);
+      x = p.t[1].times(Weight::codes(v.z, v.w), x);
     } else {
       const uint2 v = reinterpret_cast<const uint2*>(lds + far + (near ^ (grp >> 1)))[grp & 1];
-      x = p.t[0].times(Weights<NT>::codes(v.x, v.y), x);
+      x = p.t[0].times(Weight::codes(v.x, v.y), x);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] *= p.scale;
