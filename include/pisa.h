@@ -527,10 +527,12 @@ int pisa_draft_layout(int32_t B, int32_t T, const int32_t* parents, int32_t n, u
  * hold drafted rows alone, contribute nothing; distinct entries in any order.  mask:
  * [B, Nq, W] words of pisa_draft_layout, or any others (bits from Nq on are not read);
  * mask_bstride words lie between two sequences, 0 shares one mask among the batch.
- * Rows that nothing selects or masks in are hidden whatever their values.  Writes o
- * [B, H, Nq, d] and lse (nullable); a row that sees nothing gets o = 0 and lse = -inf.
- * Sums in fp32.  Weights meet bf16 values as two bf16 terms (off by 2^-16), 8-bit ones
- * as two fp16 terms (2^-22), in fp32 problems as they are.  Nq <= PISA_DRAFT_MAX; N = Nq is an empty cache.
+ * Rows that nothing selects or masks in are hidden whatever their values; an infinite
+ * value that a row sees stays infinite in o (with a weight of 2^-64 of the row's largest
+ * or more; below that it may become NaN).  Writes o [B, H, Nq, d] and lse (nullable); a
+ * row that sees nothing gets o = 0 and lse = -inf.  Sums in fp32.  Weights meet bf16
+ * values as two bf16 terms (off by 2^-16), 8-bit ones as two fp16 terms (2^-22), in fp32
+ * problems as they are.  Nq <= PISA_DRAFT_MAX; N = Nq is an empty cache.
  * o, lse and the workspace must not overlap anything else (PISA_ERR_INVALID_ARG).  The
  * workspace's size does not depend on N: one serves a cache that grows. */
 size_t pisa_draft_attn_workspace_bytes(const pisa_problem* p);

@@ -228,7 +228,9 @@ struct Unit16 {
   // The weights p of this lane's keys, times `unit`, as operands, and the values' sums
   // of dimension tile dt for them.  Two bf16 terms for a weight: with one the result was
   // 1.25 times as far from the exact one as its rounding (2.1e-3 and 1.7e-3 relative, 64
-  // tokens of 16 heads on 4), for 3% less time.
+  // tokens of 16 heads on 4), for 3% less time.  The first term is the largest one below
+  // the weight, so that the second is above 0 too and an infinite value stays what it is
+  // (a second term of 0, or of the other sign, would make it NaN).
   struct Operand {
     bf16x8a t[2];
   };
@@ -237,8 +239,9 @@ struct Unit16 {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float x = unit == 1.f ? p[2 * i] : p[2 * i] * unit, y = unit == 1.f ? p[2 * i + 1] : p[2 * i + 1] * unit;
-      w0[i] = pack2_bf16(x, y);
-      w1[i] = pack2_bf16(x - __uint_as_float(w0[i] << 16), y - __uint_as_float(w0[i] & 0xFFFF0000u));
+      const uint32_t xb = __builtin_elementwise_sub_sat(__float_as_uint(x), 1u), yb = __builtin_elementwise_sub_sat(__float_as_uint(y), 1u);
+      w0[i] = __builtin_amdgcn_perm(yb, xb, 0x07060302u);
+      w1[i] = pack2_bf16(x - __uint_as_float(xb & 0xFFFF0000u), y - __uint_as_float(yb & 0xFFFF0000u));
     }
     return {{u4_as_bf16x8(make_uint4(w0[0], w0[1], w0[2], w0[3])), u4_as_bf16x8(make_uint4(w1[0], w1[1], w1[2], w1[3]))}};
   }
