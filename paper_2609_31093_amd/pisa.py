@@ -653,40 +653,52 @@ class _Norm(QKNorm):
     """A pisa_qk_norm that keeps its weights alive."""
 
 
-def make_qk_norm(r: Rope, q_weight=None, k_weight=None, eps=1e-6, offset=0.0):
-    """A pisa_qk_norm for rotations like r; the weights are [d] on the current device, bf16 or float32 (both alike), or
-    None for all ones."""
-    given = [w for w in (q_weight, k_weight) if w is not None]
-    dt = given[0].dtype if given else torch.float32
+def _norm_weights(weights, r: Rope):
+    """(q_weight, k_weight, weight_dtype) of a pisa_qk_norm, as the weights are now."""
+    given = [w for w in weights if w is not None]
+    dt, dev = given[0].dtype if given else torch.float32, _device()
     if dt not in _DTYPES:
         raise ValueError(f"weights are bfloat16 or float32, got {dt}")
-    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+    for w, name in zip(weights, ("q_weight", "k_weight")):
         if w is not None:
-            _take(w, name, dt, (r.d,), _device())
-    m = _Norm(_ptr(q_weight), _ptr(k_weight), _DTYPES[dt], 0, eps, offset)
-    m.weights, m.place = (q_weight, k_weight), (_device(), r.d) if given else None
+            _take(w, name, dt, (r.d,), dev)
+    return _ptr(weights[0]), _ptr(weights[1]), _DTYPES[dt]
+
+
+def make_qk_norm(r: Rope, q_weight=None, k_weight=None, eps=1e-6, offset=0.0):
+    """A pisa_qk_norm for rotations like r; the weights are [d] on the current device, bf16 or float32 (both alike), or
+    None for all ones.  norm_rope_fwd and norm_rope_bwd take them as they are at the call, so a parameter may be cast or
+    get other memory in between."""
+    m = _Norm(*_norm_weights((q_weight, k_weight), r), 0, eps, offset)
+    m.weights = q_weight, k_weight
+    m.seen = _norm_seen(m, r)
     return m
 
 
-def _norm_here(m, r: Rope):
-    if m.place is not None and m.place != (_device(), r.d):
-        raise ValueError(f"the norm's weights are on cuda:{m.place[0]} for heads of {m.place[1]}, the call is on cuda:{_device()} "
-                         f"for heads of {r.d}")
+def _norm_seen(m, r: Rope):
+    """What _norm_weights' answer depends on."""
+    return _device(), r.d, *[None if w is None else (w.data_ptr(), w.dtype, w.shape, w.get_device(), w.is_contiguous()) for w in m.weights]
+
+
+def _norm_now(m, r: Rope):
+    """m with its weights as they are now; in a copy where they changed, m may be in use by another thread's call."""
+    return m if _norm_seen(m, r) == m.seen else QKNorm(*_norm_weights(m.weights, r), 0, m.eps, m.offset)
 
 
 def norm_rope_fwd(r: Rope, m, q, k=None, positions=None, q_out=None, k_out=None, stream=None):
     """Norm each head of q and k (make_qk_norm) and turn them as rope_fwd does, in one pass; tensors and results as
     there."""
+    now = _norm_now(m, r)
+
     def turn(r, q, qs, k, ks, positions, q_out, qos, k_out, kos, stream):
-        pisa_norm_rope_fwd(r, m, q, qs, k, ks, positions, q_out, qos, k_out, kos, stream)
-    _norm_here(m, r)
+        pisa_norm_rope_fwd(r, now, q, qs, k, ks, positions, q_out, qos, k_out, kos, stream)
     return _rope(turn, r, q, k, positions, q_out, k_out, stream)
 
 
 def norm_rope_bwd(r: Rope, m, q, k, d_q_out, d_k_out=None, positions=None, d_q=None, d_k=None, stream=None):
     """The gradients of norm_rope_fwd's inputs and weights from those of its outputs, the inputs q and k as they were:
     (d_q, d_k, d_q_weight, d_k_weight), the weights' in float32 (None where there is no weight or no side)."""
-    _norm_here(m, r)
+    now = _norm_now(m, r)
     if (q is None) != (d_q_out is None) or (k is None) != (d_k_out is None):
         raise ValueError("a side comes with its input and its output's gradient, or with neither")
     dt, dev, like = _TORCH[r.dtype], _device(), q if q is not None else k
@@ -704,7 +716,7 @@ def norm_rope_bwd(r: Rope, m, q, k, d_q_out, d_k_out=None, positions=None, d_q=N
         dw = [x if w else None for x, w in zip(dw.unbind(), want)]
 
     def turn(r, gq, gqs, gk, gks, positions, d_q, dqs, d_k, dks, stream):
-        pisa_norm_rope_bwd(r, m, q, qs, k, ks, gq, gqs, gk, gks, positions, d_q, dqs, d_k, dks, *dw, ws, nb, stream)
+        pisa_norm_rope_bwd(r, now, q, qs, k, ks, gq, gqs, gk, gks, positions, d_q, dqs, d_k, dks, *dw, ws, nb, stream)
     return *_rope(turn, r, d_q_out, d_k_out, positions, d_q, d_k, stream), *dw
 
 
