@@ -582,6 +582,14 @@ def _take(x, name, dtype, shape, device):
     return x
 
 
+def _take_workspace(ws, device):
+    """ws, a caller's workspace: contiguous memory of device number `device`, whatever its type; ValueError otherwise."""
+    if ws.get_device() != device or not ws.is_contiguous():
+        raise ValueError(f"ws: expected a contiguous tensor on the current device (cuda:{device}), got {tuple(ws.shape)} (strides "
+                         f"{ws.stride()}) on {ws.device}")
+    return ws
+
+
 @functools.lru_cache(maxsize=256)
 def _strides(b, h, n):
     return Strides(b, h, n)
@@ -837,6 +845,8 @@ def _draft_attn(entry, workspace_bytes, p: Problem, cache, q, block_idx, k_new, 
     ks, vs = _strided(k_new, "k_new", dt, new, dev), _strided(v_new, "v_new", dt, new, dev)
     shared = mask.dim() == 2
     _take(mask, "mask", torch.int64, (T, W) if shared else (B, T, W), dev)
+    if ws is not None:
+        _take_workspace(ws, dev)
     if o is None or lse is None or ws is None:
         with _on(stream, q.device):
             ws = _workspace(workspace_bytes(p), q.device) if ws is None else ws
@@ -854,7 +864,7 @@ def draft_attn_fwd(p: Problem, q, k, v, block_idx, k_new, v_new, mask, o=None, l
     """Attention of the Nq drafted rows of p over their selected blocks of the N - Nq rows that the cache k, v
     [B, Hkv, Ncap, d] holds, and over the drafted rows k_new, v_new [B, Hkv, Nq, d] (views with a contiguous last dimension)
     of their mask (draft_layout's, or one [Nq, W] for the batch).  Returns (o, lse), allocated with the workspace where not
-    given."""
+    given (ws: a contiguous tensor of any type, at an address that is a multiple of 256)."""
     dev, dt, shape = _device(), _TORCH[p.dtype], (p.B, p.Hkv, p.Ncap or p.N, p.d)
     _take(k, "k", dt, shape, dev)
     _take(v, "v", dt, shape, dev)
