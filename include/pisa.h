@@ -500,8 +500,12 @@ int pisa_qcache_attn_fwd(const pisa_problem* p, const pisa_qcache* c, const void
  *   pisa_draft_layout       masks, and positions for pisa_rope_fwd or pisa_norm_rope_fwd,
  *                           from the parents
  *   pisa_select, pisa_select_flat_bsa
- *                           as for T rows after n: those blocks that hold drafted
- *                           rows are forced, so that neither call reads them (T <= C)
+ *                           with causal = 1, and for at most C rows a call: the blocks
+ *                           that hold their drafted rows are then forced, and neither
+ *                           call reads nodes or keys of these.  More than C rows are
+ *                           taken in groups of C, each in a call of its own with
+ *                           Nq = its rows and N = n + Nq; in one call blocks of drafted
+ *                           rows would be ranked from nodes that nobody wrote
  *   pisa_draft_attn_fwd, pisa_qcache_draft_attn_fwd
  *   pisa_cache_append_rows, pisa_qcache_append_rows
  *                           the accepted rows, with a problem of N = n + accepted */

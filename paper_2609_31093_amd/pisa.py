@@ -582,6 +582,14 @@ def _take(x, name, dtype, shape, device):
     return x
 
 
+def _take_pyramid(p, pyramid, device):
+    """pyramid, one of problem p's layout on device number `device`; ValueError otherwise."""
+    _take(pyramid, "pyramid", torch.float32, (p.B, p.Hkv, pyramid.shape[2] if pyramid.dim() == 4 else 0, p.d), device)
+    if pyramid.numel() * 4 != pisa_pyramid_bytes(p):
+        raise ValueError(f"pyramid: {tuple(pyramid.shape)} does not fit {p}")
+    return pyramid
+
+
 def _take_workspace(ws, device):
     """ws, a caller's workspace: contiguous memory of device number `device`, whatever its type; ValueError otherwise."""
     if ws.get_device() != device or not ws.is_contiguous():
@@ -799,9 +807,7 @@ def qcache_append(p: Problem, cache: QCache, k_new, v_new, n_old: int, pyramid=N
     shape, dt, dev = (p.B, p.Hkv, p.N - n_old, p.d), _TORCH[p.dtype], cache.device
     ks, vs = _strided(k_new, "k_new", dt, shape, dev), _strided(v_new, "v_new", dt, shape, dev)
     if pyramid is not None:
-        _take(pyramid, "pyramid", torch.float32, (p.B, p.Hkv, pyramid.shape[2], p.d), dev)
-        if pyramid.numel() * 4 != pisa_pyramid_bytes(p):
-            raise ValueError(f"pyramid: {tuple(pyramid.shape)} does not fit {p}")
+        _take_pyramid(p, pyramid, dev)
     pisa_qcache_append(p, cache, k_new, ks, v_new, vs, n_old, pyramid, stream)
 
 
@@ -835,6 +841,34 @@ def draft_layout(parents, n: int, stream=None):
         positions = torch.empty((B, T), dtype=torch.int32, device=parents.device)
     pisa_draft_layout(B, T, parents, n, mask, positions, stream)
     return _results(stream, mask, positions)
+
+
+def draft_select(p: Problem, q, pyramid, k=None, stream=None):
+    """The blocks of the Nq drafted rows of p after N - Nq cached ones, int32 [B, Hkv, Nq, K]: pisa_select's, or without the
+    cache's keys k pisa_select_flat_bsa's.  The pyramid and k [B, Hkv, Ncap, d] hold the cached rows alone.  A causal call
+    leaves nodes and keys of drafted rows unread while there are at most C of these, so more are taken in groups of C, each
+    as if it came directly after the cached rows (a row's previous and own block are those of its place in the group)."""
+    if not p.causal:
+        raise ValueError("drafted rows' blocks are chosen by a causal problem: otherwise none of them is left unread")
+    dev, n, T, C = _device(), p.N - p.Nq, p.Nq, p.C
+    dt, kv = _TORCH[p.dtype], (p.B, p.Hkv, p.Ncap or p.N, p.d)
+    _take(q, "q", dt, (p.B, p.H, T, p.d), dev)
+    _take_pyramid(p, pyramid, dev)
+    if k is not None:
+        _take(k, "k", dt, kv, dev)
+
+    def group(pg, qg):
+        return select_flat_bsa(pg, qg, pyramid, stream) if k is None else select(pg, qg, k, pyramid, stream=stream)
+    if T <= C:
+        return group(p, q)
+    with _on(stream, q.device):  # the copies too
+        idx = torch.empty((p.B, p.Hkv, T, p.K), dtype=torch.int32, device=q.device)
+        for i in range(0, T, C):
+            pg = Problem.from_buffer_copy(p)
+            pg.Nq, pg.Ncap = min(C, T - i), kv[2]
+            pg.N = n + pg.Nq
+            idx[:, :, i:i + C] = group(pg, q[:, :, i:i + C].contiguous())
+    return _results(stream, idx)
 
 
 def _draft_attn(entry, workspace_bytes, p: Problem, cache, q, block_idx, k_new, v_new, mask, o, lse, ws, stream, dev):
@@ -887,9 +921,7 @@ def _append_args(p: Problem, k_new, v_new, rows, n_old, pyramid, dev):
     if rows is not None:
         _take(rows, "rows", torch.int32, (p.B, p.N - n_old), dev)
     if pyramid is not None:
-        _take(pyramid, "pyramid", torch.float32, (p.B, p.Hkv, pyramid.shape[2], p.d), dev)
-        if pyramid.numel() * 4 != pisa_pyramid_bytes(p):
-            raise ValueError(f"pyramid: {tuple(pyramid.shape)} does not fit {p}")
+        _take_pyramid(p, pyramid, dev)
     return ks, vs, n_rows
 
 

@@ -1,0 +1,119 @@
+"""Blocks of drafted rows, whose pyramid and keys end with the cached ones: at most C rows reach a selection at once, and
+nothing that the cached rows did not write is read."""
+import numpy as np
+import pytest
+import torch
+
+pisa = pytest.importorskip("paper_2609_31093_amd.pisa", reason="libpisa.so not built")
+
+
+def problem(B, H, Hkv, T, n, d, C, g, K, dtype="bf16", room=0, causal=1):
+    return pisa.make_problem(B, H, Hkv, T, n + T, d, C, g, K, causal, dtype, Ncap=n + T + room if room else 0)
+
+
+# ------------------------------------------------------------ what is called, without a GPU ---
+
+@pytest.mark.parametrize("flat", [True, False])
+@pytest.mark.parametrize("T,room", [(1, 0), (31, 5), (32, 0), (33, 7), (100, 0), (128, 64)])
+def test_groups(monkeypatch, flat, T, room):
+    B, H, Hkv, n, d, C, K = 2, 4, 2, 77, 64, 32, 5
+    p = problem(B, H, Hkv, T, n, d, C, 2, K, room=room)
+    q = torch.randn(B, H, T, d).bfloat16()
+    pyr = torch.zeros((B, Hkv, pisa.pisa_pyramid_layout(p)[1], d))
+    k = torch.zeros((B, Hkv, p.Ncap or p.N, d), dtype=torch.bfloat16)
+    seen = []
+
+    def entry(pg, qg, *a):
+        idx = a[1] if flat else a[2]
+        assert a[0] is pyr if flat else (a[0] is k and a[1] is pyr)
+        assert pg.Nq <= C and pg.N == n + pg.Nq and (pg.Ncap or pg.N) == (p.Ncap or p.N)
+        assert (pg.B, pg.H, pg.Hkv, pg.d, pg.C, pg.K, pg.causal) == (B, H, Hkv, d, C, K, 1)
+        assert pisa.pisa_pyramid_bytes(pg) == pyr.nbytes and qg.is_contiguous() and qg.shape == (B, H, pg.Nq, d)
+        seen.append(qg.clone())
+        idx.copy_(100 * len(seen) + torch.arange(idx.numel()).view_as(idx) % 97)
+        seen[-1].idx = idx.clone()
+
+    monkeypatch.setattr(pisa, "_device", lambda: -1)
+    monkeypatch.setattr(pisa, "_stream", lambda stream: 0)
+    monkeypatch.setattr(pisa, "pisa_select_flat_bsa" if flat else "pisa_select", entry)
+    idx = pisa.draft_select(p, q, pyr) if flat else pisa.draft_select(p, q, pyr, k)
+    assert len(seen) == -(-T // C)
+    assert torch.equal(torch.cat(seen, 2), q) and torch.equal(torch.cat([x.idx for x in seen], 2), idx)
+    assert (p.Nq, p.N, p.Ncap) == (T, n + T, n + T + room if room else 0)
+
+
+def test_refusals(monkeypatch):
+    monkeypatch.setattr(pisa, "_device", lambda: -1)
+    p = problem(1, 2, 1, 40, 100, 64, 32, 2, 5)
+    q, pyr = torch.zeros((1, 2, 40, 64), dtype=torch.bfloat16), torch.zeros((1, 1, pisa.pisa_pyramid_layout(p)[1], 64))
+    k = torch.zeros((1, 1, 140, 64), dtype=torch.bfloat16)
+    for bad in (dict(p=problem(1, 2, 1, 40, 100, 64, 32, 2, 5, causal=0)), dict(q=q[:, :, :39]), dict(q=q.float()), dict(pyr=pyr[:, :, :-1]),
+                dict(pyr=pyr.bfloat16()), dict(pyr=pyr[0]), dict(k=k[:, :, :100]), dict(k=k.float())):
+        a = {**dict(p=p, q=q, pyr=pyr, k=k), **bad}
+        with pytest.raises(ValueError):
+            pisa.draft_select(a["p"], a["q"], a["pyr"], a["k"])
+
+
+# ------------------------------------------------------------ results ---
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("flat", [True, False])
+@pytest.mark.parametrize("B,H,Hkv,T,n,d,C,g,K,dtype,room", [
+    (1, 2, 2, 32, 640, 64, 32, 2, 5, "bf16", 0),       # a block of drafts alone
+    (2, 4, 2, 33, 1000, 64, 32, 2, 4, "bf16", 9),      # one row more than a block
+    (1, 4, 1, 200, 1024, 128, 64, 2, 6, "f32", 0),     # the cached tokens fill the pyramid's last level
+    (2, 8, 2, 300, 2047, 64, 32, 4, 3, "bf16", 40),
+    (1, 8, 8, 1024, 500, 128, 64, 2, 16, "bf16", 0),   # more drafted rows than cached ones
+    (1, 2, 1, 100, 5, 64, 32, 2, 3, "f32", 0),
+    (1, 2, 1, 70, 0, 64, 32, 2, 3, "bf16", 0),         # nothing cached
+])
+def test_only_cached_rows_are_read(flat, B, H, Hkv, T, n, d, C, g, K, dtype, room):
+    import oracle as O
+
+    p = problem(B, H, Hkv, T, n, d, C, g, K, dtype, room)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    kind = torch.bfloat16 if dtype == "bf16" else torch.float32
+    q = torch.randn((B, H, T, d), generator=gen, device="cuda").to(kind)
+    k = torch.full((B, Hkv, p.Ncap or p.N, d), float("nan"), device="cuda", dtype=kind)
+    k[:, :, :n] = torch.randn((B, Hkv, n, d), generator=gen, device="cuda").to(kind)
+    pyr = torch.full((B, Hkv, pisa.pisa_pyramid_layout(p)[1], d), float("nan"), device="cuda")
+    if n:
+        pisa.pisa_build_pyramid(pisa.make_problem(B, H, Hkv, 1, n, d, C, g, K, 1, dtype, Ncap=p.Ncap or p.N), k, pyr)
+    idx = pisa.draft_select(p, q, pyr) if flat else pisa.draft_select(p, q, pyr, k)
+    for fill in (0.0, 9.0, -50.0):
+        held = torch.nan_to_num(pyr, fill), torch.nan_to_num(k, fill)
+        again = pisa.draft_select(p, q, held[0]) if flat else pisa.draft_select(p, q, *held)
+        assert torch.equal(idx, again)
+
+    # each group against the oracle, for which its rows follow the cached ones
+    got, q64, k64 = idx.cpu().numpy(), q.double().cpu().numpy(), k.double().cpu().numpy()
+    sure = 0
+    for i in range(0, T, C):
+        m = min(C, T - i)
+        keys = np.concatenate((k64[:, :, :n], np.zeros((B, Hkv, m, d))), 2)
+        rows = list(range(0, m, max(1, m // 8)))
+        if flat:
+            want, gap = O.select_flat_bsa(q64[:, :, i:i + m], keys, C, K, True, rows=rows)
+        else:
+            want, gap = O.select(q64[:, :, i:i + m], keys, C, g, K, True, rows=rows)
+        wrong = (got[:, :, i:i + m][:, :, rows] != want).any(-1)
+        assert not (wrong & (gap > 1e-3)).any(), (i, np.argwhere(wrong & (gap > 1e-3))[:3])
+        sure += (gap > 1e-3).sum()
+    assert sure > 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("flat", [True, False])
+def test_on_another_stream(flat):
+    B, H, Hkv, T, n, d, C = 1, 4, 2, 100, 3000, 64, 32
+    p = problem(B, H, Hkv, T, n, d, C, 2, 6)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    k = torch.randn((B, Hkv, n + T, d), generator=gen, device="cuda").bfloat16()
+    pyr, side = pisa.build_pyramid(p, k), torch.cuda.Stream()
+    for i in range(4):
+        q = torch.randn((B, H, T, d), generator=gen, device="cuda").bfloat16()
+        want = pisa.draft_select(p, q, pyr) if flat else pisa.draft_select(p, q, pyr, k)
+        torch.cuda.synchronize()
+        got = pisa.draft_select(p, q, pyr, None if flat else k, stream=side)
+        side.synchronize()
+        assert torch.equal(got, want)
