@@ -177,8 +177,8 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(RopeArgs a, NormArgs m) 
     const float r = rsqrtf(row_sum<UNITS>(sum) * (1.f / D) + m.eps);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      lo[j] *= r * wlo[j];
-      hi[j] *= r * whi[j];
+      lo[j] = lo[j] * r * wlo[j];  // (r w may be past fp32's range where x r w is not)
+      hi[j] = hi[j] * r * whi[j];
     }
     turn<LAY>(lo, hi, c, s);
     store16<LAY>(row_out<T>(io, b, h, n), at, lo, hi);
@@ -253,16 +253,17 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && LAY != kMixed ? 3 : 2) void 
     turn<LAY>(ulo, uhi, c, s);
     float sum = 0.f, dot = 0.f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      sum += lo[j] * lo[j] + hi[j] * hi[j];
-      dot += ulo[j] * wlo[j] * lo[j] + uhi[j] * whi[j] * hi[j];
-    }
+    for (int j = 0; j < 8; ++j) sum += lo[j] * lo[j] + hi[j] * hi[j];
     const float r = rsqrtf(row_sum<UNITS>(sum) * (1.f / D) + m.eps);
-    const float along = row_sum<UNITS>(dot) * r * (1.f / D);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int j = 0; j < 8; ++j) {  // (u w x may be past fp32's range where u w x r is not)
       lo[j] *= r;
       hi[j] *= r;
+      dot += ulo[j] * wlo[j] * lo[j] + uhi[j] * whi[j] * hi[j];
+    }
+    const float along = row_sum<UNITS>(dot) * (1.f / D);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
       dlo[j] = fmaf(ulo[j], lo[j], dlo[j]);
       dhi[j] = fmaf(uhi[j], hi[j], dhi[j]);
       lo[j] = r * (ulo[j] * wlo[j] - lo[j] * along);
