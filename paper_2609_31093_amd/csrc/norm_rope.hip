@@ -53,12 +53,6 @@ struct Slots {
   __device__ __forceinline__ int hi_at(int j) const { return hi + j; }
 };
 
-template <typename T>
-__device__ __forceinline__ float value(T x) {
-  if constexpr (sizeof(T) == 2) return bf16_to_f32(x);
-  else return x;
-}
-
 template <int LAY, typename T>
 __device__ __forceinline__ void load16(const T* p, const Slots<LAY>& s, float (&lo)[8], float (&hi)[8]) {
   load8(p + s.lo, lo);
