@@ -762,7 +762,7 @@ int run_draft_attn(const pisa_problem* p, const pisa::Shape& s, pisa::DraftAttn 
 // Whichever sides a call has.
 size_t norm_rope_ws(const pisa_rope* r) {
   const bool bf16 = r->dtype == PISA_DTYPE_BF16;
-  auto bytes = [&](int H, int Hkv) { return pisa::norm_rope_bwd_ws(r->B, r->N, H, Hkv, r->d, bf16); };
+  auto bytes = [&](int H, int Hkv) { return pisa::norm_rope_bwd_ws(r->B, r->N, H, Hkv, r->d, r->rot, bf16, r->layout == PISA_ROPE_HALF); };
   return std::max({bytes(r->H, r->Hkv), bytes(r->H, 0), bytes(0, r->Hkv)});
 }
 

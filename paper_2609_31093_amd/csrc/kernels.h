@@ -192,7 +192,7 @@ struct NormArgs {
   float eps, offset;
   bool w_bf16;
 };
-size_t norm_rope_bwd_ws(int B, int N, int H, int Hkv, int d, bool bf16);  // H or Hkv 0: that side is left out
+size_t norm_rope_bwd_ws(int B, int N, int H, int Hkv, int d, int rot, bool bf16, bool half);  // H or Hkv 0: that side is left out
 hipError_t launch_norm_rope(const RopeArgs& a, const NormArgs& m, const RopeSide* dq, const RopeSide* dk, bool bf16, bool half,
                             hipStream_t st);
 

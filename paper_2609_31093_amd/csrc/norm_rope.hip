@@ -30,11 +30,13 @@ namespace {
 // same with the border among a lane's pairs (pairs no multiple of 8).
 constexpr int kPairs = 0, kHalves = 1, kMixed = 2;
 
+bool mixed_pairs(bool half, int rot) { return half && rot % 16 != 0; }
+
 // Where a lane's values are: dimensions lo .. lo + 7 and hi .. hi + 7.  The lane with
 // the border (kMixed) has r < 8 pairs; its `hi` runs on into the dimensions behind the
 // rotated ones, and its `lo` has from value r on those that follow, lo2 + r ...
 // lo2 + 7.  So three runs are loaded and one value chosen from two (131072 rows of 16
-// heads: 333 us, 192 without a border; each value loaded on its own 782).
+// heads: 308 us, 192 without a border; each value loaded on its own 782).
 template <int LAY>
 struct Slots {
   int lo, hi, lo2, r, p0;
@@ -147,7 +149,8 @@ __device__ __forceinline__ void lane_angles(const RopeArgs& a, int b, int n, int
 
 }  // namespace
 
-// Workgroups (rows, heads): 256 threads take 256 / UNITS rows.
+// Workgroups (rows, heads): 256 threads take 256 / UNITS rows; bf16 kMixed ones go on to
+// others.
 template <typename T, int D, int LAY>
 __global__ __launch_bounds__(256) void norm_rope_kernel(RopeArgs a, NormArgs m) {
   constexpr int UNITS = D / 16, ROWS = 256 / UNITS;
@@ -157,26 +160,28 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(RopeArgs a, NormArgs m) 
   const RopeSide& io = heads.is_q ? a.q : a.k;
   float wlo[8], whi[8];
   load_weights<LAY>(m, heads.is_q ? m.q_weight : m.k_weight, at, wlo, whi);
-  const int row = static_cast<int>(blockIdx.x) * ROWS + threadIdx.x / UNITS;
+  int row = static_cast<int>(blockIdx.x) * ROWS + threadIdx.x / UNITS;
   if (row >= a.B * a.N) return;
-  const int b = row / a.N, n = row - b * a.N;
-  float c[8], s[8];
-  lane_angles(a, b, n, 8 * u, pairs, c, s);
-  for (int h = heads.first; h < heads.end; ++h) {
-    float lo[8], hi[8];
-    load16<LAY>(row_in<T>(io, b, h, n), at, lo, hi);
-    float sum = 0.f;
+  do {
+    const int b = row / a.N, n = row - b * a.N;
+    float c[8], s[8];
+    lane_angles(a, b, n, 8 * u, pairs, c, s);
+    for (int h = heads.first; h < heads.end; ++h) {
+      float lo[8], hi[8];
+      load16<LAY>(row_in<T>(io, b, h, n), at, lo, hi);
+      float sum = 0.f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sum += lo[j] * lo[j] + hi[j] * hi[j];
-    const float r = rsqrtf(row_sum<UNITS>(sum) * (1.f / D) + m.eps);
+      for (int j = 0; j < 8; ++j) sum += lo[j] * lo[j] + hi[j] * hi[j];
+      const float r = rsqrtf(row_sum<UNITS>(sum) * (1.f / D) + m.eps);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      lo[j] = lo[j] * r * wlo[j];  // (r w may be past fp32's range where x r w is not)
-      hi[j] = hi[j] * r * whi[j];
+      for (int j = 0; j < 8; ++j) {
+        lo[j] = lo[j] * r * wlo[j];  // (r w may be past fp32's range where x r w is not)
+        hi[j] = hi[j] * r * whi[j];
+      }
+      turn<LAY>(lo, hi, c, s);
+      store16<LAY>(row_out<T>(io, b, h, n), at, lo, hi);
     }
-    turn<LAY>(lo, hi, c, s);
-    store16<LAY>(row_out<T>(io, b, h, n), at, lo, hi);
-  }
+  } while (LAY == kMixed && sizeof(T) == 2 && (row += static_cast<int>(gridDim.x) * ROWS) < a.B * a.N);
 }
 
 // A lane's 16 values of a row as they lie in memory.
@@ -203,14 +208,17 @@ struct Raw16 {
   }
 };
 
+// Workgroups of the gradients that a CU holds at once, by their registers (four spill).
+constexpr int held(bool bf16, bool mixed) { return bf16 && !mixed ? 3 : 2; }
+
 // The next head's values are on their way while one is worked on (without: 139 us for
-// 30011 rows of 20 heads, with 95), which takes the registers of three wavefronts on a
-// SIMD in bf16, two in fp32 (at four they spill).  The weights'
+// 30011 rows of 20 heads, with 95), which takes the registers of held() wavefronts on a
+// SIMD.  The weights'
 // gradients: each thread sums its rows', then the workgroup's meet in LDS, and
 // norm_rope_weights_kernel adds the workgroups' in their order.
 template <typename T, int D, int LAY>
-__global__ __launch_bounds__(256, sizeof(T) == 2 && LAY != kMixed ? 3 : 2) void norm_rope_bwd_kernel(RopeArgs a, NormArgs m,
-                                                                                                  RopeSide dq, RopeSide dk) {
+__global__ __launch_bounds__(256, held(sizeof(T) == 2, LAY == kMixed)) void norm_rope_bwd_kernel(RopeArgs a, NormArgs m,
+                                                                                              RopeSide dq, RopeSide dk) {
   constexpr int UNITS = D / 16, ROWS = 256 / UNITS;
   __shared__ float part[4][D];
   const int u = threadIdx.x % UNITS, pairs = a.rot / 2;
@@ -336,7 +344,7 @@ namespace {
 struct Grid {
   int heads, gx, gq, gk;
 };
-Grid grid_of(int B, int N, int H, int Hkv, int d, bool bf16, bool bwd) {
+Grid grid_of(int B, int N, int H, int Hkv, int d, bool bf16, bool mixed, bool bwd) {
   const int64_t rows = static_cast<int64_t>(B) * N, groups = (rows * (d / 16) + 255) / 256;
   Grid g{};
   g.heads = groups * (H + Hkv) >= 4 * 1024 ? 4 : groups * (H + Hkv) >= 2 * 1024 ? 2 : 1;
@@ -344,11 +352,15 @@ Grid grid_of(int B, int N, int H, int Hkv, int d, bool bf16, bool bwd) {
   g.gk = (Hkv + g.heads - 1) / g.heads;
   g.gx = static_cast<int>(groups);
   // gradients: as few workgroups (and parts of the weights' sums) as the device holds
-  // at once, three (fp32: two) on each CU, each the same number of rows (20 heads at
-  // 30011 rows, bf16: 640 workgroups 108 us, 768 100, 1024 110, 4096 109)
+  // at once, each the same number of rows (20 heads at 30011 rows, bf16: 640 workgroups
+  // 108 us, 768 100, 1024 110, 4096 109; kMixed 512 130 us, 768 136)
   if (bwd) {
-    const int64_t most = 256 * (bf16 ? 3 : 2), rounds = (groups * (g.gq + g.gk) + most - 1) / most;
+    const int64_t most = 256 * held(bf16, mixed), rounds = (groups * (g.gq + g.gk) + most - 1) / most;
     g.gx = static_cast<int>((groups + rounds - 1) / rounds);
+  } else if (mixed && bf16) {
+    // workgroups that go on to other rows (131072 rows of 16 heads: 308 us, with a row to
+    // a lane group 334; fp32 710 and 706)
+    g.gx = static_cast<int>(std::min<int64_t>(groups, std::max(1, 4096 / (g.gq + g.gk))));
   }
   return g;
 }
@@ -376,20 +388,20 @@ template <typename T, int D>
 hipError_t launch_layout(const RopeArgs& a, const NormArgs& m, const RopeSide* dq, const RopeSide* dk, const Grid& g, bool half,
                          hipStream_t st) {
   if (!half) return launch<T, D, kPairs>(a, m, dq, dk, g, st);
-  return a.rot % 16 == 0 ? launch<T, D, kHalves>(a, m, dq, dk, g, st) : launch<T, D, kMixed>(a, m, dq, dk, g, st);
+  return !mixed_pairs(half, a.rot) ? launch<T, D, kHalves>(a, m, dq, dk, g, st) : launch<T, D, kMixed>(a, m, dq, dk, g, st);
 }
 
 }  // namespace
 
-size_t norm_rope_bwd_ws(int B, int N, int H, int Hkv, int d, bool bf16) {
-  const Grid g = grid_of(B, N, H, Hkv, d, bf16, true);
+size_t norm_rope_bwd_ws(int B, int N, int H, int Hkv, int d, int rot, bool bf16, bool half) {
+  const Grid g = grid_of(B, N, H, Hkv, d, bf16, mixed_pairs(half, rot), true);
   return static_cast<size_t>(g.gx) * (g.gq + g.gk) * d * sizeof(float);
 }
 
 hipError_t launch_norm_rope(const RopeArgs& args, const NormArgs& m, const RopeSide* dq, const RopeSide* dk, bool bf16, bool half,
                             hipStream_t st) {
   RopeArgs a = args;
-  const Grid g = grid_of(a.B, a.N, a.H, a.HH - a.H, a.d, bf16, dq != nullptr);
+  const Grid g = grid_of(a.B, a.N, a.H, a.HH - a.H, a.d, bf16, mixed_pairs(half, a.rot), dq != nullptr);
   a.heads = g.heads;
   if (bf16)
     return a.d == 128 ? launch_layout<uint16_t, 128>(a, m, dq, dk, g, half, st) : launch_layout<uint16_t, 64>(a, m, dq, dk, g, half, st);
