@@ -994,14 +994,19 @@ int unit_keys(const Shape& s, bool q8) {
 }
 
 // How a tile's units are spread: over the wavefronts of a workgroup, and workgroups.
-// A CU holds eight of these wavefronts (twelve in bf16 of 64 dimensions); beyond that
-// they only share units more finely.  Otherwise a unit to a wavefront is best, with
-// as many to spare as rows may want other blocks, up to 64 and where that is much more
-// than one workgroup can do: the second launch that joins workgroups costs what 32 units
-// of bf16 and 64 dimensions do in eight wavefronts (12 units of 64 dimensions, 118
+// A SIMD holds two of these wavefronts (three in bf16 of 64 dimensions), so a CU one
+// workgroup of five to eight, or two (three) of up to four.  With more tiles than CUs
+// they are of four at most (bf16 of 128 dimensions, 32 heads on 2, 400 tiles: 16.4 us,
+// seven 22; 64 dimensions, 280 tiles: 11.7, eight 14.6), and share units more finely
+// where the device does not hold them at once.  Otherwise a unit to a wavefront is best,
+// with as many to spare as rows may want other blocks, up to 64 and where that is much
+// more than one workgroup can do: the second launch that joins workgroups costs what 32
+// units of bf16 and 64 dimensions do in eight wavefronts (12 units of 64 dimensions, 118
 // tiles: 8.0 us in one workgroup, 10.6 in two; 50 of 128, 8 tiles: 34 in one, 12.2 in
 // eight of eight wavefronts, 11.4 in sixteen of four).  Workgroups of four where that
-// leaves at most one to a CU (above), of eight elsewhere (64 tiles of 32: 13.8 and 15.4).
+// leaves at most one to a CU (above), of eight elsewhere (64 tiles of 32: 13.8 and 15.4),
+// and no more of these than CUs (64 dimensions, 128 tiles of 4 blocks: 12.1 in two each,
+// 16.1 in three).
 struct Spread {
   int ks, splits;
 };
@@ -1027,16 +1032,16 @@ Units units_of(const Shape& s, bool q8, int64_t M) {
 }
 Spread spread(const Shape& s, bool q8) {
   const Units u = units_of(s, q8, (s.N - s.Nq + s.C - 1) / s.C);
+  if (u.tiles > kDeviceCUs) return {static_cast<int>(std::min<int64_t>(u.w, 4)), 1};
   if (!u.split) return {static_cast<int>(std::min<int64_t>(u.w, kMaxWaves)), 1};
   const int ks = u.tiles * ((u.w + 3) / 4) <= kDeviceCUs ? 4 : kMaxWaves;
-  return {ks, static_cast<int>(u.w == u.held ? u.w / ks : (u.w + ks - 1) / ks)};
+  return {ks, static_cast<int>(std::min((u.w + ks - 1) / ks, kDeviceCUs / u.tiles))};
 }
 // Most splits that spread() takes whatever the cache holds, so that one workspace serves
 // a cache that grows.
 int most_splits(const Shape& s, bool q8) {
   const Units u = units_of(s, q8, INT32_MAX);
-  if (!u.split) return 1;
-  return static_cast<int>(std::max(std::min((u.w + 3) / 4, kDeviceCUs / u.tiles), (u.w + kMaxWaves - 1) / kMaxWaves));
+  return u.split ? static_cast<int>(std::max<int64_t>(1, std::min((u.w + 3) / 4, kDeviceCUs / u.tiles))) : 1;
 }
 
 size_t al256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
