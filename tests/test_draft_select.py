@@ -117,3 +117,32 @@ def test_on_another_stream(flat):
         got = pisa.draft_select(p, q, pyr, None if flat else k, stream=side)
         side.synchronize()
         assert torch.equal(got, want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("flat", [True, False])
+def test_captured(flat):
+    """Two graphs of grouped selections, replayed with other queries and eager calls between them."""
+    B, H, Hkv, T, n, d, C = 2, 4, 2, 70, 1500, 64, 32
+    p = problem(B, H, Hkv, T, n, d, C, 2, 6)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    k = torch.randn((B, Hkv, n + T, d), generator=gen, device="cuda").bfloat16()
+    pyr, q = pisa.build_pyramid(p, k), torch.randn((B, H, T, d), generator=gen, device="cuda").bfloat16()
+
+    def call():
+        return pisa.draft_select(p, q, pyr) if flat else pisa.draft_select(p, q, pyr, k)
+    call()
+    graphs = []
+    for _ in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = call()
+        graphs.append((graph, out))
+    for _ in range(4):
+        q.copy_(torch.randn((B, H, T, d), generator=gen, device="cuda"))
+        want = call()
+        torch.cuda.synchronize()
+        for graph, out in graphs:
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, want)
