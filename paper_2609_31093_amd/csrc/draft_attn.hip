@@ -23,11 +23,13 @@
 // multiplied as qcache_attn.hip does it, with two fp16 terms of a weight.
 //
 // What bounds it: few tokens the chain of latencies (the list 1.2 us, a unit's loads
-// 1.5 and products 1.6, the wavefronts' sums 1.2; 10.9 us with the second launch for 16
-// tokens of 8 heads over 131071 in 8 bits); many the vector instructions of a unit, half
-// of them conversions and the sums' rescaling (256 tokens of 8 heads on 2 over 523776:
-// 37.1 us; with operands straight from the cache, whose scattered pieces a CU takes in
-// at 13 bytes a clock, 48).
+// 1.5 and products 1.6, the wavefronts' sums 1.2; 11.0 us with the second launch for 16
+// tokens of 8 heads over 131071 in 8 bits); many a unit's vector instructions, half of
+// them conversions and the sums' rescaling, and what two wavefronts to a SIMD leave
+// unhidden of its waits (256 tokens of 8 heads on 2 over 523776: 37.1 us, in which the
+// two issue vector instructions in 54% of a SIMD's cycles and each waits in 37% of its
+// own; with operands straight from the cache, whose scattered pieces a CU takes in at 13
+// bytes a clock, 48 before the weights' second term).
 //
 // The running maximum is that of the products before the softmax's scale.  Sums of
 // weights times values are held in units of kUnit, so that values up to the type's
